@@ -13,6 +13,8 @@
  *   cs_encode              the encoder task on one packed, variable-length batch
  *   cs_forward_embeddings  the consumer-side placement of received embedding rows
  *                          into the LLM's input-embedding buffer
+ *   cs_attention_cache     the consumer's attention over a 4-bit cache, with the calls that
+ *                          fill it (cs_qk_norm_rope, cs_cache_write)
  *
  * The paper does not describe the inside of an encoder.  Two towers are built:
  * a Qwen2.5-VL-style vision transformer (RMSNorm, 2-D/3-D rotary, window and
@@ -281,6 +283,106 @@ cs_status cs_channel_forward(cs_channel* ch, int32_t slot, const int64_t* placeh
 cs_status cs_channel_release(cs_channel* ch, int32_t slot, void* stream);
 cs_status cs_channel_describe(cs_channel* ch, int32_t slot, int32_t* state, const void** dev_ptr, int64_t* n_rows,
                               int32_t* hidden, int32_t* dtype, int32_t* arrived);
+
+/* ---- the LLM task's attention over what it received ------------------------------------------------------------
+ * The consumer of the hand-off (Listing 1: the LLM task takes embeddings instead of encoding) runs its layers over
+ * sequences that mix text tokens and the placed rows of images, clips and audio.  The paper says nothing of the inside
+ * of that task; these calls are the attention part of one of its layers, behind the caller's QKV projection
+ * (cs_linear_bf16 or another) and in front of its output projection:
+ *
+ *   cs_qk_norm_rope     queries and keys normed per head and rotated by positions with up to three axes
+ *   cs_cache_write      keys and values quantised to 4 bits into a paged cache
+ *   cs_cache_read       cached rows back as values (a prefix handed on, a check)
+ *   cs_attention_cache  attention of new tokens over the cache: one token, a few drafted ones, chunks of a prompt
+ *
+ * All four enqueue on `stream`, allocate nothing, wait for nothing and read their lengths, slots and positions on the
+ * GPU, so a recorded graph replays them on whatever those arrays hold.  An entry the kernels cannot use (a slot or
+ * page beyond the pool, a position beyond the table, more keys or queries than the host was told) is left out, never
+ * followed, and sets bit 0 of *err_flag (dev int32 or NULL; bits are only ever set).
+ *
+ * Rotation and norm in one pass.  Per row t and head, with the head's values x[head_dim]:
+ *   y = x * gain / sqrt(mean(x^2) + eps)                 (gain NULL: y = x)
+ *   pair j < rotary_dim/2, (c, s) = cos_sin[positions[t, axis(j)], j]:
+ *   out[j] = y[j] c - y[j + rotary_dim/2] s;   out[j + rotary_dim/2] = y[j + rotary_dim/2] c + y[j] s;
+ *   the values behind rotary_dim pass.  Sums in fp32, one rounding to dtype at the end.
+ *  config       host.  axes 1..3; sections[a] pairs follow axis a and sum to rotary_dim/2.  interleaved 0: section after
+ *               section; 1 (three axes, sections[1] and [2] at most a third of the pairs): pair j follows axis j % 3 while
+ *               j < 3 * sections[j % 3], axis 0 otherwise.  head_dim and rotary_dim multiples of 16, head_dim <= 256.
+ *  q, k         dev rows of `dtype`, head h of row t at [t * row + h * head_dim]; parts of one packed QKV row may be passed.
+ *               q_out, k_out may be q, k themselves (same pointer and row), but overlap them in no other way.  Pointers and rows: multiples of 16 bytes.
+ *  q_gain, k_gain  dev fp32 [head_dim], 16-byte aligned, or both NULL
+ *  cos_sin      dev fp32 [n_positions, rotary_dim/2, 2], 16-byte aligned
+ *  positions    dev int32 [n_rows, axes].  A row with a position outside the table is not written and sets *err_flag.
+ * Errors (nothing enqueued): CS_ERR_INVALID_ARG, CS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t n_heads, n_kv_heads;   /* heads of q and of k (either may be 0: the other alone) */
+  int32_t head_dim, rotary_dim;
+  int32_t axes, interleaved;
+  int32_t sections[3];
+  int64_t n_positions;
+  float eps;
+} cs_qk_config;
+cs_status cs_qk_norm_rope(const cs_qk_config* config, const void* q, int64_t q_row, const void* k, int64_t k_row, void* q_out,
+                          int64_t q_out_row, void* k_out, int64_t k_out_row, int32_t dtype, const float* q_gain,
+                          const float* k_gain, const float* cos_sin, const int32_t* positions, int64_t n_rows,
+                          int32_t* err_flag, void* stream);
+
+/* The cache: a pool of n_pages pages in device memory of the caller's, each page_tokens tokens of every key/value head.
+ * Keys and values are held in 4 bits: 32 consecutive values of a head share a power of two 2^e and each is one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0..7; bit 3 is the sign) times it.  With amax the group's largest magnitude,
+ *   e = floor(log2 amax) - 2, one more where amax >= 1.75 * 2^floor(log2 amax), kept within [-125, 125],
+ * and a value becomes the nearest multiple (ties to the even code).  Every step is exact, so what a row is held as is defined
+ * to the bit.  A NaN is held as 0 and an infinity as the largest finite value; both set bit 1 of *err_flag.
+ * 4.25 bits a value.  Layout, with D = head_dim (64 or 128), P = page_tokens (a multiple of 32), NG = D/32: the block of
+ * page p and head h starts at byte (p * n_kv_heads + h) * P * (D + 2 NG) of the pool and holds, byte offsets in it,
+ *   K codes of dims d, d+1 (d even: low bits) of token o:   o D/2 + ((d % 32 / 8) NG + d / 32) 4 + d % 8 / 2
+ *   V codes:  P D/2 + (o / 4) 2 D + d / (D/16) * 4 NG + o % 4 * NG + d % (D/16) / 2
+ *   K scales e + 127 of group g:   P D + o NG + g            V scales:   P (D + NG) + o / 8 * 8 NG + 8 g + o % 8
+ * A slot is a token's place in the pool: page number * page_tokens + token within the page. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t n_kv_heads, head_dim, page_tokens;
+  int64_t n_pages;
+} cs_cache_config;
+/* Host-only: bytes of a page (all heads) and of the pool; either out pointer may be NULL. */
+cs_status cs_cache_query(const cs_cache_config* config, size_t* page_bytes, size_t* pool_bytes);
+/* pool[slots[t]] = quantised (k[t], v[t]).  slots dev int64 [n_rows], -1 skips the row; two rows with one slot are a
+ * caller error (what the slot then holds is a mix of both).  k, v dev rows of `dtype` (CS_BF16 or CS_F32), head h at
+ * [t * row + h * head_dim]; pointers, rows and pool: multiples of 16 bytes. */
+cs_status cs_cache_write(const cs_cache_config* config, void* pool, const void* k, int64_t k_row, const void* v, int64_t v_row,
+                         int32_t dtype, const int64_t* slots, int64_t n_rows, int32_t* err_flag, void* stream);
+/* k[t], v[t] = the values slots[t] holds (exact in either dtype); slot -1, or one beyond the pool, gives zeros. */
+cs_status cs_cache_read(const cs_cache_config* config, const void* pool, const int64_t* slots, int64_t n_rows, void* k, int64_t k_row,
+                        void* v, int64_t v_row, int32_t dtype, int32_t* err_flag, void* stream);
+
+/* Attention over the cache.  Sequence b has the rows [cu_queries[b], cu_queries[b+1]) of q, its newest tokens, and
+ * n_keys[b] keys, theirs included: its query i of nq stands at key n_keys[b] - nq + i.  Key t is in page
+ * page_table[b, t / page_tokens].  out = softmax(scale q k^T) v over the keys of head h / (n_heads / n_kv_heads), up to and
+ * including the query's own (causal) or all (causal 0); a query that sees no key gives zeros.  What lies in a page
+ * behind a sequence's last key may be anything.
+ *  batch       host struct: n_queries = rows of q and out; max_queries, max_keys = the most a sequence has, from which
+ *              the launches are laid out (larger numbers on the GPU are cut to them and set *err_flag; tight ones cost less)
+ *  q, out      dev bf16, head h of row t at [t * row + h * head_dim]; pointers and rows multiples of 16 bytes; out must not overlap q
+ *  workspace   dev, 16-byte aligned, at least what cs_attention_cache_query reports; contents are scratch
+ * Scores, softmax statistics and sums are fp32; probabilities are rounded to bf16 for the second product.  Results are
+ * deterministic, and do not depend on the order of pages. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t n_seqs;
+  int64_t n_queries;
+  int32_t max_queries;
+  int32_t table_width;         /* entries of page_table per sequence */
+  int64_t max_keys;            /* at most 2^30 */
+  const int32_t* cu_queries;   /* dev [n_seqs + 1] */
+  const int32_t* n_keys;       /* dev [n_seqs] */
+  const int32_t* page_table;   /* dev [n_seqs, table_width]; entries behind a sequence's last key are not read */
+} cs_cache_batch;
+/* Host-only (the device pointers of `batch` are not looked at). */
+cs_status cs_attention_cache_query(const cs_cache_config* config, const cs_cache_batch* batch, int32_t n_heads, size_t* workspace_bytes);
+cs_status cs_attention_cache(const cs_cache_config* config, const void* pool, const cs_cache_batch* batch, const void* q, int64_t q_row,
+                             void* out, int64_t out_row, int32_t n_heads, float scale, int32_t causal, void* workspace,
+                             size_t workspace_bytes, int32_t* err_flag, void* stream);
 
 /* cs_xchannel: the same hand-off between TWO PROCESSES on one GPU, as the paper's executors are
  * (separate processes joined by a per-GPU Sidecar, Sec. 2.1 "Data Plane"; the sender writes the tensor

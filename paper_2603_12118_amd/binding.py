@@ -44,6 +44,23 @@ class cs_attention_plan(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_full", "n_tail", "q_per_block", "key_groups", "tail_key_groups")]
 
 
+class cs_qk_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "n_heads", "n_kv_heads", "head_dim", "rotary_dim", "axes", "interleaved")] + [
+        ("sections", C.c_int32 * 3), ("n_positions", C.c_int64), ("eps", C.c_float)]
+
+
+class cs_cache_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32),
+                ("n_pages", C.c_int64)]
+
+
+class cs_cache_batch(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_seqs", C.c_int32), ("n_queries", C.c_int64), ("max_queries", C.c_int32),
+                ("table_width", C.c_int32), ("max_keys", C.c_int64), ("cu_queries", C.c_void_p), ("n_keys", C.c_void_p),
+                ("page_table", C.c_void_p)]
+
+
 class cs_tensor(C.Structure):
     _fields_ = [("name", C.c_char_p), ("data", C.c_void_p), ("numel", C.c_int64)]
 
@@ -99,6 +116,13 @@ def lib() -> C.CDLL:
         L.cs_xchannel_release.argtypes = [vp, C.c_int32]
         L.cs_xchannel_describe.argtypes = [vp, C.c_int32, i32p, C.POINTER(vp), C.POINTER(i64), i32p, i32p,
                                            C.POINTER(i64), C.POINTER(i64)]
+        cfgp, batchp = C.POINTER(cs_cache_config), C.POINTER(cs_cache_batch)
+        L.cs_qk_norm_rope.argtypes = [C.POINTER(cs_qk_config), vp, i64, vp, i64, vp, i64, vp, i64, C.c_int32, vp, vp, vp, vp, i64, vp, vp]
+        L.cs_cache_query.argtypes = [cfgp, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+        L.cs_cache_write.argtypes = [cfgp, vp, vp, i64, vp, i64, C.c_int32, vp, i64, vp, vp]
+        L.cs_cache_read.argtypes = [cfgp, vp, vp, i64, vp, i64, vp, i64, C.c_int32, vp, vp]
+        L.cs_attention_cache_query.argtypes = [cfgp, batchp, C.c_int32, C.POINTER(C.c_size_t)]
+        L.cs_attention_cache.argtypes = [cfgp, vp, batchp, vp, i64, vp, i64, C.c_int32, C.c_float, C.c_int32, vp, C.c_size_t, vp, vp]
         L.cs_mfma_ceiling.argtypes = [vp, C.c_size_t, C.c_int32, C.c_int32, C.POINTER(C.c_double), vp]
         L.cs_encoder_step_kernel.argtypes = [vp, C.c_int32, i64, C.c_char_p, C.c_size_t]
         L.cs_encoder_batch_kernel.argtypes = [vp, C.c_int32, i64, C.c_char_p, C.c_size_t]
@@ -116,7 +140,8 @@ def lib() -> C.CDLL:
                   "cs_channel_acquire", "cs_channel_publish", "cs_channel_forward", "cs_channel_release",
                   "cs_channel_describe", "cs_xchannel_create", "cs_xchannel_open", "cs_xchannel_acquire",
                   "cs_xchannel_publish", "cs_xchannel_wait", "cs_xchannel_forward", "cs_xchannel_release",
-                  "cs_xchannel_describe"):
+                  "cs_xchannel_describe", "cs_qk_norm_rope", "cs_cache_query", "cs_cache_write", "cs_cache_read",
+                  "cs_attention_cache_query", "cs_attention_cache"):
             getattr(L, f).restype = C.c_int
         _lib = L
     return _lib
@@ -495,6 +520,149 @@ def cs_attention_varlen_groups(qk, vt, out, seg_cu: Sequence[int], n_heads: int,
     seg = _i32(seg_cu)
     _check(lib().cs_attention_varlen_groups(qk.data_ptr(), vt.data_ptr(), vt.stride(0), out.data_ptr(), _i32p(seg),
                                             len(seg) - 1, n_heads, head_dim, key_groups, _stream(stream)))
+
+
+# ---- the LLM task's attention: tensors of heads are [rows, heads, head_dim] with packed heads; rows may lie apart
+def _dtype_code(x) -> int:
+    import torch
+    if x.dtype == torch.bfloat16:
+        return CS_BF16
+    if x.dtype == torch.float32:
+        return CS_F32
+    raise TypeError("rows must be bf16 or fp32")
+
+
+def _head_rows(x, name: str):
+    """-> (pointer, elements between rows) of [rows, heads, head_dim]"""
+    rows, heads, dim = x.shape
+    sr, sh, sd = x.stride()
+    if x.device.type != "cuda" or sd != 1 or (heads > 1 and sh != dim):
+        raise ValueError(f"{name}: heads of a row must be packed, on the GPU")
+    return x.data_ptr(), sr if rows > 1 else heads * dim
+
+
+def _dev(x, dtype, name: str, shape=None):
+    if x.device.type != "cuda" or x.dtype != dtype or not x.is_contiguous() or (shape is not None and tuple(x.shape) != shape):
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor on the GPU" + (f" of shape {shape}" if shape is not None else ""))
+    return x.data_ptr()
+
+
+def _empty(shape, dtype, device, stream):
+    """A new tensor of the stream the call runs on (the current one unless given), so that its memory is free there."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _flag(err_flag):
+    import torch
+    return None if err_flag is None else _dev(err_flag, torch.int32, "err_flag", (1,))
+
+
+def cs_qk_norm_rope(q, k, cos_sin, positions, sections, q_gain=None, k_gain=None, eps: float = 1e-6, interleaved: bool = False,
+                    q_out=None, k_out=None, err_flag=None, stream=None):
+    """Queries [T, heads, head_dim] and keys [T, kv_heads, head_dim] (parts of one packed QKV tensor, say) normed per head where
+    gains (fp32 [head_dim]) are given, and rotated: cos_sin fp32 [n_positions, pairs, 2], positions int32 [T, axes],
+    `sections` pairs per axis.  Returns (q_out, k_out), new tensors unless given (q, k themselves to work in place)."""
+    import torch
+    T, H, D = q.shape
+    K = k.shape[1]
+    if tuple(k.shape) != (T, K, D) or k.dtype != q.dtype:
+        raise ValueError("k: expected the rows, head_dim and type of q")
+    n, half = cos_sin.shape[0], cos_sin.shape[1]
+    if len(sections) > 3:
+        raise ValueError("sections: at most three axes")
+    q_out = _empty((T, H, D), q.dtype, q.device, stream) if q_out is None else q_out
+    k_out = _empty((T, K, D), q.dtype, q.device, stream) if k_out is None else k_out
+    if q_out.shape != q.shape or k_out.shape != k.shape or q_out.dtype != q.dtype or k_out.dtype != q.dtype:
+        raise ValueError("q_out, k_out: expected the shapes and type of q, k")
+    c = cs_qk_config(C.sizeof(cs_qk_config), H, K, D, 2 * half, len(sections), int(interleaved), (C.c_int32 * 3)(*sections), n, eps)
+    f32 = torch.float32
+    qp, qs = _head_rows(q, "q")
+    kp, ks = _head_rows(k, "k")
+    qo, qos = _head_rows(q_out, "q_out")
+    ko, kos = _head_rows(k_out, "k_out")
+    _check(lib().cs_qk_norm_rope(C.byref(c), qp, qs, kp, ks, qo, qos, ko, kos, _dtype_code(q),
+                                 None if q_gain is None else _dev(q_gain, f32, "q_gain", (D,)),
+                                 None if k_gain is None else _dev(k_gain, f32, "k_gain", (D,)), _dev(cos_sin, f32, "cos_sin", (n, half, 2)),
+                                 _dev(positions, torch.int32, "positions", (T, len(sections))), T, _flag(err_flag), _stream(stream)))
+    return q_out, k_out
+
+
+def cs_cache_query(n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int = 1):
+    """Host-only: (bytes of a page, bytes of the pool).  A pool is a uint8 tensor [n_pages, page bytes]."""
+    c, page, pool = cs_cache_config(C.sizeof(cs_cache_config), n_kv_heads, head_dim, page_tokens, n_pages), C.c_size_t(), C.c_size_t()
+    _check(lib().cs_cache_query(C.byref(c), C.byref(page), C.byref(pool)))
+    return page.value, pool.value
+
+
+def _cache(pool, n_kv_heads: int, head_dim: int, page_tokens: int):
+    """-> (config, pointer) of a pool tensor [n_pages, page bytes]"""
+    import torch
+    if pool.dim() != 2 or pool.shape[1] != n_kv_heads * page_tokens * (head_dim + head_dim // 16):
+        raise ValueError("pool: expected [n_pages, page bytes] of cs_cache_query")
+    return cs_cache_config(C.sizeof(cs_cache_config), n_kv_heads, head_dim, page_tokens, pool.shape[0]), _dev(pool, torch.uint8, "pool")
+
+
+def cs_cache_write(pool, k, v, slots, page_tokens: int, err_flag=None, stream=None) -> None:
+    """pool[slots[t]] = (k[t], v[t]) in 4 bits; k, v [T, kv_heads, head_dim] bf16 or fp32, slots int64 [T] (-1: no slot)."""
+    import torch
+    T, K, D = k.shape
+    if tuple(v.shape) != (T, K, D) or v.dtype != k.dtype:
+        raise ValueError("v: expected the shape and type of k")
+    c, pp = _cache(pool, K, D, page_tokens)
+    kp, ks = _head_rows(k, "k")
+    vp, vs = _head_rows(v, "v")
+    _check(lib().cs_cache_write(C.byref(c), pp, kp, ks, vp, vs, _dtype_code(k), _dev(slots, torch.int64, "slots", (T,)), T, _flag(err_flag),
+                                _stream(stream)))
+
+
+def cs_cache_read(pool, slots, n_kv_heads: int, head_dim: int, page_tokens: int, dtype=None, k=None, v=None, err_flag=None, stream=None):
+    """The values the slots hold -> (k, v) [T, kv_heads, head_dim] of dtype (bf16 unless given)."""
+    import torch
+    shape = (slots.shape[0], n_kv_heads, head_dim)
+    dtype = dtype or (torch.bfloat16 if k is None else k.dtype)
+    k = _empty(shape, dtype, pool.device, stream) if k is None else k
+    v = _empty(shape, dtype, pool.device, stream) if v is None else v
+    if tuple(k.shape) != shape or tuple(v.shape) != shape or k.dtype != dtype or v.dtype != dtype:
+        raise ValueError(f"k, v: expected {shape} of one type")
+    c, pp = _cache(pool, n_kv_heads, head_dim, page_tokens)
+    kp, ks = _head_rows(k, "k")
+    vp, vs = _head_rows(v, "v")
+    _check(lib().cs_cache_read(C.byref(c), pp, _dev(slots, torch.int64, "slots", shape[:1]), shape[0], kp, ks, vp, vs, _dtype_code(k),
+                               _flag(err_flag), _stream(stream)))
+    return k, v
+
+
+def cs_attention_cache(q, pool, page_table, n_keys, cu_queries, max_queries: int, max_keys: int, n_kv_heads: int, page_tokens: int,
+                       scale: Optional[float] = None, causal: bool = True, out=None, workspace=None, err_flag=None, stream=None):
+    """Attention of q [T, heads, head_dim] bf16 over the cache: sequence b has the rows cu_queries[b] .. cu_queries[b + 1] and
+    n_keys[b] keys in the pages page_table[b] (int32 tensors on the GPU).  Returns out [T, heads, head_dim]; a workspace of fewer
+    bytes than needed (or None) is replaced by a new one."""
+    import torch
+    T, H, D = q.shape
+    B, i32 = n_keys.shape[0], torch.int32
+    if q.dtype != torch.bfloat16:
+        raise TypeError("q must be bf16")
+    out = _empty((T, H, D), q.dtype, q.device, stream) if out is None else out
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out: expected the shape and type of q")
+    c, pp = _cache(pool, n_kv_heads, D, page_tokens)
+    qp, qs = _head_rows(q, "q")
+    op, os_ = _head_rows(out, "out")
+    width = page_table.shape[1]
+    b = cs_cache_batch(C.sizeof(cs_cache_batch), B, T, max_queries, width, max_keys, _dev(cu_queries, i32, "cu_queries", (B + 1,)),
+                       _dev(n_keys, i32, "n_keys", (B,)), _dev(page_table, i32, "page_table", (B, width)))
+    need = C.c_size_t()
+    _check(lib().cs_attention_cache_query(C.byref(c), C.byref(b), H, C.byref(need)))
+    if need.value and (workspace is None or workspace.numel() * workspace.element_size() < need.value):
+        workspace = _empty(need.value, torch.uint8, q.device, stream)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(lib().cs_attention_cache(C.byref(c), pp, C.byref(b), qp, qs, op, os_, H, D ** -0.5 if scale is None else scale, int(causal), ws,
+                                    ws_bytes, _flag(err_flag), _stream(stream)))
+    return out
 
 
 def cs_pack_batch(grid_thw, row_budget: int, max_items: int = 1 << 30):

@@ -1,0 +1,77 @@
+// Declarations of the LLM task's side: rotation of queries and keys, the 4-bit cache and attention over it.
+#pragma once
+#include "common.h"
+
+namespace cs {
+
+// n / d for n < 2^32 and 2 <= d <= 2^31 as a product with recip64(d)
+inline uint64_t recip64(uint64_t d) { return ~0ull / d + 1; }
+
+struct QkArgs {
+  const void *q, *k;
+  void *q_out, *k_out;
+  int64_t q_row, k_row, q_out_row, k_out_row;   // elements between rows
+  int32_t norm;                                 // 0: gains are not looked at
+  const float *q_gain, *k_gain;
+  const float* cos_sin;                         // [n_positions, half, 2]
+  const int32_t* positions;                     // [n_rows, axes]
+  int64_t n_rows, n_positions;
+  int32_t n_heads, n_kv_heads, head_dim, half, axes;
+  int32_t end0, end1;                           // contiguous sections: pair j follows axis 0 below end0, 1 below end1, then 2
+  int32_t lim1, lim2;                           // interleaved: pair j % 3 == 1 below lim1 follows axis 1, == 2 below lim2 axis 2
+  int32_t interleaved;
+  float eps;
+  int32_t* err;
+  int32_t parts;                                // set by the launcher: workgroup rows that share out a token's heads
+};
+cs_status launch_qk_norm_rope(const QkArgs& a, int dtype, hipStream_t s);
+
+// A pool of pages (layout: cs_cache_config)
+struct CacheShape {
+  int32_t n_kv_heads, head_dim, page_tokens;
+  int64_t n_pages;
+  int64_t head_bytes;     // block of one page and head
+  int64_t slots;          // n_pages * page_tokens
+  uint64_t page_recip;    // recip64(page_tokens)
+};
+inline CacheShape cache_shape(const cs_cache_config& c) {
+  const int64_t head_bytes = (int64_t)c.page_tokens * (c.head_dim + 2 * (c.head_dim / 32));
+  return CacheShape{c.n_kv_heads, c.head_dim, c.page_tokens, c.n_pages, head_bytes, c.n_pages * c.page_tokens, recip64((uint64_t)c.page_tokens)};
+}
+struct CacheRows {
+  unsigned char* pool;
+  void *k, *v;
+  int64_t k_row, v_row;   // elements
+  const int64_t* slots;
+  int64_t n_rows;
+  CacheShape shape;
+  int32_t* err;
+};
+cs_status launch_cache_write(const CacheRows& a, int dtype, hipStream_t s);
+cs_status launch_cache_read(const CacheRows& a, int dtype, hipStream_t s);
+
+struct CacheAttnArgs {
+  const unsigned char* pool;
+  const bf16_t* q;
+  bf16_t* out;
+  int64_t q_row, out_row;
+  const int32_t *cu, *n_keys, *table;
+  float* part_o;          // splits > 1: [splits, n_queries * n_heads, head_dim] sums not yet normalised
+  float* part_ml;         // ... [splits, n_queries * n_heads, 2] their maximum (log2 domain) and weight
+  int64_t n_queries, max_keys;
+  int32_t n_seqs, max_queries, table_width;
+  int32_t n_heads, group; // group: heads that share a key/value head
+  float scale_log2;       // softmax scale * log2(e)
+  int32_t causal;
+  CacheShape shape;
+  int32_t* err;
+  // set by plan_cache_attention
+  int32_t row_tiles;      // tiles of 16 rows (a row: a query and a head) per sequence and key/value head
+  int32_t splits;         // workgroups that share the keys of a row tile, each `chunk` tiles of 32 keys
+  int32_t chunk;
+};
+// Fills the plan's fields from the sizes; bytes of workspace the launch needs.
+size_t plan_cache_attention(CacheAttnArgs& a);
+cs_status launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);
+
+}  // namespace cs

@@ -1,0 +1,258 @@
+"""Attention over the 4-bit cache against the fp64 checker, which reads the same bytes.
+
+Tolerance, per value: out = sum p v.  Probabilities are rounded to bf16 (at most 2^-8 of each), the result is too (2^-8 of
+it); scores are sums of exact products in fp32, off by at most 2 D 2^-24 sum |q k| scale, which moves a probability by that share
+(sum |q k| scale stays below 64 here: 2^-10 with D = 128); the fp32 sums over keys add less than 2^-10 of sum p |v|.
+So |error| <= 2^-8 |out| + (2^-8 + 2^-9) sum p |v|, and the smallest normal number, below which results may be zero."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as O
+from paper_2603_12118_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+class Batch:
+    """Sequences with random pages in a pool of random bytes; their keys written by the checker."""
+
+    def __init__(self, lens, heads, kv_heads, dim, page, seed=0, spare_width=2, loud=False):
+        rng = np.random.default_rng(seed)
+        self.lens, self.kv_heads, self.dim, self.page = lens, kv_heads, dim, page
+        need = [-(-n // page) for _, n in lens]
+        pages = sum(need) + 2
+        self.pool = rng.integers(0, 256, (pages, kv_heads * page * (dim + dim // 16)), dtype=np.uint8)
+        order = rng.permutation(pages)
+        self.table = np.full((len(lens), max(need) + spare_width), -1, np.int32)
+        self.k, self.v, at = [], [], 0
+        slots, ks, vs = [], [], []
+        for b, (_, n) in enumerate(lens):
+            self.table[b, :need[b]] = order[at:at + need[b]]
+            at += need[b]
+            t = np.arange(n)
+            slots.append(self.table[b, t // page].astype(np.int64) * page + t % page)
+            k, v = rng.standard_normal((2, n, kv_heads, dim))
+            if loud:
+                k, v = k * 3.0, v * 10.0 ** rng.integers(-6, 6, (n, 1, 1))
+            ks.append(k)
+            vs.append(v)
+        # (the checker's writer is slow: the bytes come from its quantiser, a page at a time where whole)
+        self.slots = np.concatenate(slots) if slots else np.zeros(0, np.int64)
+        k, v = np.concatenate(ks), np.concatenate(vs)
+        codes = [O.quantise(x) for x in (k, v)]
+        block = page * (dim + dim // 16)
+        heads_at = np.arange(kv_heads)[:, None] * block
+        where = [O.code_addresses(o, page, dim) for o in range(page)]
+        for t, slot in enumerate(self.slots):
+            p, o = divmod(int(slot), page)
+            for (c, s), ci, si in ((codes[0], 0, 2), (codes[1], 1, 3)):
+                self.pool[p, heads_at + where[o][ci]] = c[t, :, 0::2] | c[t, :, 1::2] << 4
+                self.pool[p, heads_at + where[o][si]] = s[t]
+        hk, hv = O.values(*codes[0]), O.values(*codes[1])
+        cuts = np.cumsum([n for _, n in lens])[:-1]
+        self.k, self.v = np.split(hk, cuts), np.split(hv, cuts)
+        T = sum(q for q, _ in lens)
+        self.q = torch.from_numpy(rng.standard_normal((T, heads, dim))).to(torch.bfloat16).to(DEV)
+        dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)       # noqa: E731
+        self.dpool, self.dtable = dev(self.pool), dev(self.table)
+        self.n_keys, self.cu = dev(np.array([n for _, n in lens], np.int32)), dev(np.cumsum([0] + [q for q, _ in lens]).astype(np.int32))
+        self.max_q, self.max_k = max(q for q, _ in lens), max(n for _, n in lens)
+
+    def run(self, q=None, **kw):
+        args = dict(q=self.q if q is None else q, pool=self.dpool, page_table=self.dtable, n_keys=self.n_keys, cu_queries=self.cu,
+                    max_queries=self.max_q, max_keys=self.max_k, n_kv_heads=self.kv_heads, page_tokens=self.page) | kw
+        return B.cs_attention_cache(**args)
+
+    def check(self, got, causal=True, scale=None, lens=None, q=None):
+        lens = lens or self.lens
+        k, v = ([x[:n] for x, (_, n) in zip(xs, lens)] for xs in (self.k, self.v))
+        want, weight = O.attention((self.q if q is None else q).double().cpu().numpy(), k, v, [n for n, _ in lens],
+                                   self.dim ** -0.5 if scale is None else scale, causal)
+        g = got.double().cpu().numpy()
+        assert g.shape == want.shape and np.isfinite(g).all()
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -9) * weight + 2.0 ** -126
+        bad = np.abs(g - want) > tol
+        assert not bad.any(), (np.argwhere(bad)[:5], np.abs(g - want).max())
+
+
+HEADS = [(28, 4, 128), (8, 2, 64), (5, 5, 128), (16, 1, 64), (32, 1, 128), (3, 1, 128)]
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", HEADS)
+@pytest.mark.parametrize("page", [32, 96])
+def test_one_token_against_lengths_around_the_tiles(heads, kv_heads, dim, page):
+    b = Batch([(1, n) for n in (1, 0, 2, 31, 32, 33, 63, 64, 65, 95, 96, 97, 128, 200, 0, 257)], heads, kv_heads, dim, page)
+    b.check(b.run())
+    b.check(b.run(causal=False), causal=False)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", HEADS[:4])
+@pytest.mark.parametrize("lens", [[(2, 2), (3, 70), (8, 8), (5, 33)], [(1, 1), (7, 400), (0, 5), (0, 0), (2, 64), (8, 9)],
+                                  [(4, 0), (6, 3), (3, 100)], [(1, 31), (17, 17), (1, 300), (9, 90)]])
+def test_a_few_queries_and_rows_without_keys(lens, heads, kv_heads, dim):
+    b = Batch(lens, heads, kv_heads, dim, 32)
+    for causal in (True, False):
+        got = b.run(causal=causal)
+        b.check(got, causal)
+    at = 0
+    got = b.run()
+    for q, n in lens:                                      # causal: the queries in front of the first key
+        assert not got[at:at + max(0, q - n)].any()
+        at += q
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 2, 64), (7, 1, 128), (4, 4, 128), (6, 2, 128), (4, 4, 64)])
+@pytest.mark.parametrize("lens", [[(150, 150)], [(33, 300), (129, 130), (1, 77), (64, 64)], [(257, 400)]])
+def test_chunks_of_a_prompt(lens, heads, kv_heads, dim):
+    b = Batch(lens, heads, kv_heads, dim, 32 if len(lens) > 1 else 160)
+    for causal in (True, False):
+        b.check(b.run(causal=causal), causal)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_long_sequences_share_their_keys_out(dim):
+    b = Batch([(1, 5001), (1, 700), (1, 0), (1, 4096)], 4, 2, dim, 64, seed=3)
+    got = b.run()
+    b.check(got)
+    assert torch.equal(got, b.run())                       # the same bits again
+    b.check(b.run(max_keys=100000, max_queries=7))         # looser bounds: other shares
+    b2 = Batch([(3, 3001)], 2, 1, dim, 128, seed=4)
+    b2.check(b2.run())
+
+
+def test_loud_scores_and_values_of_all_sizes():
+    b = Batch([(2, 500), (1, 64), (20, 333)], 8, 2, 128, 64, seed=5, loud=True)
+    for scale in (0.02, 0.0, -0.02):
+        b.check(b.run(scale=scale), scale=scale)
+
+
+def test_a_maximum_that_moves_in_every_tile():
+    # scores grow from key to key, by far more than the running maximum's slack, or fall: every wave's share has its own
+    for sign in (1, -1):
+        b = Batch([(1, 640), (40, 320)], 4, 1, 64, 32, seed=6)
+        # keys k[t] = r_t * e with r growing; rewrite them through the library
+        t = np.concatenate([np.arange(640), np.arange(320)])
+        r = np.round(np.where(sign > 0, t, 640 - t) / 20.0)
+        k = np.zeros((960, 1, 64))
+        k[:, 0] = np.exp2(np.floor(np.log2(r + 1)))[:, None]
+        v = np.random.default_rng(1).standard_normal((960, 1, 64))
+        kd, vd = (torch.from_numpy(x).to(torch.bfloat16).to(DEV) for x in (k, v))
+        B.cs_cache_write(b.dpool, kd, vd, torch.from_numpy(b.slots).to(DEV), 32)
+        b.k, b.v = (np.split(O.held(x.double().cpu().numpy()), [640]) for x in (kd, vd))
+        b.q = torch.ones_like(b.q)
+        b.check(b.run(scale=0.25), scale=0.25)
+
+
+def test_rows_that_lie_apart_and_a_given_workspace():
+    b = Batch([(1, 2000), (4, 90)], 8, 2, 128, 64, seed=7)
+    wide = torch.full((5, 12, 128), 9.0, dtype=torch.bfloat16, device=DEV)
+    q = torch.zeros(5, 10, 128, dtype=torch.bfloat16, device=DEV)
+    q[:, 1:9] = b.q
+    ws = torch.full((1 << 22,), 255, dtype=torch.uint8, device=DEV)          # NaN in every word
+    out = b.run(q=q[:, 1:9], out=wide[:, 2:10], workspace=ws)
+    assert torch.equal(out, b.run()) and (wide[:, :2] == 9).all() and (wide[:, 10:] == 9).all()
+    b.check(out)
+
+
+def test_the_order_of_pages_does_not_matter():
+    b = Batch([(1, 1000), (30, 200)], 4, 2, 64, 32, seed=8)
+    a = b.run()
+    perm = torch.randperm(b.dpool.shape[0], device=DEV)
+    pool = torch.empty_like(b.dpool)
+    pool[perm] = b.dpool
+    table = torch.where(b.dtable >= 0, perm[b.dtable.clamp(min=0).long()].int(), -1)
+    assert torch.equal(a, b.run(pool=pool, page_table=table))
+
+
+def test_what_lies_behind_the_last_key_does_not_matter():
+    b = Batch([(1, 45), (3, 70), (40, 99)], 4, 2, 128, 64, seed=9)
+    a = b.run()
+    for fill in (0x00, 0xff, 0x7f):
+        free = torch.ones(b.dpool.shape[0] * 64, dtype=torch.bool, device=DEV)
+        free[torch.from_numpy(b.slots).to(DEV)] = False
+        pool = b.dpool.cpu().numpy().copy()
+        for slot in np.flatnonzero(free.cpu().numpy()):
+            p, o = divmod(int(slot), 64)
+            for h in range(2):
+                for at in O.code_addresses(o, 64, 128):
+                    pool[p, h * 64 * 136 + at] = fill
+        assert torch.equal(a, b.run(pool=torch.from_numpy(pool).to(DEV))), fill
+
+
+def test_lengths_and_pages_that_cannot_be_are_cut_and_flagged():
+    b = Batch([(1, 100), (2, 64), (1, 40)], 4, 2, 64, 32, seed=10, spare_width=0)
+    flag = torch.zeros(1, dtype=torch.int32, device=DEV)
+    b.check(b.run(err_flag=flag))
+    assert flag.item() == 0
+    got = b.run(max_keys=64, err_flag=flag)                                   # fewer keys than the first sequence has
+    b.check(got, lens=[(1, 64), (2, 64), (1, 40)])
+    assert flag.item() == 1
+    flag.zero_()
+    b.check(b.run(n_keys=torch.tensor([100, 64, 1 << 30], dtype=torch.int32, device=DEV), page_table=b.dtable[:, :4].contiguous(),
+                  err_flag=flag)[:3], lens=[(1, 100), (2, 64)], q=b.q[:3])
+    assert flag.item() == 1
+    flag.zero_()
+    got = b.run(n_keys=torch.tensor([100, -5, 40], dtype=torch.int32, device=DEV), err_flag=flag)
+    assert flag.item() == 1 and not got[1:3].any()
+    flag.zero_()
+    table = b.dtable.clone()
+    table[1, 1], table[0, 0] = b.dpool.shape[0], -7                          # pages 32..63 of sequence 1, 0..31 of sequence 0
+    got = b.run(page_table=table, err_flag=flag, causal=False)
+    assert flag.item() == 1
+    k, v = ([x[0][32:100], x[1][:32], x[2]] for x in (b.k, b.v))
+    want, weight = O.attention(b.q.double().cpu().numpy(), k, v, [1, 2, 1], 64 ** -0.5, causal=False)
+    assert (np.abs(got.double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -9) * weight).all()
+    flag.zero_()
+    for cu in ([0, 1, 3, 1 << 30], [0, 1, 0, 4], [-3, 1, 3, 4], [0, 4, 4, 4]):
+        b.run(cu_queries=torch.tensor(cu, dtype=torch.int32, device=DEV), err_flag=flag)
+        assert flag.item() == 1, cu
+        flag.zero_()
+    b.run(n_keys=torch.tensor([100, 64, 99], dtype=torch.int32, device=DEV), max_keys=50)      # no flag given
+
+
+def test_a_pool_past_4_gib():
+    heads, page, pages = 8, 128, 32000
+    pool = torch.randint(0, 256, (1, heads * page * 136), dtype=torch.uint8, device=DEV).expand(pages, -1).contiguous()
+    assert pool.numel() > 1 << 32
+    small = Batch([(1, 300), (20, 129)], 16, heads, 128, page, seed=11)
+    at = torch.tensor([31999, 4, 20000, 31500, 16000, 31001, 777], device=DEV)[:small.dpool.shape[0]]
+    pool[at] = small.dpool
+    table = torch.where(small.dtable >= 0, at[small.dtable.clamp(min=0).long()].int(), -1)
+    got = small.run(pool=pool, page_table=table)
+    assert torch.equal(got, small.run())
+    small.check(got)
+
+
+def test_on_another_stream_and_in_a_graph():
+    b = Batch([(1, 3000), (1, 10), (1, 0)], 8, 2, 128, 32, seed=12)
+    eager = b.run()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    other = b.run(stream=side)
+    side.synchronize()
+    assert torch.equal(eager, other)
+    out, ws = torch.empty_like(eager), torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.run(out=out, workspace=ws)
+    for lens in ([3000, 10, 0], [1, 0, 31], [2048, 33, 64], [3000, 10, 0]):            # other lengths, the same recording
+        b.n_keys.copy_(torch.tensor(lens, dtype=torch.int32))
+        b.dtable[2, :2] = b.dtable[0, :2]
+        b.dtable[1, :2] = b.dtable[0, 2:4]
+        ws.fill_(0xff)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, b.run()), lens
+
+
+def test_nothing_to_do():
+    b = Batch([(1, 5)], 4, 2, 64, 32)
+    out = torch.full((1, 4, 64), 3.0, dtype=torch.bfloat16, device=DEV)
+    b.run(cu_queries=torch.zeros(2, dtype=torch.int32, device=DEV), out=out)           # no sequence has queries
+    assert (out == 3).all()
+    b.run(max_keys=0, out=out)                                                         # told that there are no keys
+    assert not out.any()
+    assert b.run(q=b.q[:0], cu_queries=torch.zeros(2, dtype=torch.int32, device=DEV)).shape == (0, 4, 64)
