@@ -61,6 +61,9 @@ class cs_cache_batch(C.Structure):
                 ("page_table", C.c_void_p)]
 
 
+_QK_SIZE, _CACHE_SIZE, _BATCH_SIZE = (C.sizeof(t) for t in (cs_qk_config, cs_cache_config, cs_cache_batch))
+
+
 class cs_tensor(C.Structure):
     _fields_ = [("name", C.c_char_p), ("data", C.c_void_p), ("numel", C.c_int64)]
 
@@ -522,43 +525,51 @@ def cs_attention_varlen_groups(qk, vt, out, seg_cu: Sequence[int], n_heads: int,
                                             len(seg) - 1, n_heads, head_dim, key_groups, _stream(stream)))
 
 
-# ---- the LLM task's attention: tensors of heads are [rows, heads, head_dim] with packed heads; rows may lie apart
-def _dtype_code(x) -> int:
+# ---- the LLM task's attention: tensors of heads are [rows, heads, head_dim] with packed heads; rows may lie apart.
+# (A decode step makes these calls once a layer on a few rows, where the time of a call is the host's: every look at a
+# tensor costs 0.1 to 0.3 us, so each is looked at once.)
+def _rows(x, heads: int, dim: int, name: str):
+    """-> (pointer, elements between rows) of [rows, heads, head_dim]"""
+    sr, sh, sd = x.stride()
+    if not x.is_cuda or sd != 1 or (sh != dim and heads > 1):
+        raise ValueError(f"{name}: heads of a row must be packed, on the GPU")
+    return x.data_ptr(), sr if sr >= heads * dim or x.shape[0] > 1 else heads * dim
+
+
+def _flat(x, dtype, shape, name: str) -> int:
+    if not x.is_cuda or x.dtype is not dtype or x.shape != shape or not x.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape} on the GPU")
+    return x.data_ptr()
+
+
+def _empty(shape, like, stream, dtype=None):
+    """A new tensor of the stream the call runs on (the current one unless given), so that its memory is free there."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
     import torch
-    if x.dtype == torch.bfloat16:
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _call_stream(stream, like) -> int:
+    import torch
+    return torch._C._cuda_getCurrentRawStream(like.device.index) if stream is None else stream.cuda_stream
+
+
+def _code(dtype) -> int:
+    import torch
+    if dtype is torch.bfloat16:
         return CS_BF16
-    if x.dtype == torch.float32:
+    if dtype is torch.float32:
         return CS_F32
     raise TypeError("rows must be bf16 or fp32")
 
 
-def _head_rows(x, name: str):
-    """-> (pointer, elements between rows) of [rows, heads, head_dim]"""
-    rows, heads, dim = x.shape
-    sr, sh, sd = x.stride()
-    if x.device.type != "cuda" or sd != 1 or (heads > 1 and sh != dim):
-        raise ValueError(f"{name}: heads of a row must be packed, on the GPU")
-    return x.data_ptr(), sr if rows > 1 else heads * dim
-
-
-def _dev(x, dtype, name: str, shape=None):
-    if x.device.type != "cuda" or x.dtype != dtype or not x.is_contiguous() or (shape is not None and tuple(x.shape) != shape):
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor on the GPU" + (f" of shape {shape}" if shape is not None else ""))
-    return x.data_ptr()
-
-
-def _empty(shape, dtype, device, stream):
-    """A new tensor of the stream the call runs on (the current one unless given), so that its memory is free there."""
-    import torch
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
 def _flag(err_flag):
+    if err_flag is None:
+        return None
     import torch
-    return None if err_flag is None else _dev(err_flag, torch.int32, "err_flag", (1,))
+    return _flat(err_flag, torch.int32, (1,), "err_flag")
 
 
 def cs_qk_norm_rope(q, k, cos_sin, positions, sections, q_gain=None, k_gain=None, eps: float = 1e-6, interleaved: bool = False,
@@ -566,34 +577,39 @@ def cs_qk_norm_rope(q, k, cos_sin, positions, sections, q_gain=None, k_gain=None
     """Queries [T, heads, head_dim] and keys [T, kv_heads, head_dim] (parts of one packed QKV tensor, say) normed per head where
     gains (fp32 [head_dim]) are given, and rotated: cos_sin fp32 [n_positions, pairs, 2], positions int32 [T, axes],
     `sections` pairs per axis.  Returns (q_out, k_out), new tensors unless given (q, k themselves to work in place)."""
-    import torch
-    T, H, D = q.shape
-    K = k.shape[1]
-    if tuple(k.shape) != (T, K, D) or k.dtype != q.dtype:
+    from torch import float32, int32
+    T, H, D = q_shape = q.shape
+    K, axes, dtype = k.shape[1], len(sections), q.dtype
+    n, half, _ = cs_shape = cos_sin.shape
+    k_shape = (T, K, D)
+    if k.shape != k_shape or k.dtype is not dtype:
         raise ValueError("k: expected the rows, head_dim and type of q")
-    n, half = cos_sin.shape[0], cos_sin.shape[1]
-    if len(sections) > 3:
+    if axes > 3:
         raise ValueError("sections: at most three axes")
-    q_out = _empty((T, H, D), q.dtype, q.device, stream) if q_out is None else q_out
-    k_out = _empty((T, K, D), q.dtype, q.device, stream) if k_out is None else k_out
-    if q_out.shape != q.shape or k_out.shape != k.shape or q_out.dtype != q.dtype or k_out.dtype != q.dtype:
-        raise ValueError("q_out, k_out: expected the shapes and type of q, k")
-    c = cs_qk_config(C.sizeof(cs_qk_config), H, K, D, 2 * half, len(sections), int(interleaved), (C.c_int32 * 3)(*sections), n, eps)
-    f32 = torch.float32
-    qp, qs = _head_rows(q, "q")
-    kp, ks = _head_rows(k, "k")
-    qo, qos = _head_rows(q_out, "q_out")
-    ko, kos = _head_rows(k_out, "k_out")
-    _check(lib().cs_qk_norm_rope(C.byref(c), qp, qs, kp, ks, qo, qos, ko, kos, _dtype_code(q),
-                                 None if q_gain is None else _dev(q_gain, f32, "q_gain", (D,)),
-                                 None if k_gain is None else _dev(k_gain, f32, "k_gain", (D,)), _dev(cos_sin, f32, "cos_sin", (n, half, 2)),
-                                 _dev(positions, torch.int32, "positions", (T, len(sections))), T, _flag(err_flag), _stream(stream)))
+    if q_out is None:
+        q_out = _empty(q_shape, q, stream)
+    elif q_out.shape != q_shape or q_out.dtype is not dtype:
+        raise ValueError("q_out: expected the shape and type of q")
+    if k_out is None:
+        k_out = _empty(k_shape, q, stream)
+    elif k_out.shape != k_shape or k_out.dtype is not dtype:
+        raise ValueError("k_out: expected the shape and type of k")
+    qp, qs = _rows(q, H, D, "q")
+    kp, ks = _rows(k, K, D, "k")
+    qo, qos = _rows(q_out, H, D, "q_out")
+    ko, kos = _rows(k_out, K, D, "k_out")
+    c = cs_qk_config(_QK_SIZE, H, K, D, 2 * half, axes, interleaved, tuple(sections), n, eps)
+    _check(lib().cs_qk_norm_rope(C.byref(c), qp, qs, kp, ks, qo, qos, ko, kos, _code(dtype),
+                                 None if q_gain is None else _flat(q_gain, float32, (D,), "q_gain"),
+                                 None if k_gain is None else _flat(k_gain, float32, (D,), "k_gain"),
+                                 _flat(cos_sin, float32, (n, half, 2), "cos_sin"), _flat(positions, int32, (T, axes), "positions"), T,
+                                 _flag(err_flag), _call_stream(stream, q)))
     return q_out, k_out
 
 
 def cs_cache_query(n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int = 1):
     """Host-only: (bytes of a page, bytes of the pool).  A pool is a uint8 tensor [n_pages, page bytes]."""
-    c, page, pool = cs_cache_config(C.sizeof(cs_cache_config), n_kv_heads, head_dim, page_tokens, n_pages), C.c_size_t(), C.c_size_t()
+    c, page, pool = cs_cache_config(_CACHE_SIZE, n_kv_heads, head_dim, page_tokens, n_pages), C.c_size_t(), C.c_size_t()
     _check(lib().cs_cache_query(C.byref(c), C.byref(page), C.byref(pool)))
     return page.value, pool.value
 
@@ -601,38 +617,45 @@ def cs_cache_query(n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: in
 def _cache(pool, n_kv_heads: int, head_dim: int, page_tokens: int):
     """-> (config, pointer) of a pool tensor [n_pages, page bytes]"""
     import torch
-    if pool.dim() != 2 or pool.shape[1] != n_kv_heads * page_tokens * (head_dim + head_dim // 16):
-        raise ValueError("pool: expected [n_pages, page bytes] of cs_cache_query")
-    return cs_cache_config(C.sizeof(cs_cache_config), n_kv_heads, head_dim, page_tokens, pool.shape[0]), _dev(pool, torch.uint8, "pool")
+    n = pool.shape[0]
+    return (cs_cache_config(_CACHE_SIZE, n_kv_heads, head_dim, page_tokens, n),
+            _flat(pool, torch.uint8, (n, n_kv_heads * page_tokens * (head_dim + head_dim // 16)), "pool (pages of cs_cache_query's bytes)"))
 
 
 def cs_cache_write(pool, k, v, slots, page_tokens: int, err_flag=None, stream=None) -> None:
     """pool[slots[t]] = (k[t], v[t]) in 4 bits; k, v [T, kv_heads, head_dim] bf16 or fp32, slots int64 [T] (-1: no slot)."""
-    import torch
-    T, K, D = k.shape
-    if tuple(v.shape) != (T, K, D) or v.dtype != k.dtype:
+    from torch import int64
+    T, K, D = shape = k.shape
+    dtype = k.dtype
+    if v.shape != shape or v.dtype is not dtype:
         raise ValueError("v: expected the shape and type of k")
     c, pp = _cache(pool, K, D, page_tokens)
-    kp, ks = _head_rows(k, "k")
-    vp, vs = _head_rows(v, "v")
-    _check(lib().cs_cache_write(C.byref(c), pp, kp, ks, vp, vs, _dtype_code(k), _dev(slots, torch.int64, "slots", (T,)), T, _flag(err_flag),
-                                _stream(stream)))
+    kp, ks = _rows(k, K, D, "k")
+    vp, vs = _rows(v, K, D, "v")
+    _check(lib().cs_cache_write(C.byref(c), pp, kp, ks, vp, vs, _code(dtype), _flat(slots, int64, (T,), "slots"), T, _flag(err_flag),
+                                _call_stream(stream, k)))
 
 
 def cs_cache_read(pool, slots, n_kv_heads: int, head_dim: int, page_tokens: int, dtype=None, k=None, v=None, err_flag=None, stream=None):
     """The values the slots hold -> (k, v) [T, kv_heads, head_dim] of dtype (bf16 unless given)."""
-    import torch
-    shape = (slots.shape[0], n_kv_heads, head_dim)
-    dtype = dtype or (torch.bfloat16 if k is None else k.dtype)
-    k = _empty(shape, dtype, pool.device, stream) if k is None else k
-    v = _empty(shape, dtype, pool.device, stream) if v is None else v
-    if tuple(k.shape) != shape or tuple(v.shape) != shape or k.dtype != dtype or v.dtype != dtype:
-        raise ValueError(f"k, v: expected {shape} of one type")
+    from torch import bfloat16, int64
+    T = slots.shape[0]
+    shape = (T, n_kv_heads, head_dim)
+    if dtype is None:
+        dtype = bfloat16 if k is None else k.dtype
     c, pp = _cache(pool, n_kv_heads, head_dim, page_tokens)
-    kp, ks = _head_rows(k, "k")
-    vp, vs = _head_rows(v, "v")
-    _check(lib().cs_cache_read(C.byref(c), pp, _dev(slots, torch.int64, "slots", shape[:1]), shape[0], kp, ks, vp, vs, _dtype_code(k),
-                               _flag(err_flag), _stream(stream)))
+    if k is None:
+        k = _empty(shape, pool, stream, dtype)
+    elif k.shape != shape or k.dtype is not dtype:
+        raise ValueError(f"k: expected {shape} {dtype}")
+    if v is None:
+        v = _empty(shape, pool, stream, dtype)
+    elif v.shape != shape or v.dtype is not dtype:
+        raise ValueError(f"v: expected {shape} {dtype}")
+    kp, ks = _rows(k, n_kv_heads, head_dim, "k")
+    vp, vs = _rows(v, n_kv_heads, head_dim, "v")
+    _check(lib().cs_cache_read(C.byref(c), pp, _flat(slots, int64, (T,), "slots"), T, kp, ks, vp, vs, _code(dtype), _flag(err_flag),
+                               _call_stream(stream, pool)))
     return k, v
 
 
@@ -641,27 +664,30 @@ def cs_attention_cache(q, pool, page_table, n_keys, cu_queries, max_queries: int
     """Attention of q [T, heads, head_dim] bf16 over the cache: sequence b has the rows cu_queries[b] .. cu_queries[b + 1] and
     n_keys[b] keys in the pages page_table[b] (int32 tensors on the GPU).  Returns out [T, heads, head_dim]; a workspace of fewer
     bytes than needed (or None) is replaced by a new one."""
-    import torch
-    T, H, D = q.shape
-    B, i32 = n_keys.shape[0], torch.int32
-    if q.dtype != torch.bfloat16:
+    from torch import bfloat16, int32, uint8
+    T, H, D = q_shape = q.shape
+    if q.dtype is not bfloat16:
         raise TypeError("q must be bf16")
-    out = _empty((T, H, D), q.dtype, q.device, stream) if out is None else out
-    if out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("out: expected the shape and type of q")
     c, pp = _cache(pool, n_kv_heads, D, page_tokens)
-    qp, qs = _head_rows(q, "q")
-    op, os_ = _head_rows(out, "out")
-    width = page_table.shape[1]
-    b = cs_cache_batch(C.sizeof(cs_cache_batch), B, T, max_queries, width, max_keys, _dev(cu_queries, i32, "cu_queries", (B + 1,)),
-                       _dev(n_keys, i32, "n_keys", (B,)), _dev(page_table, i32, "page_table", (B, width)))
-    need = C.c_size_t()
-    _check(lib().cs_attention_cache_query(C.byref(c), C.byref(b), H, C.byref(need)))
-    if need.value and (workspace is None or workspace.numel() * workspace.element_size() < need.value):
-        workspace = _empty(need.value, torch.uint8, q.device, stream)
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _check(lib().cs_attention_cache(C.byref(c), pp, C.byref(b), qp, qs, op, os_, H, D ** -0.5 if scale is None else scale, int(causal), ws,
-                                    ws_bytes, _flag(err_flag), _stream(stream)))
+    B, width = page_table.shape
+    b = cs_cache_batch(_BATCH_SIZE, B, T, max_queries, width, max_keys, _flat(cu_queries, int32, (B + 1,), "cu_queries"),
+                       _flat(n_keys, int32, (B,), "n_keys"), _flat(page_table, int32, (B, width), "page_table"))
+    if out is None:
+        out = _empty(q_shape, q, stream)
+    elif out.shape != q_shape or out.dtype is not bfloat16:
+        raise ValueError("out: expected the shape and type of q")
+    qp, qs = _rows(q, H, D, "q")
+    op, os_ = _rows(out, H, D, "out")
+    L, need, ws = lib(), C.c_size_t(), None
+    _check(L.cs_attention_cache_query(C.byref(c), C.byref(b), H, C.byref(need)))
+    if need.value:
+        if workspace is None or workspace.nbytes < need.value:
+            workspace = _empty((need.value,), q, stream, uint8)
+        elif not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a contiguous tensor on the GPU")
+        ws = workspace.data_ptr()
+    _check(L.cs_attention_cache(C.byref(c), pp, C.byref(b), qp, qs, op, os_, H, D ** -0.5 if scale is None else scale, causal, ws, need.value,
+                                _flag(err_flag), _call_stream(stream, q)))
     return out
 
 

@@ -56,19 +56,26 @@ struct CacheAttnArgs {
   bf16_t* out;
   int64_t q_row, out_row;
   const int32_t *cu, *n_keys, *table;
-  float* part_o;          // splits > 1: [splits, n_queries * n_heads, head_dim] sums not yet normalised
-  float* part_ml;         // ... [splits, n_queries * n_heads, 2] their maximum (log2 domain) and weight
   int64_t n_queries, max_keys;
   int32_t n_seqs, max_queries, table_width;
   int32_t n_heads, group; // group: heads that share a key/value head
-  float scale_log2;       // softmax scale * log2(e)
+  float scale_log2;       // |softmax scale| * log2(e), not zero
+  uint32_t q_sign;        // 0x80008000 where the scale is negative: the queries turn their signs
   int32_t causal;
   CacheShape shape;
   int32_t* err;
   // set by plan_cache_attention
-  int32_t row_tiles;      // tiles of 16 rows (a row: a query and a head) per sequence and key/value head
-  int32_t splits;         // workgroups that share the keys of a row tile, each `chunk` tiles of 32 keys
-  int32_t chunk;
+  int32_t rows;           // rows (a row: a query and a head) a workgroup takes: 16 or 32 (their keys shared out to its waves), 64, 128, 256
+  int32_t row_blocks;     // blocks of so many rows that a sequence and key/value head have at most
+  int32_t target;         // workgroups that fill the chip once
+  int32_t least;          // tiles of 32 keys that a workgroup takes at least, if there are so many
+  int32_t blocks;         // workgroups of the launch: those without work end at once
+  int32_t join;           // 0: no sequence can be shared out; else the threads, in sixteens, that share a row's parts
+  int32_t join_groups;    // workgroups of the joining launch for a block of rows
+  // parts, where a sequence's keys are shared out: [blocks, rows, head_dim] sums not yet normalised, and [blocks, rows, 2]
+  // their maximum (log2 domain) and weight
+  float *part_o, *part_ml;
+  int32_t* share_of;      // [n_seqs, 4] first workgroup, shares, tiles of a share: left by the first launch for the joining one
 };
 // Fills the plan's fields from the sizes; bytes of workspace the launch needs.
 size_t plan_cache_attention(CacheAttnArgs& a);

@@ -1,5 +1,7 @@
 // C entry points of the LLM task's side (argument checks and the launch plan; the kernels are in cache.hip and
 // cache_attention.hip).
+#include <algorithm>
+#include <cmath>
 #include <string>
 
 #include "cache.h"
@@ -157,10 +159,13 @@ cs_status attention_cache(const cs_cache_config* c, const void* pool, const cs_c
   a.q = static_cast<const bf16_t*>(q); a.q_row = q_row;
   a.out = static_cast<bf16_t*>(out); a.out_row = out_row;
   a.cu = b->cu_queries; a.n_keys = b->n_keys; a.table = b->page_table;
-  a.scale_log2 = scale * 1.4426950408889634f;
+  // (a scale of zero as one too small to matter: -inf, a masked score, stays what it is)
+  a.scale_log2 = std::max(std::fabs(scale) * 1.4426950408889634f, 1e-30f);
+  a.q_sign = scale < 0 ? 0x80008000u : 0;
   a.causal = causal; a.err = err_flag;
   a.part_o = static_cast<float*>(workspace);
-  a.part_ml = a.part_o + (size_t)a.splits * (size_t)a.n_queries * (size_t)n_heads * (size_t)c->head_dim;
+  a.part_ml = a.part_o + (size_t)a.blocks * (size_t)a.rows * (size_t)c->head_dim;
+  a.share_of = reinterpret_cast<int32_t*>(a.part_ml + (size_t)a.blocks * (size_t)a.rows * 2);
   return launch_cache_attention(a, static_cast<hipStream_t>(stream));
 }
 

@@ -17,6 +17,7 @@ typedef __bf16 abf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 abf16x2 __attribute__((ext_vector_type(2)));
 typedef float af32x2 __attribute__((ext_vector_type(2)));
 typedef float af32x4 __attribute__((ext_vector_type(4)));
+typedef float af32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned int au32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int au32x4 __attribute__((ext_vector_type(4)));
 template <int N> struct Words;
@@ -38,6 +39,14 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t w) {
   return (B == 3 ? w >> 1 : w << (23 - 8 * B)) & 0x7f800000u;
 }
 
+// eight values of a query, their signs turned where `sign` has the sign bits of a pair
+__device__ __forceinline__ abf16x8 load_q(const bf16_t* p, uint32_t sign) {
+  au32x4 w = *reinterpret_cast<const au32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] ^= sign;
+  return __builtin_bit_cast(abf16x8, w);
+}
+
 // A wave's part of a 32-key tile as it lies in the cache
 template <int NG>
 struct KeyTile {
@@ -46,17 +55,18 @@ struct KeyTile {
   au32x2 v_scale;                        // of tokens 8p..8p+7, the group of the lane's V columns
 };
 
-// Sequence, key/value head and row tile of a workgroup, and the keys its rows see
-struct RowTile {
-  int b, h, q0, nq, keys, first, rows, tiles;
-  bool cut;     // the GPU's lengths are larger than the host was told
+// ---- who does what.  The lengths are on the GPU only, so the workgroups share the work out themselves: every wave reads
+// all lengths, and from them come the tiles a workgroup takes (`chunk`: all work over `target` workgroups), the number of
+// shares of each sequence's keys, and the sequence a workgroup belongs to.  A batch of long and short sequences then fills
+// the chip as evenly as one of equal ones (64 sequences of 160 .. 16384 keys, shares by the longest: 62 us).
+struct Sequence {
+  int q0, nq, keys, units, tiles;   // units: blocks of rows of all key/value heads
+  bool cut;                         // a length on the GPU is not what the host was told
 };
-__device__ __forceinline__ RowTile row_tile(const CacheAttnArgs& a, int unit) {
-  RowTile t;
-  const int rt = unit % a.row_tiles, bh = unit / a.row_tiles;
-  t.h = bh % a.shape.n_kv_heads;
-  t.b = bh / a.shape.n_kv_heads;
-  const int64_t c0 = a.cu[t.b], c1 = a.cu[t.b + 1], n = a.n_keys[t.b];
+__device__ __forceinline__ Sequence sequence(const CacheAttnArgs& a, int b, int rows) {
+  Sequence t = {};
+  if (b >= a.n_seqs) return t;
+  const int64_t c0 = a.cu[b], c1 = a.cu[b + 1], n = a.n_keys[b];
   const int64_t q0 = c0 < 0 ? 0 : c0 > a.n_queries ? a.n_queries : c0;
   int64_t q1 = c1 < q0 ? q0 : c1 > a.n_queries ? a.n_queries : c1;
   t.cut = q0 != c0 || q1 != c1 || q1 - q0 > a.max_queries;
@@ -66,54 +76,142 @@ __device__ __forceinline__ RowTile row_tile(const CacheAttnArgs& a, int unit) {
   t.cut |= t.keys != n;
   t.q0 = (int)q0;
   t.nq = (int)(q1 - q0);
-  t.rows = t.nq * a.group;
-  t.first = rt * 16;
-  int seen = t.keys;
-  if (a.causal) {
-    const int last = (t.first + 15 < t.rows ? t.first + 15 : t.rows - 1) / a.group;
-    seen = t.keys - t.nq + last + 1;
-  }
-  t.tiles = t.first < t.rows && seen > 0 ? (seen + 31) >> 5 : 0;
+  t.units = (int)(((int64_t)t.nq * a.group + rows - 1) / rows) * a.shape.n_kv_heads;
+  t.tiles = (t.keys + 31) >> 5;
   return t;
 }
+struct Share {
+  Sequence seq;
+  int b, chunk, shares, first;   // first: the sequence's first workgroup
+};
+// The share of workgroup `id`; false where there is none.  Whole waves.
+__device__ __forceinline__ bool find_share(const CacheAttnArgs& a, int rows, int id, Share& s) {
+  const int lane = threadIdx.x & 63, n = a.n_seqs;
+  const Sequence mine = sequence(a, lane, rows);
+  float work = (float)mine.units * (float)mine.tiles;
+  bool cut = mine.cut;
+  for (int b = 64 + lane; b < n; b += 64) {
+    const Sequence t = sequence(a, b, rows);
+    work += (float)t.units * (float)t.tiles;
+    cut |= t.cut;
+  }
+  if (id == 0 && cut && a.err) atomicOr(a.err, 1);
+  for (int m = 1; m < 64 && m < n; m <<= 1) work += __shfl_xor(work, m);
+  work = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(work)));
+  // (more than work / target, so that the workgroups are fewer than target and one a unit)
+  const float per = work / (float)a.target;
+  int chunk = per > 3e7f ? 1 << 25 : (int)per + 1;
+  chunk = chunk < a.least ? a.least : (chunk + 1) & ~1;
+  int before = 0;
+  for (int b0 = 0; b0 < n; b0 += 64) {
+    const Sequence t = b0 ? sequence(a, b0 + lane, rows) : mine;
+    const int shares = t.tiles > chunk ? (t.tiles + chunk - 1) / chunk : 1;
+    int upto = t.units * shares;
+    const int own = upto;
+    for (int m = 1; m < 64 && m < n; m <<= 1) {
+      const int x = __shfl_up(upto, m);
+      upto += lane >= m ? x : 0;
+    }
+    const uint64_t hit = __ballot(before + upto > id);
+    if (hit) {
+      const int f = __builtin_ctzll(hit);
+      s.b = b0 + f;
+      s.chunk = chunk;
+      s.shares = __builtin_amdgcn_readlane(shares, f);
+      s.first = before + __builtin_amdgcn_readlane(upto - own, f);
+      s.seq.q0 = __builtin_amdgcn_readlane(t.q0, f);
+      s.seq.nq = __builtin_amdgcn_readlane(t.nq, f);
+      s.seq.keys = __builtin_amdgcn_readlane(t.keys, f);
+      s.seq.units = __builtin_amdgcn_readlane(t.units, f);
+      s.seq.tiles = __builtin_amdgcn_readlane(t.tiles, f);
+      return true;
+    }
+    const int last = n - b0 < 64 ? n - b0 - 1 : 63;
+    before += __builtin_amdgcn_readlane(upto, last);
+  }
+  return false;
+}
+// The block of rows that `unit` of a sequence is: the last rows, which see the most keys, first
+struct RowBlock {
+  int h, first, rows, seen;   // rows first .. of `rows`; keys its last row sees
+};
+__device__ __forceinline__ RowBlock row_block(const CacheAttnArgs& a, const Sequence& q, int unit, int rows) {
+  RowBlock r;
+  const int rb = unit / a.shape.n_kv_heads;
+  r.h = unit - rb * a.shape.n_kv_heads;
+  r.rows = q.nq * a.group;
+  r.first = (q.units / a.shape.n_kv_heads - 1 - rb) * rows;
+  const int last = (r.first + rows < r.rows ? r.first + rows : r.rows) - 1;
+  r.seen = a.causal ? q.keys - q.nq + last / a.group + 1 : q.keys;
+  r.seen = r.seen < 0 ? 0 : r.seen;
+  return r;
+}
 
+// The running maximum moves only when a score exceeds it by more than SLACK, in the log2 domain: probabilities stay below 2^8, and the
+// accumulators are rescaled on the first tile and on such a jump instead of on nearly every tile.
+constexpr float SLACK = 8.f;
+
+// values jc .. jc + 2 NG - 1 of row r, normalised
 template <int NG>
-__global__ __launch_bounds__(256) void attend_rows_kernel(CacheAttnArgs a) {
-  constexpr int D = 32 * NG, WAVES = 4, PITCH = D + 4;
+__device__ __forceinline__ void store_row(const CacheAttnArgs& a, int q0, int h, int r, int jc, const float (&acc)[2 * NG], float weight) {
+  const float inv = weight > 0.f ? 1.f / weight : weight == 0.f ? 0.f : weight;     // no key: zeros; NaN stays
+  typename Words<NG>::type w;
+#pragma unroll
+  for (int i = 0; i < NG; ++i) w[i] = pack2_k(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+  const int query = r / a.group;
+  const int64_t head = h * a.group + (r - query * a.group);
+  *reinterpret_cast<typename Words<NG>::type*>(a.out + (q0 + query) * a.out_row + head * (32 * NG) + jc) = w;
+}
+
+// ---- few rows: 16 RT of them, a wave's keys its own
+template <int NG, int RT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 4 : 2))) void attend_rows_kernel(CacheAttnArgs a) {
+  constexpr int D = 32 * NG, WAVES = 4, PITCH = D + 4, ROWS = 16 * RT;
   typedef typename Words<NG>::type words;
   __shared__ __align__(16) float state_o[WAVES][16][PITCH];
   __shared__ float state_m[WAVES][16], state_l[WAVES][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l15 = lane & 15, p = lane >> 4;
-  const int split = blockIdx.x % a.splits;
-  const RowTile t = row_tile(a, blockIdx.x / a.splits);
-  if (t.cut && a.err && tid == 0) atomicOr(a.err, 1);
-  if (t.first >= t.rows) return;                                    // (whole workgroups, before any barrier)
-  if (split > 0 && split * a.chunk >= t.tiles) return;
+  Share t;
+  if (!find_share(a, ROWS, blockIdx.x, t)) return;           // (whole workgroups, before any barrier)
+  const int rank = blockIdx.x - t.first, share = rank / t.seq.units, unit = rank - share * t.seq.units;
+  const RowBlock rb = row_block(a, t.seq, unit, ROWS);
+  if (a.join && rank == 0 && tid == 0) *reinterpret_cast<int4*>(a.share_of + 4 * t.b) = make_int4(t.first, t.shares, t.chunk, 0);
 
   // ---- this wave's tiles
-  int t0 = split * a.chunk, t1 = t0 + a.chunk < t.tiles ? t0 + a.chunk : t.tiles;
+  int t0 = share * t.chunk, t1 = (rb.seen + 31) >> 5;
   {
+    if (share > 0 && t0 >= t1) return;
+    t1 = t0 + t.chunk < t1 ? t0 + t.chunk : t1;
     const int per = (t1 - t0 + WAVES - 1) / WAVES;
     t0 += wave * per;
     t1 = t0 + per < t1 ? t0 + per : t1;
   }
-  // ---- the lane's row
-  const int r = t.first + l15, rr = r < t.rows ? r : t.rows - 1, query = rr / a.group, sub = rr - query * a.group;
-  const int64_t head = t.h * a.group + sub;
-  int seen = a.causal ? t.keys - t.nq + query + 1 : t.keys;         // keys the row sees
-  if (r >= t.rows || seen < 0) seen = 0;
-  int seen_by_all = a.causal ? t.keys - t.nq + t.first / a.group + 1 : t.keys;   // ... and every row of the tile
-  abf16x8 qf[NG];
-  {
-    const bf16_t* qp = a.q + (t.q0 + query) * a.q_row + head * D + 8 * p;
+  // ---- the lane's rows
+  const int keys = t.seq.keys, nq = t.seq.nq;
+  int seen[RT];                                                       // keys a row sees
+  abf16x8 qf[RT][NG];
 #pragma unroll
-    for (int g = 0; g < NG; ++g) qf[g] = *reinterpret_cast<const abf16x8*>(qp + 32 * g);
+  for (int x = 0; x < RT; ++x) {
+    const int r = rb.first + 16 * x + l15, rr = r < rb.rows ? r : rb.rows - 1, query = rr / a.group;
+    const int64_t head = rb.h * a.group + (rr - query * a.group);
+    seen[x] = a.causal ? keys - nq + query + 1 : keys;
+    if (r >= rb.rows) seen[x] = 0;
+    const bf16_t* qp = a.q + (t.seq.q0 + query) * a.q_row + head * D + 8 * p;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) qf[x][g] = load_q(qp + 32 * g, a.q_sign);
   }
-  af32x4 o[2 * NG];
+  const int seen_by_all = a.causal ? keys - nq + rb.first / a.group + 1 : keys;
+  af32x4 o[RT][2 * NG];
+  float m[RT], shift[RT], sum[RT];       // the running maximum of the scores, the same times the scale, the weight
+  const float slack = SLACK / a.scale_log2;
 #pragma unroll
-  for (int i = 0; i < 2 * NG; ++i) o[i] = af32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, sum = 0.f;
+  for (int x = 0; x < RT; ++x) {
+    m[x] = -INFINITY;
+    shift[x] = sum[x] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * NG; ++i) o[x][i] = af32x4{0.f, 0.f, 0.f, 0.f};
+  }
 
   // ---- addresses.  Pages are found 64 at a time: lane i holds the number of page first_page + i.
   const int P = a.shape.page_tokens, page_tiles = P >> 5;
@@ -140,7 +238,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(CacheAttnArgs a) {
     const int id = __builtin_amdgcn_readlane(pages, page - first_page);
     next_bad = id < 0 || id >= a.shape.n_pages;
     bad |= next_bad;
-    const unsigned char* block = a.pool + ((int64_t)(next_bad ? 0 : id) * a.shape.n_kv_heads + t.h) * a.shape.head_bytes;
+    const unsigned char* block = a.pool + ((int64_t)(next_bad ? 0 : id) * a.shape.n_kv_heads + rb.h) * a.shape.head_bytes;
     const unsigned char* kp = block + in_page * (16 * D) + k_off;
     next.k[0] = *reinterpret_cast<const words*>(kp);
     next.k[1] = *reinterpret_cast<const words*>(kp + 2 * D);
@@ -168,7 +266,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(CacheAttnArgs a) {
     if (tile + 1 < t1) load();
     if (skip) continue;
     const int kv = tile * 32;
-    af32x4 s[2] = {};
+    af32x4 s[RT][2] = {};
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       auto group = [&](auto G) {
@@ -179,7 +277,8 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(CacheAttnArgs a) {
         w[1] = widen2<1>(c.k[u][g], sc);
         w[2] = widen2<2>(c.k[u][g], sc);
         w[3] = widen2<3>(c.k[u][g], sc);
-        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(abf16x8, w), qf[g], s[u], 0, 0, 0);
+#pragma unroll
+        for (int x = 0; x < RT; ++x) s[x][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(abf16x8, w), qf[x][g], s[x][u], 0, 0, 0);
       };
       group(std::integral_constant<int, 0>());
       group(std::integral_constant<int, 1>());
@@ -188,42 +287,49 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(CacheAttnArgs a) {
         group(std::integral_constant<int, 3>());
       }
     }
-    // ---- softmax in the log2 domain.  A score that the row does not see becomes -inf by selection: what lies behind
-    // a sequence's end may be anything, NaN included, and so the V scales there become zero.
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3] * a.scale_log2;
-    if (kv + 32 > seen_by_all) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (kv + 8 * p + i >= seen) x[i] = -INFINITY;
-      const int held = t.keys - (kv + 8 * p);       // tokens of the lane's eight that exist
+    const bool masked = kv + 32 > seen_by_all;
+    if (masked) {
+      const int held = keys - (kv + 8 * p);           // tokens of the lane's eight that exist
       if (held < 8) {
         c.v_scale[0] = held >= 4 ? c.v_scale[0] : held > 0 ? c.v_scale[0] & ((1u << (8 * held)) - 1) : 0;
         c.v_scale[1] = held > 4 ? c.v_scale[1] & ((1u << (8 * (held - 4))) - 1) : 0;
       }
     }
-    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-    constexpr float SLACK = 8.f;   // the running maximum moves only when a score exceeds it by more: probabilities stay below 2^8
-    if (__any(top > m + SLACK || (m == -INFINITY && top > m))) {
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float moved = top > m + SLACK || m == -INFINITY ? fmaxf(top, m) : m;
-      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - moved);
-      m = moved;
-      sum *= alpha;
+    // ---- softmax, exp2 of scaled differences.  A score that the row does not see becomes -inf by selection: what lies behind
+    // a sequence's end may be anything, NaN included, and so the V scales there are zero.
+    abf16x8 pf[RT];
 #pragma unroll
-      for (int i = 0; i < 2 * NG; ++i) o[i] *= alpha;
-    }
-    const float shift = m == -INFINITY ? 0.f : m;
-    au32x4 pw;
+    for (int r = 0; r < RT; ++r) {
+      float x[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float p0 = __builtin_amdgcn_exp2f(x[2 * i] - shift), p1 = __builtin_amdgcn_exp2f(x[2 * i + 1] - shift);
-      sum += p0 + p1;
-      pw[i] = pack2_k(p0, p1);
+      for (int i = 0; i < 8; ++i) x[i] = s[r][i >> 2][i & 3];
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (kv + 8 * p + i >= seen[r]) x[i] = -INFINITY;
+      }
+      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__any(top > m[r] + slack || (m[r] == -INFINITY && top > m[r]))) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float moved = top > m[r] + slack || m[r] == -INFINITY ? fmaxf(top, m[r]) : m[r];
+        const float alpha = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift[r] - moved * a.scale_log2);
+        m[r] = moved;
+        shift[r] = m[r] == -INFINITY ? 0.f : m[r] * a.scale_log2;
+        sum[r] *= alpha;
+#pragma unroll
+        for (int i = 0; i < 2 * NG; ++i) o[r][i] *= alpha;
+      }
+      au32x4 pw;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(x[2 * i], a.scale_log2, -shift[r]));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(x[2 * i + 1], a.scale_log2, -shift[r]));
+        sum[r] += p0 + p1;
+        pw[i] = pack2_k(p0, p1);
+      }
+      pf[r] = __builtin_bit_cast(abf16x8, pw);
     }
-    const abf16x8 pf = __builtin_bit_cast(abf16x8, pw);
     // ---- O^T += V^T P^T: columns 2b and 2b+1 of the lane's 2 NG, tokens 8p .. 8p+7
     uint32_t vs[8];
     vs[0] = scale_of<0>(c.v_scale[0]); vs[1] = scale_of<1>(c.v_scale[0]); vs[2] = scale_of<2>(c.v_scale[0]); vs[3] = scale_of<3>(c.v_scale[0]);
@@ -244,8 +350,11 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(CacheAttnArgs a) {
         lo[i] = __builtin_amdgcn_perm(f, e, 0x05040100u);
         hi[i] = __builtin_amdgcn_perm(f, e, 0x07060302u);
       }
-      o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(abf16x8, lo), pf, o[2 * b], 0, 0, 0);
-      o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(abf16x8, hi), pf, o[2 * b + 1], 0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < RT; ++x) {
+        o[x][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(abf16x8, lo), pf[x], o[x][2 * b], 0, 0, 0);
+        o[x][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(abf16x8, hi), pf[x], o[x][2 * b + 1], 0, 0, 0);
+      }
     };
     column(std::integral_constant<int, 0>());
     column(std::integral_constant<int, 1>());
@@ -256,100 +365,412 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(CacheAttnArgs a) {
   }
   if (bad && a.err && lane == 0) atomicOr(a.err, 1);
 
-  // ---- the waves' states, joined in their order.  o[i][e] is value (4p + e) 2 NG + i of the row
-  sum += __shfl_xor(sum, 16);
-  sum += __shfl_xor(sum, 32);
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-#pragma unroll
-    for (int i = 0; i < 2 * NG; i += 4)
-      *reinterpret_cast<af32x4*>(&state_o[wave][l15][(4 * p + e) * 2 * NG + i]) = af32x4{o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]};
-  if (p == 0) {
-    state_m[wave][l15] = m;
-    state_l[wave][l15] = sum;
-  }
-  __syncthreads();
+  // ---- the waves' states, joined in their order, 16 rows at a time.  o[x][i][e] is value (4p + e) 2 NG + i of the row
   const int jr = tid >> 4, jc = (tid & 15) * (2 * NG);
-  if (t.first + jr >= t.rows) return;
-  float mm = state_m[0][jr];
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) mm = fmaxf(mm, state_m[w][jr]);
-  float ll = 0.f, acc[2 * NG] = {};
+  for (int x = 0; x < RT; ++x) {
+    sum[x] += __shfl_xor(sum[x], 16);
+    sum[x] += __shfl_xor(sum[x], 32);
+    if (x > 0) __syncthreads();
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    const float mw = state_m[w][jr], f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mm);
-    ll += f * state_l[w][jr];
+    for (int e = 0; e < 4; ++e)
 #pragma unroll
-    for (int i = 0; i < 2 * NG; ++i) acc[i] += f * state_o[w][jr][jc + i];
-  }
-  const int jq = (t.first + jr) / a.group;
-  const int64_t token = t.q0 + jq, jh = t.h * a.group + (t.first + jr - jq * a.group);
-  if (a.splits > 1) {
-    const int64_t at = (split * a.n_queries + token) * a.n_heads + jh;
-    af32x4* to = reinterpret_cast<af32x4*>(a.part_o + at * D + jc);
+      for (int i = 0; i < 2 * NG; i += 4)
+        *reinterpret_cast<af32x4*>(&state_o[wave][l15][(4 * p + e) * 2 * NG + i]) = af32x4{o[x][i][e], o[x][i + 1][e], o[x][i + 2][e], o[x][i + 3][e]};
+    if (p == 0) {
+      state_m[wave][l15] = m[x] == -INFINITY ? m[x] : shift[x];
+      state_l[wave][l15] = sum[x];
+    }
+    __syncthreads();
+    const int r = rb.first + 16 * x + jr;
+    if (r >= rb.rows) continue;
+    float mm = state_m[0][jr];
 #pragma unroll
-    for (int i = 0; i < 2 * NG; i += 4) to[i / 4] = af32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
-    if ((tid & 15) == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(mm, ll);
-  } else {
-    const float inv = ll > 0.f ? 1.f / ll : 0.f;
-    typename Words<NG>::type w;
+    for (int w = 1; w < WAVES; ++w) mm = fmaxf(mm, state_m[w][jr]);
+    float ll = 0.f, acc[2 * NG] = {};
 #pragma unroll
-    for (int i = 0; i < NG; ++i) w[i] = pack2_k(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-    *reinterpret_cast<typename Words<NG>::type*>(a.out + token * a.out_row + jh * D + jc) = w;
+    for (int w = 0; w < WAVES; ++w) {
+      const float mw = state_m[w][jr], f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mm);
+      ll += f * state_l[w][jr];
+#pragma unroll
+      for (int i = 0; i < 2 * NG; ++i) acc[i] += f * state_o[w][jr][jc + i];
+    }
+    if (t.shares > 1) {
+      const int64_t at = (int64_t)blockIdx.x * ROWS + 16 * x + jr;
+      af32x4* to = reinterpret_cast<af32x4*>(a.part_o + at * D + jc);
+#pragma unroll
+      for (int i = 0; i < 2 * NG; i += 4) to[i / 4] = af32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+      if ((tid & 15) == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(mm, ll);
+    } else {
+      store_row<NG>(a, t.seq.q0, rb.h, r, jc, acc, ll);
+    }
   }
 }
 
-// The splits of a row tile, joined in their order: 16 lanes a row, as the workgroups above end
-template <int NG>
-__global__ __launch_bounds__(256) void join_splits_kernel(CacheAttnArgs a) {
-  constexpr int D = 32 * NG;
-  const RowTile t = row_tile(a, blockIdx.x);
-  const int jr = threadIdx.x >> 4, jc = (threadIdx.x & 15) * (2 * NG);
-  if (t.first + jr >= t.rows) return;
-  const int used = t.tiles > 0 ? (t.tiles + a.chunk - 1) / a.chunk : 1;
-  const int jq = (t.first + jr) / a.group;
-  const int64_t token = t.q0 + jq, jh = t.h * a.group + (t.first + jr - jq * a.group);
-  const int64_t at = token * a.n_heads + jh, step = a.n_queries * a.n_heads;
-  float mm = -INFINITY;
-  for (int s = 0; s < used; ++s) mm = fmaxf(mm, a.part_ml[(at + s * step) * 2]);
-  float ll = 0.f, acc[2 * NG] = {};
-  for (int s = 0; s < used; ++s) {
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (at + s * step) * 2);
-    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mm);
-    ll += f * ml.y;
-    const af32x4* from = reinterpret_cast<const af32x4*>(a.part_o + (at + s * step) * D + jc);
+// ---- many rows: 32 a wave, the waves' keys the same.  Tiles of 64 keys are widened once, into LDS, by the whole workgroup:
+// K as it is, V transposed, so that both products read 16 bytes a lane.  S^T = K Q^T and O^T = V^T P^T with
+// v_mfma_f32_32x32x16_bf16: lane l has row l % 32 throughout, and what the exponential leaves is the second product's operand.
+// A column of V^T (value 2 NG j + d of a head, j = the word of a token that holds it) is row 16 d + j of the tile: the 16 lanes
+// that write one d then write neighbouring rows, and a lane's results come out 2 NG values at a time.
+template <int NG, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void attend_block_kernel(CacheAttnArgs a) {
+  constexpr int D = 32 * NG, ROWS = 32 * NW, NT = 64 * NW, KS = D / 16;
+  constexpr int KSTR = D * 2 + 16, VSTR = 64 * 2 + 16;      // bytes between rows of the tiles
+  constexpr int ITEMS = NW == 8 ? 1 : 256 / NT;             // 256 pieces of K and 256 of V a tile; eight waves: half the waves each
+  typedef typename Words<NG>::type words;
+  __shared__ __align__(16) unsigned char k_lds[64 * KSTR];
+  __shared__ __align__(16) unsigned char v_lds[D * VSTR];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l31 = lane & 31, lhi = lane >> 5;
+  Share t;
+  if (!find_share(a, ROWS, blockIdx.x, t)) return;          // (whole workgroups, before any barrier)
+  const int rank = blockIdx.x - t.first, share = rank / t.seq.units, unit = rank - share * t.seq.units;
+  const RowBlock rb = row_block(a, t.seq, unit, ROWS);
+  if (a.join && rank == 0 && tid == 0) *reinterpret_cast<int4*>(a.share_of + 4 * t.b) = make_int4(t.first, t.shares, t.chunk, 0);
+  const int t0 = share * t.chunk, seen_tiles = (rb.seen + 31) >> 5;       // (chunks are even)
+  if (share > 0 && t0 >= seen_tiles) return;
+  const int t1 = t0 + t.chunk < seen_tiles ? t0 + t.chunk : seen_tiles;
+
+  // ---- the lane's row
+  const int keys = t.seq.keys, nq = t.seq.nq, wave_first = rb.first + 32 * wave;
+  const int r = wave_first + l31, rr = r < rb.rows ? r : rb.rows - 1, query = rr / a.group;
+  const int64_t head = rb.h * a.group + (rr - query * a.group);
+  const int seen = r < rb.rows ? (a.causal ? keys - nq + query + 1 : keys) : 0;
+  // ... and of the wave: keys its first and its last row see
+  const int wave_last = wave_first + 31 < rb.rows ? wave_first + 31 : rb.rows - 1;
+  const int seen_first = a.causal ? keys - nq + wave_first / a.group + 1 : keys;
+  const int seen_last = wave_first >= rb.rows ? 0 : a.causal ? keys - nq + wave_last / a.group + 1 : keys;
+  abf16x8 qf[KS];
+  {
+    const bf16_t* qp = a.q + (t.seq.q0 + query) * a.q_row + head * D + 8 * lhi;
 #pragma unroll
-    for (int i = 0; i < 2 * NG; ++i) acc[i] += f * from[i / 4][i & 3];
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = load_q(qp + 16 * ks, a.q_sign);
   }
-  const float inv = ll > 0.f ? 1.f / ll : 0.f;
-  typename Words<NG>::type w;
+  af32x16 o[NG];
 #pragma unroll
-  for (int i = 0; i < NG; ++i) w[i] = pack2_k(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-  *reinterpret_cast<typename Words<NG>::type*>(a.out + token * a.out_row + jh * D + jc) = w;
+  for (int i = 0; i < NG; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m = -INFINITY, shift = 0.f, sum = 0.f;
+  const float slack = SLACK / a.scale_log2;
+
+  // ---- staging: cache -> registers, a tile ahead -> LDS
+  const int P = a.shape.page_tokens, page_tiles = P >> 5;
+  const int32_t* table = a.table + (int64_t)t.b * a.table_width;
+  int page = t0 / page_tiles, in_page = t0 - page * page_tiles, first_page = page, ahead = t0;
+  const int last_page = t1 > t0 ? (t1 - 1) / page_tiles : page;
+  auto load_pages = [&]() {
+    const int x = first_page + lane;
+    return x <= last_page ? table[x] : 0;
+  };
+  int pages = t1 > t0 ? load_pages() : 0;
+  bool bad = false;
+  const bool does_k = NW < 8 || wave < 4, does_v = NW < 8 || wave >= 4;
+  words kw[ITEMS], vw[ITEMS];
+  uint32_t ksc[ITEMS], vsc[ITEMS];
+  bool lost[2];                 // halves of the tile in registers that are in no page
+  auto load_tile = [&]() {      // the tile of 64 keys at (page, in_page) = `ahead` tiles of 32, and the step to the next
+    int page1 = page, in1 = in_page + 1;
+    if (in1 == page_tiles) {
+      in1 = 0;
+      ++page1;
+    }
+    if (page1 - first_page >= 64) {
+      first_page = page;
+      pages = load_pages();
+    }
+    const int id0 = __builtin_amdgcn_readlane(pages, page - first_page), id1 = __builtin_amdgcn_readlane(pages, page1 - first_page);
+    const bool there = ahead + 1 < t1;
+    lost[0] = id0 < 0 || id0 >= a.shape.n_pages;
+    lost[1] = there && (id1 < 0 || id1 >= a.shape.n_pages);
+    bad |= lost[0] || lost[1];
+    const unsigned char* block0 = a.pool + ((int64_t)(lost[0] ? 0 : id0) * a.shape.n_kv_heads + rb.h) * a.shape.head_bytes;
+    const unsigned char* block1 = a.pool + ((int64_t)(lost[1] || !there ? 0 : id1) * a.shape.n_kv_heads + rb.h) * a.shape.head_bytes;
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+      const int i = (NW == 8 ? tid & 255 : tid) + u * NT;
+      const int half = __builtin_amdgcn_readfirstlane(i >> 7);       // (a wave's pieces lie in one half)
+      const unsigned char* block = half ? block1 : block0;
+      const int at = half ? in1 : in_page;
+      if (does_k) {
+        const int key = (i >> 2) & 31;
+        kw[u] = *reinterpret_cast<const words*>(block + at * (16 * D) + key * (D / 2) + (i & 3) * (4 * NG));
+        const unsigned char* sp = block + P * D + (at * 32 + key) * NG;
+        if constexpr (NG == 4) ksc[u] = *reinterpret_cast<const uint32_t*>(sp);
+        else ksc[u] = *reinterpret_cast<const uint16_t*>(sp);
+      }
+      if (does_v) {
+        const int quad = (i >> 4) & 7, j = i & 15;
+        vw[u] = *reinterpret_cast<const words*>(block + P * (D / 2) + at * (16 * D) + quad * (2 * D) + j * (4 * NG));
+        vsc[u] = *reinterpret_cast<const uint32_t*>(block + P * (D + NG) + at * (32 * NG) + (quad >> 1) * (8 * NG) + (j * NG >> 4) * 8 + (quad & 1) * 4);
+        // tokens that do not exist have a scale of nothing: their codes may be anything, their product with zero must be zero
+        const int held = (half ? lost[1] || !there : lost[0]) ? 0 : keys - (ahead * 32 + half * 32 + quad * 4);
+        if (held < 4) vsc[u] = held > 0 ? vsc[u] & ((1u << (8 * held)) - 1) : 0;
+      }
+    }
+    ahead += 2;
+    in_page = in1 + 1;
+    page = page1;
+    if (in_page == page_tiles) {
+      in_page = 0;
+      ++page;
+    }
+  };
+  auto store_tile = [&]() {
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+      const int i = (NW == 8 ? tid & 255 : tid) + u * NT;
+      if (does_k) {
+        unsigned char* to = k_lds + (i >> 2) * KSTR + (i & 3) * 16;
+        auto group = [&](auto G) {
+          constexpr int g = decltype(G)::value;
+          const uint32_t sc = scale_of<g>(ksc[u]);
+          *reinterpret_cast<au32x4*>(to + g * 64) =
+              au32x4{widen2<0>(kw[u][g], sc), widen2<1>(kw[u][g], sc), widen2<2>(kw[u][g], sc), widen2<3>(kw[u][g], sc)};
+        };
+        group(std::integral_constant<int, 0>());
+        group(std::integral_constant<int, 1>());
+        if constexpr (NG == 4) {
+          group(std::integral_constant<int, 2>());
+          group(std::integral_constant<int, 3>());
+        }
+      }
+      if (does_v) {
+        // (quads 1 and 2 of every four change places: the eight tokens of a lane's operand are then 16 bytes side by side)
+        const int quad = i >> 4, place = (quad & 12) | ((quad & 1) << 1) | ((quad >> 1) & 1);
+        unsigned char* to = v_lds + (i & 15) * VSTR + place * 8;
+        const uint32_t s0 = scale_of<0>(vsc[u]), s1 = scale_of<1>(vsc[u]), s2 = scale_of<2>(vsc[u]), s3 = scale_of<3>(vsc[u]);
+        auto column = [&](auto B) {
+          constexpr int b = decltype(B)::value;
+          uint32_t x0, x1, x2, x3;          // values 2b, 2b + 1 of the four tokens
+          if constexpr (NG == 4) {
+            x0 = widen2<b>(vw[u][0], s0); x1 = widen2<b>(vw[u][1], s1); x2 = widen2<b>(vw[u][2], s2); x3 = widen2<b>(vw[u][3], s3);
+          } else {
+            x0 = widen2<b>(vw[u][0], s0); x1 = widen2<b + 2>(vw[u][0], s1); x2 = widen2<b>(vw[u][1], s2); x3 = widen2<b + 2>(vw[u][1], s3);
+          }
+          *reinterpret_cast<au32x2*>(to + 2 * b * 16 * VSTR) = au32x2{__builtin_amdgcn_perm(x1, x0, 0x05040100u), __builtin_amdgcn_perm(x3, x2, 0x05040100u)};
+          *reinterpret_cast<au32x2*>(to + (2 * b + 1) * 16 * VSTR) = au32x2{__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u)};
+        };
+        column(std::integral_constant<int, 0>());
+        column(std::integral_constant<int, 1>());
+        if constexpr (NG == 4) {
+          column(std::integral_constant<int, 2>());
+          column(std::integral_constant<int, 3>());
+        }
+      }
+    }
+  };
+
+  if (t0 < t1) load_tile();
+  for (int tile = t0; tile < t1; tile += 2) {
+    const int kv = tile * 32;
+    __syncthreads();              // the tile before is consumed
+    store_tile();
+    const bool lost0 = lost[0], lost1 = lost[1];
+    __syncthreads();
+    if (tile + 2 < t1) load_tile();
+    __builtin_amdgcn_sched_barrier(0);
+    if (kv >= seen_last) continue;                  // (the whole wave) no row sees a key of the tile
+    af32x16 s[2];
+#pragma unroll
+    for (int jt = 0; jt < 2; ++jt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[jt][e] = 0.f;
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int jt = 0; jt < 2; ++jt) {
+        const abf16x8 kf = *reinterpret_cast<const abf16x8*>(k_lds + (jt * 32 + l31) * KSTR + ks * 32 + lhi * 16);
+        s[jt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[jt], 0, 0, 0);
+      }
+    __builtin_amdgcn_s_setprio(0);
+    // register e of a product holds key 8 (e / 4) + 4 lhi + e % 4
+    if (kv + 64 > seen_first || lost0 || lost1) {
+#pragma unroll
+      for (int jt = 0; jt < 2; ++jt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if ((jt ? lost1 : lost0) || kv + jt * 32 + 8 * (e >> 2) + 4 * lhi + (e & 3) >= seen) s[jt][e] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int jt = 0; jt < 2; ++jt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[jt][e]);
+    if (__any(top > m + slack || (m == -INFINITY && top > m))) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float moved = top > m + slack || m == -INFINITY ? fmaxf(top, m) : m;
+      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift - moved * a.scale_log2);
+      m = moved;
+      shift = m == -INFINITY ? 0.f : m * a.scale_log2;
+      sum *= alpha;
+#pragma unroll
+      for (int i = 0; i < NG; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+    }
+    abf16x8 pf[4];
+#pragma unroll
+    for (int jt = 0; jt < 2; ++jt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        au32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[jt][8 * u + 2 * e], a.scale_log2, -shift));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[jt][8 * u + 2 * e + 1], a.scale_log2, -shift));
+          sum += p0 + p1;
+          w[e] = pack2_k(p0, p1);
+        }
+        pf[jt * 2 + u] = __builtin_bit_cast(abf16x8, w);
+      }
+#pragma unroll
+    for (int ku = 0; ku < 4; ++ku)
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const abf16x8 vf = *reinterpret_cast<const abf16x8*>(v_lds + (i * 32 + l31) * VSTR + ku * 32 + lhi * 16);
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ku], o[i], 0, 0, 0);
+      }
+  }
+  if (bad && a.err && lane == 0) atomicOr(a.err, 1);
+
+  // ---- register e of o[i] is row 16 (2 i + e / 8) + 8 (e / 4 % 2) + 4 lhi + e % 4 of the V^T tile
+  sum += __shfl_xor(sum, 32);
+  if (r >= rb.rows) return;
+  const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+  const int64_t at = (int64_t)blockIdx.x * ROWS + 32 * wave + l31;
+  if (t.shares > 1 && lhi == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m == -INFINITY ? m : shift, sum);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int j = 8 * (e >> 2) + 4 * lhi + (e & 3);
+    float x[2 * NG];
+#pragma unroll
+    for (int d = 0; d < 2 * NG; ++d) x[d] = o[d >> 1][8 * (d & 1) + e];
+    if (t.shares > 1) {
+      af32x4* to = reinterpret_cast<af32x4*>(a.part_o + at * D + j * (2 * NG));
+#pragma unroll
+      for (int d = 0; d < 2 * NG; d += 4) to[d / 4] = af32x4{x[d], x[d + 1], x[d + 2], x[d + 3]};
+    } else {
+      words w;
+#pragma unroll
+      for (int d = 0; d < NG; ++d) w[d] = pack2_k(x[2 * d] * inv, x[2 * d + 1] * inv);
+      *reinterpret_cast<words*>(a.out + (t.seq.q0 + query) * a.out_row + head * D + j * (2 * NG)) = w;
+    }
+  }
+}
+
+// ---- the shares of a row's keys, joined: 16 lanes a part, `join` parts of a row at a time, in an order that depends on
+// the lengths alone
+template <int NG>
+__global__ __launch_bounds__(256) void join_shares_kernel(CacheAttnArgs a) {
+  constexpr int D = 32 * NG;
+  __shared__ __align__(16) float state_o[16][D + 4];
+  __shared__ float state_m[16], state_l[16];
+  const int per = 16 / a.join;                               // rows of a workgroup
+  const int block = blockIdx.x / a.join_groups, units = a.row_blocks * a.shape.n_kv_heads, b = block / units, unit = block - b * units;
+  const Sequence seq = sequence(a, b, a.rows);
+  if (unit >= seq.units) return;                             // (whole workgroups, before any barrier)
+  const int4 share = *reinterpret_cast<const int4*>(a.share_of + 4 * b);
+  const int first = share.x, chunk = share.z;
+  if (share.y == 1) return;
+  const RowBlock rb = row_block(a, seq, unit, a.rows);
+  const int slot = threadIdx.x >> 4, jc = (threadIdx.x & 15) * (2 * NG);
+  const int in_block = (blockIdx.x - block * a.join_groups) * per + slot / a.join;
+  const int r = in_block < a.rows ? rb.first + in_block : rb.rows;
+  const int seen_tiles = (rb.seen + 31) >> 5, used = seen_tiles > 0 ? (seen_tiles + chunk - 1) / chunk : 1;
+  float mm = -INFINITY, ll = 0.f, acc[2 * NG] = {};
+  if (r < rb.rows) {
+    const int64_t at = ((int64_t)first + unit) * a.rows + in_block, step = (int64_t)seq.units * a.rows;
+    constexpr int AHEAD = 4;                                 // parts asked for at a time
+    for (int s0 = slot % a.join; s0 < used; s0 += AHEAD * a.join) {
+      float2 ml[AHEAD];
+      af32x4 v[AHEAD][NG / 2];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int s = s0 + u * a.join < used ? s0 + u * a.join : s0;
+        ml[u] = *reinterpret_cast<const float2*>(a.part_ml + (at + s * step) * 2);
+#pragma unroll
+        for (int i = 0; i < NG / 2; ++i) v[u][i] = reinterpret_cast<const af32x4*>(a.part_o + (at + s * step) * D + jc)[i];
+      }
+      float top = mm;
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) top = fmaxf(top, ml[u].x);
+      const float keep = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mm - top);
+      mm = top;
+      ll *= keep;
+#pragma unroll
+      for (int i = 0; i < 2 * NG; ++i) acc[i] *= keep;
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        if (s0 + u * a.join >= used) continue;
+        const float f = ml[u].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[u].x - mm);    // (a NaN weight stays one)
+        ll += f * ml[u].y;
+#pragma unroll
+        for (int i = 0; i < 2 * NG; ++i) acc[i] += f * v[u][i >> 2][i & 3];
+      }
+    }
+  }
+  if (a.join > 1) {
+    state_m[slot] = mm;
+    state_l[slot] = ll;
+#pragma unroll
+    for (int i = 0; i < 2 * NG; i += 4) *reinterpret_cast<af32x4*>(&state_o[slot][jc + i]) = af32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+    __syncthreads();
+    if (slot % a.join) return;
+    for (int u = 0; u < a.join; ++u) mm = fmaxf(mm, state_m[slot + u]);
+    ll = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * NG; ++i) acc[i] = 0.f;
+    for (int u = 0; u < a.join; ++u) {
+      const float mu = state_m[slot + u], f = mu == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mu - mm);
+      ll += f * state_l[slot + u];
+#pragma unroll
+      for (int i = 0; i < 2 * NG; ++i) acc[i] += f * state_o[slot + u][jc + i];
+    }
+  }
+  if (r < rb.rows) store_row<NG>(a, seq.q0, rb.h, r, jc, acc, ll);
 }
 
 size_t plan_cache_attention(CacheAttnArgs& a) {
-  const int64_t rows = (int64_t)a.max_queries * a.group;
-  a.row_tiles = (int32_t)((rows + 15) / 16);
-  const int64_t tiles = std::max<int64_t>(1, (a.max_keys + 31) / 32), base = std::max<int64_t>(1, (int64_t)a.n_seqs * a.shape.n_kv_heads * a.row_tiles);
-  // four workgroups of four waves a compute unit, two tiles a wave at least
-  const int64_t want = (1024 + base - 1) / base;
-  a.chunk = (int32_t)std::max<int64_t>(8, (tiles + want - 1) / want);
-  a.splits = (int32_t)((tiles + a.chunk - 1) / a.chunk);
-  if (a.splits <= 1) return 0;
-  const size_t parts = (size_t)a.splits * (size_t)a.n_queries * (size_t)a.n_heads;
-  return parts * (size_t)(a.shape.head_dim + 2) * 4;
+  const int64_t rows = (int64_t)a.max_queries * a.group, tiles = (a.max_keys + 31) / 32;
+  // rows of a workgroup, and workgroups that are on the chip at once (registers and LDS)
+  a.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  a.target = a.rows == 16 || a.rows == 64 ? 1024 : a.rows == 256 ? 256 : 512;
+  a.least = 8;
+  a.row_blocks = (int32_t)((rows + a.rows - 1) / a.rows);
+  const int64_t units = (int64_t)a.n_seqs * a.shape.n_kv_heads * a.row_blocks, most = std::max<int64_t>(1, (tiles + a.least - 1) / a.least);
+  // (see find_share: a share is at least `least` tiles, and more than the work over `target`)
+  const int64_t blocks = most > (1 << 20) ? units + a.target + 64 : std::min(units * most, units + a.target + 64);
+  a.blocks = blocks > 0x7fffffff ? 0 : (int32_t)blocks;
+  a.join = most == 1 ? 0 : 1;
+  if (!a.join || !a.blocks) return 0;
+  // a row's parts at a time: sixteen while the chip has room for the threads
+  const int64_t of_block = std::min<int64_t>(rows, a.rows);
+  while (a.join < 16 && a.join < most && units * of_block * a.join * 2 <= 32768) a.join *= 2;
+  a.join_groups = (int32_t)((of_block * a.join + 15) / 16);
+  return (size_t)a.blocks * (size_t)a.rows * (size_t)(a.shape.head_dim + 2) * 4 + (size_t)a.n_seqs * 16;
+}
+
+template <int NG>
+static void launch_attend(const CacheAttnArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)a.blocks);
+  if (a.rows == 16) hipLaunchKernelGGL((attend_rows_kernel<NG, 1>), grid, dim3(256), 0, stream, a);
+  else if (a.rows == 32) hipLaunchKernelGGL((attend_rows_kernel<NG, 2>), grid, dim3(256), 0, stream, a);
+  else if (a.rows == 64) hipLaunchKernelGGL((attend_block_kernel<NG, 2>), grid, dim3(128), 0, stream, a);
+  else if (a.rows == 128) hipLaunchKernelGGL((attend_block_kernel<NG, 4>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((attend_block_kernel<NG, 8>), grid, dim3(512), 0, stream, a);
 }
 
 cs_status launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream) {
-  const int64_t units = (int64_t)a.n_seqs * a.shape.n_kv_heads * a.row_tiles, blocks = units * a.splits;
-  if (blocks > 0x7fffffff) return fail(CS_ERR_UNSUPPORTED, "cs_attention_cache: too many rows");
-  if (a.shape.head_dim == 128) hipLaunchKernelGGL((attend_rows_kernel<4>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((attend_rows_kernel<2>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
+  const int64_t joins = (int64_t)a.n_seqs * a.shape.n_kv_heads * a.row_blocks * a.join_groups;
+  if (!a.blocks || joins > 0x7fffffff) return fail(CS_ERR_UNSUPPORTED, "cs_attention_cache: too many rows");
+  if (a.shape.head_dim == 128) launch_attend<4>(a, stream);
+  else launch_attend<2>(a, stream);
   CS_HIP(hipGetLastError());
-  if (a.splits > 1) {
-    if (a.shape.head_dim == 128) hipLaunchKernelGGL((join_splits_kernel<4>), dim3((unsigned)units), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((join_splits_kernel<2>), dim3((unsigned)units), dim3(256), 0, stream, a);
+  if (a.join) {
+    if (a.shape.head_dim == 128) hipLaunchKernelGGL((join_shares_kernel<4>), dim3((unsigned)joins), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((join_shares_kernel<2>), dim3((unsigned)joins), dim3(256), 0, stream, a);
     CS_HIP(hipGetLastError());
   }
   return CS_OK;

@@ -248,6 +248,18 @@ def test_on_another_stream_and_in_a_graph():
         assert torch.equal(out, b.run()), lens
 
 
+def test_a_query_of_nan_stays_one_and_its_own():
+    for lens in ([(1, 40), (1, 5000)], [(2, 3000), (3, 50)], [(70, 1500), (3, 50)]):
+        b = Batch(lens, 4, 2, 64, 32, seed=13)
+        clean = b.run()
+        q = b.q.clone()
+        q[1, 2, 7] = float("nan")
+        got = b.run(q=q)
+        assert got[1, 2].isnan().all()
+        got[1, 2] = clean[1, 2]
+        assert torch.equal(got, clean)
+
+
 def test_nothing_to_do():
     b = Batch([(1, 5)], 4, 2, 64, 32)
     out = torch.full((1, 4, 64), 3.0, dtype=torch.bfloat16, device=DEV)
