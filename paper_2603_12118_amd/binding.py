@@ -530,22 +530,30 @@ def cs_attention_varlen_groups(qk, vt, out, seg_cu: Sequence[int], n_heads: int,
 # tensor costs 0.1 to 0.3 us, so each is looked at once.)
 def _rows(x, heads: int, dim: int, name: str):
     """-> (pointer, elements between rows) of [rows, heads, head_dim]"""
-    sr, sh, sd = x.stride()
-    if not x.is_cuda or sd != 1 or (sh != dim and heads > 1):
+    row, head, one = x.stride()
+    if one != 1 or not x.is_cuda or (head != dim and heads > 1):
         raise ValueError(f"{name}: heads of a row must be packed, on the GPU")
-    return x.data_ptr(), sr if sr >= heads * dim or x.shape[0] > 1 else heads * dim
+    return x.data_ptr(), row if row >= heads * dim or x.shape[0] > 1 else heads * dim
 
 
-def _flat(x, dtype, shape, name: str) -> int:
-    if not x.is_cuda or x.dtype is not dtype or x.shape != shape or not x.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape} on the GPU")
+def _given(x, shape, dtype, heads: int, dim: int, name: str):
+    """The same of a tensor to be written."""
+    if x.shape != shape or x.dtype is not dtype:
+        raise ValueError(f"{name}: expected {tuple(shape)} {dtype}")
+    return _rows(x, heads, dim, name)
+
+
+def _flat(x, dtype, size: int, name: str) -> int:
+    """Pointer of a contiguous tensor of `size` elements"""
+    if x.dtype is not dtype or x.numel() != size or not x.is_contiguous() or not x.is_cuda:
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {size} elements on the GPU")
     return x.data_ptr()
 
 
-def _empty(shape, like, stream, dtype=None):
+def _new(shape, like, dtype, stream):
     """A new tensor of the stream the call runs on (the current one unless given), so that its memory is free there."""
     if stream is None:
-        return like.new_empty(shape, dtype=dtype)
+        return like.new_empty(shape) if dtype is like.dtype else like.new_empty(shape, dtype=dtype)
     import torch
     with torch.cuda.stream(stream):
         return like.new_empty(shape, dtype=dtype)
@@ -556,8 +564,7 @@ def _call_stream(stream, like) -> int:
     return torch._C._cuda_getCurrentRawStream(like.device.index) if stream is None else stream.cuda_stream
 
 
-def _code(dtype) -> int:
-    import torch
+def _code(dtype, torch) -> int:
     if dtype is torch.bfloat16:
         return CS_BF16
     if dtype is torch.float32:
@@ -565,45 +572,39 @@ def _code(dtype) -> int:
     raise TypeError("rows must be bf16 or fp32")
 
 
-def _flag(err_flag):
-    if err_flag is None:
-        return None
-    import torch
-    return _flat(err_flag, torch.int32, (1,), "err_flag")
-
-
 def cs_qk_norm_rope(q, k, cos_sin, positions, sections, q_gain=None, k_gain=None, eps: float = 1e-6, interleaved: bool = False,
                     q_out=None, k_out=None, err_flag=None, stream=None):
     """Queries [T, heads, head_dim] and keys [T, kv_heads, head_dim] (parts of one packed QKV tensor, say) normed per head where
     gains (fp32 [head_dim]) are given, and rotated: cos_sin fp32 [n_positions, pairs, 2], positions int32 [T, axes],
     `sections` pairs per axis.  Returns (q_out, k_out), new tensors unless given (q, k themselves to work in place)."""
-    from torch import float32, int32
+    import torch
     T, H, D = q_shape = q.shape
-    K, axes, dtype = k.shape[1], len(sections), q.dtype
-    n, half, _ = cs_shape = cos_sin.shape
-    k_shape = (T, K, D)
-    if k.shape != k_shape or k.dtype is not dtype:
+    KT, K, KD = k_shape = k.shape
+    n, half, two = cos_sin.shape
+    axes, dtype, f32 = len(sections), q.dtype, torch.float32
+    if KT != T or KD != D or k.dtype is not dtype:
         raise ValueError("k: expected the rows, head_dim and type of q")
-    if axes > 3:
-        raise ValueError("sections: at most three axes")
-    if q_out is None:
-        q_out = _empty(q_shape, q, stream)
-    elif q_out.shape != q_shape or q_out.dtype is not dtype:
-        raise ValueError("q_out: expected the shape and type of q")
-    if k_out is None:
-        k_out = _empty(k_shape, q, stream)
-    elif k_out.shape != k_shape or k_out.dtype is not dtype:
-        raise ValueError("k_out: expected the shape and type of k")
+    if axes > 3 or two != 2:
+        raise ValueError("sections, cos_sin: expected at most three axes, and pairs of cos and sin")
+    code = _code(dtype, torch)
     qp, qs = _rows(q, H, D, "q")
     kp, ks = _rows(k, K, D, "k")
-    qo, qos = _rows(q_out, H, D, "q_out")
-    ko, kos = _rows(k_out, K, D, "k_out")
+    if q_out is None:
+        q_out = _new(q_shape, q, dtype, stream)
+        qo, qos = q_out.data_ptr(), H * D
+    else:
+        qo, qos = _given(q_out, q_shape, dtype, H, D, "q_out")
+    if k_out is None:
+        k_out = _new(k_shape, q, dtype, stream)
+        ko, kos = k_out.data_ptr(), K * D
+    else:
+        ko, kos = _given(k_out, k_shape, dtype, K, D, "k_out")
     c = cs_qk_config(_QK_SIZE, H, K, D, 2 * half, axes, interleaved, tuple(sections), n, eps)
-    _check(lib().cs_qk_norm_rope(C.byref(c), qp, qs, kp, ks, qo, qos, ko, kos, _code(dtype),
-                                 None if q_gain is None else _flat(q_gain, float32, (D,), "q_gain"),
-                                 None if k_gain is None else _flat(k_gain, float32, (D,), "k_gain"),
-                                 _flat(cos_sin, float32, (n, half, 2), "cos_sin"), _flat(positions, int32, (T, axes), "positions"), T,
-                                 _flag(err_flag), _call_stream(stream, q)))
+    _check(lib().cs_qk_norm_rope(C.byref(c), qp, qs, kp, ks, qo, qos, ko, kos, code,
+                                 None if q_gain is None else _flat(q_gain, f32, D, "q_gain"),
+                                 None if k_gain is None else _flat(k_gain, f32, D, "k_gain"),
+                                 _flat(cos_sin, f32, 2 * n * half, "cos_sin"), _flat(positions, torch.int32, T * axes, "positions"), T,
+                                 None if err_flag is None else _flat(err_flag, torch.int32, 1, "err_flag"), _call_stream(stream, q)))
     return q_out, k_out
 
 
@@ -614,48 +615,47 @@ def cs_cache_query(n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: in
     return page.value, pool.value
 
 
-def _cache(pool, n_kv_heads: int, head_dim: int, page_tokens: int):
+def _cache(pool, n_kv_heads: int, head_dim: int, page_tokens: int, torch):
     """-> (config, pointer) of a pool tensor [n_pages, page bytes]"""
-    import torch
-    n = pool.shape[0]
-    return (cs_cache_config(_CACHE_SIZE, n_kv_heads, head_dim, page_tokens, n),
-            _flat(pool, torch.uint8, (n, n_kv_heads * page_tokens * (head_dim + head_dim // 16)), "pool (pages of cs_cache_query's bytes)"))
+    n, page = pool.shape
+    if page != n_kv_heads * page_tokens * (head_dim + head_dim // 16):
+        raise ValueError("pool: expected [n_pages, page bytes] as cs_cache_query says")
+    return cs_cache_config(_CACHE_SIZE, n_kv_heads, head_dim, page_tokens, n), _flat(pool, torch.uint8, n * page, "pool")
 
 
 def cs_cache_write(pool, k, v, slots, page_tokens: int, err_flag=None, stream=None) -> None:
     """pool[slots[t]] = (k[t], v[t]) in 4 bits; k, v [T, kv_heads, head_dim] bf16 or fp32, slots int64 [T] (-1: no slot)."""
-    from torch import int64
+    import torch
     T, K, D = shape = k.shape
     dtype = k.dtype
-    if v.shape != shape or v.dtype is not dtype:
-        raise ValueError("v: expected the shape and type of k")
-    c, pp = _cache(pool, K, D, page_tokens)
+    c, pp = _cache(pool, K, D, page_tokens, torch)
     kp, ks = _rows(k, K, D, "k")
-    vp, vs = _rows(v, K, D, "v")
-    _check(lib().cs_cache_write(C.byref(c), pp, kp, ks, vp, vs, _code(dtype), _flat(slots, int64, (T,), "slots"), T, _flag(err_flag),
-                                _call_stream(stream, k)))
+    vp, vs = _given(v, shape, dtype, K, D, "v")
+    _check(lib().cs_cache_write(C.byref(c), pp, kp, ks, vp, vs, _code(dtype, torch), _flat(slots, torch.int64, T, "slots"), T,
+                                None if err_flag is None else _flat(err_flag, torch.int32, 1, "err_flag"), _call_stream(stream, k)))
 
 
 def cs_cache_read(pool, slots, n_kv_heads: int, head_dim: int, page_tokens: int, dtype=None, k=None, v=None, err_flag=None, stream=None):
     """The values the slots hold -> (k, v) [T, kv_heads, head_dim] of dtype (bf16 unless given)."""
-    from torch import bfloat16, int64
-    T = slots.shape[0]
+    import torch
+    T = slots.numel()
     shape = (T, n_kv_heads, head_dim)
     if dtype is None:
-        dtype = bfloat16 if k is None else k.dtype
-    c, pp = _cache(pool, n_kv_heads, head_dim, page_tokens)
+        dtype = torch.bfloat16 if k is None else k.dtype
+    code = _code(dtype, torch)
+    c, pp = _cache(pool, n_kv_heads, head_dim, page_tokens, torch)
     if k is None:
-        k = _empty(shape, pool, stream, dtype)
-    elif k.shape != shape or k.dtype is not dtype:
-        raise ValueError(f"k: expected {shape} {dtype}")
+        k = _new(shape, pool, dtype, stream)
+        kp, ks = k.data_ptr(), n_kv_heads * head_dim
+    else:
+        kp, ks = _given(k, shape, dtype, n_kv_heads, head_dim, "k")
     if v is None:
-        v = _empty(shape, pool, stream, dtype)
-    elif v.shape != shape or v.dtype is not dtype:
-        raise ValueError(f"v: expected {shape} {dtype}")
-    kp, ks = _rows(k, n_kv_heads, head_dim, "k")
-    vp, vs = _rows(v, n_kv_heads, head_dim, "v")
-    _check(lib().cs_cache_read(C.byref(c), pp, _flat(slots, int64, (T,), "slots"), T, kp, ks, vp, vs, _code(dtype), _flag(err_flag),
-                               _call_stream(stream, pool)))
+        v = _new(shape, pool, dtype, stream)
+        vp, vs = v.data_ptr(), n_kv_heads * head_dim
+    else:
+        vp, vs = _given(v, shape, dtype, n_kv_heads, head_dim, "v")
+    _check(lib().cs_cache_read(C.byref(c), pp, _flat(slots, torch.int64, T, "slots"), T, kp, ks, vp, vs, code,
+                               None if err_flag is None else _flat(err_flag, torch.int32, 1, "err_flag"), _call_stream(stream, pool)))
     return k, v
 
 
@@ -664,30 +664,32 @@ def cs_attention_cache(q, pool, page_table, n_keys, cu_queries, max_queries: int
     """Attention of q [T, heads, head_dim] bf16 over the cache: sequence b has the rows cu_queries[b] .. cu_queries[b + 1] and
     n_keys[b] keys in the pages page_table[b] (int32 tensors on the GPU).  Returns out [T, heads, head_dim]; a workspace of fewer
     bytes than needed (or None) is replaced by a new one."""
-    from torch import bfloat16, int32, uint8
-    T, H, D = q_shape = q.shape
-    if q.dtype is not bfloat16:
+    import torch
+    dtype, i32 = q.dtype, torch.int32
+    if dtype is not torch.bfloat16:
         raise TypeError("q must be bf16")
-    c, pp = _cache(pool, n_kv_heads, D, page_tokens)
+    T, H, D = shape = q.shape
     B, width = page_table.shape
-    b = cs_cache_batch(_BATCH_SIZE, B, T, max_queries, width, max_keys, _flat(cu_queries, int32, (B + 1,), "cu_queries"),
-                       _flat(n_keys, int32, (B,), "n_keys"), _flat(page_table, int32, (B, width), "page_table"))
-    if out is None:
-        out = _empty(q_shape, q, stream)
-    elif out.shape != q_shape or out.dtype is not bfloat16:
-        raise ValueError("out: expected the shape and type of q")
+    c, pp = _cache(pool, n_kv_heads, D, page_tokens, torch)
     qp, qs = _rows(q, H, D, "q")
-    op, os_ = _rows(out, H, D, "out")
-    L, need, ws = lib(), C.c_size_t(), None
-    _check(L.cs_attention_cache_query(C.byref(c), C.byref(b), H, C.byref(need)))
-    if need.value:
-        if workspace is None or workspace.nbytes < need.value:
-            workspace = _empty((need.value,), q, stream, uint8)
+    if out is None:
+        out = _new(shape, q, dtype, stream)
+        op, os_ = out.data_ptr(), H * D
+    else:
+        op, os_ = _given(out, shape, dtype, H, D, "out")
+    b = cs_cache_batch(_BATCH_SIZE, B, T, max_queries, width, max_keys, _flat(cu_queries, i32, B + 1, "cu_queries"),
+                       _flat(n_keys, i32, B, "n_keys"), _flat(page_table, i32, B * width, "page_table"))
+    L, cp, bp, need, ws = lib(), C.byref(c), C.byref(b), C.c_size_t(), None
+    _check(L.cs_attention_cache_query(cp, bp, H, C.byref(need)))
+    size = need.value
+    if size:
+        if workspace is None or workspace.nbytes < size:
+            workspace = _new((size,), q, torch.uint8, stream)
         elif not workspace.is_cuda or not workspace.is_contiguous():
             raise ValueError("workspace: expected a contiguous tensor on the GPU")
         ws = workspace.data_ptr()
-    _check(L.cs_attention_cache(C.byref(c), pp, C.byref(b), qp, qs, op, os_, H, D ** -0.5 if scale is None else scale, causal, ws, need.value,
-                                _flag(err_flag), _call_stream(stream, q)))
+    _check(L.cs_attention_cache(cp, pp, bp, qp, qs, op, os_, H, D ** -0.5 if scale is None else scale, causal, ws, size,
+                                None if err_flag is None else _flat(err_flag, i32, 1, "err_flag"), _call_stream(stream, q)))
     return out
 
 
