@@ -61,9 +61,6 @@ class cs_cache_batch(C.Structure):
                 ("page_table", C.c_void_p)]
 
 
-_QK_SIZE, _CACHE_SIZE, _BATCH_SIZE = (C.sizeof(t) for t in (cs_qk_config, cs_cache_config, cs_cache_batch))
-
-
 class cs_tensor(C.Structure):
     _fields_ = [("name", C.c_char_p), ("data", C.c_void_p), ("numel", C.c_int64)]
 
@@ -526,50 +523,28 @@ def cs_attention_varlen_groups(qk, vt, out, seg_cu: Sequence[int], n_heads: int,
 
 
 # ---- the LLM task's attention: tensors of heads are [rows, heads, head_dim] with packed heads; rows may lie apart.
-# (A decode step makes these calls once a layer on a few rows, where the time of a call is the host's: every look at a
-# tensor costs 0.1 to 0.3 us, so each is looked at once.)
-def _rows(x, heads: int, dim: int, name: str):
-    """-> (pointer, elements between rows) of [rows, heads, head_dim]"""
-    row, head, one = x.stride()
-    if one != 1 or not x.is_cuda or (head != dim and heads > 1):
-        raise ValueError(f"{name}: heads of a row must be packed, on the GPU")
-    return x.data_ptr(), row if row >= heads * dim or x.shape[0] > 1 else heads * dim
+# A decode step makes these calls once a layer on a few rows, where the time of a call is the host's, so the tensors are
+# looked at in C++ (csrc/calls.cpp); everything is refused there or by the C entry point, before anything is enqueued.
+_calls_module = None
 
 
-def _given(x, shape, dtype, heads: int, dim: int, name: str):
-    """The same of a tensor to be written."""
-    if x.shape != shape or x.dtype is not dtype:
-        raise ValueError(f"{name}: expected {tuple(shape)} {dtype}")
-    return _rows(x, heads, dim, name)
+def _calls():
+    global _calls_module
+    if _calls_module is None:
+        lib()
+        import torch  # noqa: F401  (its libraries are the module's)
+        try:
+            from . import _calls as m
+        except ImportError as e:
+            raise RuntimeError(f"_calls.so is not built ({e}); run __graft_entry__.build() (python -m paper_2603_12118_amd.build)") from e
+        _calls_module = m
+    return _calls_module
 
 
-def _flat(x, dtype, size: int, name: str) -> int:
-    """Pointer of a contiguous tensor of `size` elements"""
-    if x.dtype is not dtype or x.numel() != size or not x.is_contiguous() or not x.is_cuda:
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {size} elements on the GPU")
-    return x.data_ptr()
-
-
-def _new(shape, like, dtype, stream):
-    """A new tensor of the stream the call runs on (the current one unless given), so that its memory is free there."""
-    if stream is None:
-        return like.new_empty(shape) if dtype is like.dtype else like.new_empty(shape, dtype=dtype)
+def _on(stream):
+    """Current stream for a call that was given one (its new tensors are then that stream's, too)."""
     import torch
-    with torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
-
-
-def _call_stream(stream, like) -> int:
-    import torch
-    return torch._C._cuda_getCurrentRawStream(like.device.index) if stream is None else stream.cuda_stream
-
-
-def _code(dtype, torch) -> int:
-    if dtype is torch.bfloat16:
-        return CS_BF16
-    if dtype is torch.float32:
-        return CS_F32
-    raise TypeError("rows must be bf16 or fp32")
+    return torch.cuda.stream(stream)
 
 
 def cs_qk_norm_rope(q, k, cos_sin, positions, sections, q_gain=None, k_gain=None, eps: float = 1e-6, interleaved: bool = False,
@@ -577,120 +552,64 @@ def cs_qk_norm_rope(q, k, cos_sin, positions, sections, q_gain=None, k_gain=None
     """Queries [T, heads, head_dim] and keys [T, kv_heads, head_dim] (parts of one packed QKV tensor, say) normed per head where
     gains (fp32 [head_dim]) are given, and rotated: cos_sin fp32 [n_positions, pairs, 2], positions int32 [T, axes],
     `sections` pairs per axis.  Returns (q_out, k_out), new tensors unless given (q, k themselves to work in place)."""
-    import torch
-    T, H, D = q_shape = q.shape
-    KT, K, KD = k_shape = k.shape
-    n, half, two = cos_sin.shape
-    axes, dtype, f32 = len(sections), q.dtype, torch.float32
-    if KT != T or KD != D or k.dtype is not dtype:
-        raise ValueError("k: expected the rows, head_dim and type of q")
-    if axes > 3 or two != 2:
-        raise ValueError("sections, cos_sin: expected at most three axes, and pairs of cos and sin")
-    code = _code(dtype, torch)
-    qp, qs = _rows(q, H, D, "q")
-    kp, ks = _rows(k, K, D, "k")
-    if q_out is None:
-        q_out = _new(q_shape, q, dtype, stream)
-        qo, qos = q_out.data_ptr(), H * D
-    else:
-        qo, qos = _given(q_out, q_shape, dtype, H, D, "q_out")
-    if k_out is None:
-        k_out = _new(k_shape, q, dtype, stream)
-        ko, kos = k_out.data_ptr(), K * D
-    else:
-        ko, kos = _given(k_out, k_shape, dtype, K, D, "k_out")
-    c = cs_qk_config(_QK_SIZE, H, K, D, 2 * half, axes, interleaved, tuple(sections), n, eps)
-    _check(lib().cs_qk_norm_rope(C.byref(c), qp, qs, kp, ks, qo, qos, ko, kos, code,
-                                 None if q_gain is None else _flat(q_gain, f32, D, "q_gain"),
-                                 None if k_gain is None else _flat(k_gain, f32, D, "k_gain"),
-                                 _flat(cos_sin, f32, 2 * n * half, "cos_sin"), _flat(positions, torch.int32, T * axes, "positions"), T,
-                                 None if err_flag is None else _flat(err_flag, torch.int32, 1, "err_flag"), _call_stream(stream, q)))
-    return q_out, k_out
+    if stream is not None:
+        with _on(stream):
+            return cs_qk_norm_rope(q, k, cos_sin, positions, sections, q_gain, k_gain, eps, interleaved, q_out, k_out, err_flag)
+    r = _calls().qk_norm_rope(q, k, cos_sin, positions, sections, q_gain, k_gain, eps, interleaved, q_out, k_out, err_flag)
+    if type(r) is int:
+        _check(r)
+    return r
 
 
 def cs_cache_query(n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int = 1):
     """Host-only: (bytes of a page, bytes of the pool).  A pool is a uint8 tensor [n_pages, page bytes]."""
-    c, page, pool = cs_cache_config(_CACHE_SIZE, n_kv_heads, head_dim, page_tokens, n_pages), C.c_size_t(), C.c_size_t()
+    c = cs_cache_config(C.sizeof(cs_cache_config), n_kv_heads, head_dim, page_tokens, n_pages)
+    page, pool = C.c_size_t(), C.c_size_t()
     _check(lib().cs_cache_query(C.byref(c), C.byref(page), C.byref(pool)))
     return page.value, pool.value
 
 
-def _cache(pool, n_kv_heads: int, head_dim: int, page_tokens: int, torch):
-    """-> (config, pointer) of a pool tensor [n_pages, page bytes]"""
-    n, page = pool.shape
-    if page != n_kv_heads * page_tokens * (head_dim + head_dim // 16):
-        raise ValueError("pool: expected [n_pages, page bytes] as cs_cache_query says")
-    return cs_cache_config(_CACHE_SIZE, n_kv_heads, head_dim, page_tokens, n), _flat(pool, torch.uint8, n * page, "pool")
-
-
 def cs_cache_write(pool, k, v, slots, page_tokens: int, err_flag=None, stream=None) -> None:
     """pool[slots[t]] = (k[t], v[t]) in 4 bits; k, v [T, kv_heads, head_dim] bf16 or fp32, slots int64 [T] (-1: no slot)."""
-    import torch
-    T, K, D = shape = k.shape
-    dtype = k.dtype
-    c, pp = _cache(pool, K, D, page_tokens, torch)
-    kp, ks = _rows(k, K, D, "k")
-    vp, vs = _given(v, shape, dtype, K, D, "v")
-    _check(lib().cs_cache_write(C.byref(c), pp, kp, ks, vp, vs, _code(dtype, torch), _flat(slots, torch.int64, T, "slots"), T,
-                                None if err_flag is None else _flat(err_flag, torch.int32, 1, "err_flag"), _call_stream(stream, k)))
+    if stream is not None:
+        with _on(stream):
+            return cs_cache_write(pool, k, v, slots, page_tokens, err_flag)
+    r = _calls().cache_write(pool, k, v, slots, page_tokens, err_flag)
+    if r is not None:
+        _check(r)
 
 
 def cs_cache_read(pool, slots, n_kv_heads: int, head_dim: int, page_tokens: int, dtype=None, k=None, v=None, err_flag=None, stream=None):
     """The values the slots hold -> (k, v) [T, kv_heads, head_dim] of dtype (bf16 unless given)."""
     import torch
-    T = slots.numel()
-    shape = (T, n_kv_heads, head_dim)
+    if stream is not None:
+        with _on(stream):
+            return cs_cache_read(pool, slots, n_kv_heads, head_dim, page_tokens, dtype, k, v, err_flag)
     if dtype is None:
         dtype = torch.bfloat16 if k is None else k.dtype
-    code = _code(dtype, torch)
-    c, pp = _cache(pool, n_kv_heads, head_dim, page_tokens, torch)
-    if k is None:
-        k = _new(shape, pool, dtype, stream)
-        kp, ks = k.data_ptr(), n_kv_heads * head_dim
-    else:
-        kp, ks = _given(k, shape, dtype, n_kv_heads, head_dim, "k")
-    if v is None:
-        v = _new(shape, pool, dtype, stream)
-        vp, vs = v.data_ptr(), n_kv_heads * head_dim
-    else:
-        vp, vs = _given(v, shape, dtype, n_kv_heads, head_dim, "v")
-    _check(lib().cs_cache_read(C.byref(c), pp, _flat(slots, torch.int64, T, "slots"), T, kp, ks, vp, vs, code,
-                               None if err_flag is None else _flat(err_flag, torch.int32, 1, "err_flag"), _call_stream(stream, pool)))
-    return k, v
+    code = CS_BF16 if dtype is torch.bfloat16 else CS_F32 if dtype is torch.float32 else -1
+    if code < 0:
+        raise TypeError("rows must be bf16 or fp32")
+    r = _calls().cache_read(pool, slots, n_kv_heads, head_dim, page_tokens, code, k, v, err_flag)
+    if type(r) is int:
+        _check(r)
+    return r
 
 
 def cs_attention_cache(q, pool, page_table, n_keys, cu_queries, max_queries: int, max_keys: int, n_kv_heads: int, page_tokens: int,
                        scale: Optional[float] = None, causal: bool = True, out=None, workspace=None, err_flag=None, stream=None):
     """Attention of q [T, heads, head_dim] bf16 over the cache: sequence b has the rows cu_queries[b] .. cu_queries[b + 1] and
-    n_keys[b] keys in the pages page_table[b] (int32 tensors on the GPU).  Returns out [T, heads, head_dim]; a workspace of fewer
-    bytes than needed (or None) is replaced by a new one."""
-    import torch
-    dtype, i32 = q.dtype, torch.int32
-    if dtype is not torch.bfloat16:
-        raise TypeError("q must be bf16")
-    T, H, D = shape = q.shape
-    B, width = page_table.shape
-    c, pp = _cache(pool, n_kv_heads, D, page_tokens, torch)
-    qp, qs = _rows(q, H, D, "q")
-    if out is None:
-        out = _new(shape, q, dtype, stream)
-        op, os_ = out.data_ptr(), H * D
-    else:
-        op, os_ = _given(out, shape, dtype, H, D, "out")
-    b = cs_cache_batch(_BATCH_SIZE, B, T, max_queries, width, max_keys, _flat(cu_queries, i32, B + 1, "cu_queries"),
-                       _flat(n_keys, i32, B, "n_keys"), _flat(page_table, i32, B * width, "page_table"))
-    L, cp, bp, need, ws = lib(), C.byref(c), C.byref(b), C.c_size_t(), None
-    _check(L.cs_attention_cache_query(cp, bp, H, C.byref(need)))
-    size = need.value
-    if size:
-        if workspace is None or workspace.nbytes < size:
-            workspace = _new((size,), q, torch.uint8, stream)
-        elif not workspace.is_cuda or not workspace.is_contiguous():
-            raise ValueError("workspace: expected a contiguous tensor on the GPU")
-        ws = workspace.data_ptr()
-    _check(L.cs_attention_cache(cp, pp, bp, qp, qs, op, os_, H, D ** -0.5 if scale is None else scale, causal, ws, size,
-                                None if err_flag is None else _flat(err_flag, i32, 1, "err_flag"), _call_stream(stream, q)))
-    return out
+    n_keys[b] keys in the pages page_table[b] (int32 tensors on the GPU); scale is 1/sqrt(head_dim) unless given.  Returns out
+    [T, heads, head_dim]; a workspace of fewer bytes than needed (or None) is replaced by a new one."""
+    if stream is not None:
+        with _on(stream):
+            return cs_attention_cache(q, pool, page_table, n_keys, cu_queries, max_queries, max_keys, n_kv_heads, page_tokens, scale, causal, out,
+                                      workspace, err_flag)
+    r = _calls().attention_cache(q, pool, page_table, n_keys, cu_queries, max_queries, max_keys, n_kv_heads, page_tokens, scale, causal, out,
+                                 workspace, err_flag)
+    if type(r) is int:
+        _check(r)
+    return r
 
 
 def cs_pack_batch(grid_thw, row_budget: int, max_items: int = 1 << 30):
