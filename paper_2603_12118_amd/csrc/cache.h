@@ -65,7 +65,7 @@ struct CacheAttnArgs {
   CacheShape shape;
   int32_t* err;
   // set by plan_cache_attention
-  int32_t rows;           // rows (a row: a query and a head) a workgroup takes: 16 or 32 (their keys shared out to its waves), 64, 128, 256
+  int32_t rows;           // rows (a row: a query and a head) a workgroup takes: 16 or 32 (their keys shared out to its waves) or 128
   int32_t row_blocks;     // blocks of so many rows that a sequence and key/value head have at most
   int32_t target;         // workgroups that fill the chip once
   int32_t least;          // tiles of 32 keys that a workgroup takes at least, if there are so many

@@ -408,16 +408,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 4
   }
 }
 
-// ---- many rows: 32 a wave, the waves' keys the same.  Tiles of 64 keys are widened once, into LDS, by the whole workgroup:
-// K as it is, V transposed, so that both products read 16 bytes a lane.  S^T = K Q^T and O^T = V^T P^T with
+// ---- many rows: 128 of them, 32 a wave, the waves' keys the same.  Tiles of 64 keys are widened once, into LDS, by the whole
+// workgroup (a thread: a quarter of a token of K, a word of four tokens of V): K as it is, V transposed, so that both products read
+// 16 bytes a lane.  S^T = K Q^T and O^T = V^T P^T with
 // v_mfma_f32_32x32x16_bf16: lane l has row l % 32 throughout, and what the exponential leaves is the second product's operand.
 // A column of V^T (value 2 NG j + d of a head, j = the word of a token that holds it) is row 16 d + j of the tile: the 16 lanes
 // that write one d then write neighbouring rows, and a lane's results come out 2 NG values at a time.
-template <int NG, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void attend_block_kernel(CacheAttnArgs a) {
-  constexpr int D = 32 * NG, ROWS = 32 * NW, NT = 64 * NW, KS = D / 16;
+template <int NG>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void attend_block_kernel(CacheAttnArgs a) {
+  constexpr int D = 32 * NG, ROWS = 128, KS = D / 16;
   constexpr int KSTR = D * 2 + 16, VSTR = 64 * 2 + 16;      // bytes between rows of the tiles
-  constexpr int ITEMS = NW == 8 ? 1 : 256 / NT;             // 256 pieces of K and 256 of V a tile; eight waves: half the waves each
   typedef typename Words<NG>::type words;
   __shared__ __align__(16) unsigned char k_lds[64 * KSTR];
   __shared__ __align__(16) unsigned char v_lds[D * VSTR];
@@ -466,9 +466,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
   };
   int pages = t1 > t0 ? load_pages() : 0;
   bool bad = false;
-  const bool does_k = NW < 8 || wave < 4, does_v = NW < 8 || wave >= 4;
-  words kw[ITEMS], vw[ITEMS];
-  uint32_t ksc[ITEMS], vsc[ITEMS];
+  words kw, vw;
+  uint32_t ksc, vsc;
+  // a thread's piece: token k_token of a half, part k_part of it; tokens 4 quad .., word j of each
+  const int half = wave >> 1, k_token = (tid >> 2) & 31, k_part = tid & 3, quad = (tid >> 4) & 7, j = tid & 15;
   bool lost[2];                 // halves of the tile in registers that are in no page
   auto load_tile = [&]() {      // the tile of 64 keys at (page, in_page) = `ahead` tiles of 32, and the step to the next
     int page1 = page, in1 = in_page + 1;
@@ -487,28 +488,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     bad |= lost[0] || lost[1];
     const unsigned char* block0 = a.pool + ((int64_t)(lost[0] ? 0 : id0) * a.shape.n_kv_heads + rb.h) * a.shape.head_bytes;
     const unsigned char* block1 = a.pool + ((int64_t)(lost[1] || !there ? 0 : id1) * a.shape.n_kv_heads + rb.h) * a.shape.head_bytes;
-#pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      const int i = (NW == 8 ? tid & 255 : tid) + u * NT;
-      const int half = __builtin_amdgcn_readfirstlane(i >> 7);       // (a wave's pieces lie in one half)
-      const unsigned char* block = half ? block1 : block0;
-      const int at = half ? in1 : in_page;
-      if (does_k) {
-        const int key = (i >> 2) & 31;
-        kw[u] = *reinterpret_cast<const words*>(block + at * (16 * D) + key * (D / 2) + (i & 3) * (4 * NG));
-        const unsigned char* sp = block + P * D + (at * 32 + key) * NG;
-        if constexpr (NG == 4) ksc[u] = *reinterpret_cast<const uint32_t*>(sp);
-        else ksc[u] = *reinterpret_cast<const uint16_t*>(sp);
-      }
-      if (does_v) {
-        const int quad = (i >> 4) & 7, j = i & 15;
-        vw[u] = *reinterpret_cast<const words*>(block + P * (D / 2) + at * (16 * D) + quad * (2 * D) + j * (4 * NG));
-        vsc[u] = *reinterpret_cast<const uint32_t*>(block + P * (D + NG) + at * (32 * NG) + (quad >> 1) * (8 * NG) + (j * NG >> 4) * 8 + (quad & 1) * 4);
-        // tokens that do not exist have a scale of nothing: their codes may be anything, their product with zero must be zero
-        const int held = (half ? lost[1] || !there : lost[0]) ? 0 : keys - (ahead * 32 + half * 32 + quad * 4);
-        if (held < 4) vsc[u] = held > 0 ? vsc[u] & ((1u << (8 * held)) - 1) : 0;
-      }
-    }
+    const unsigned char* block = half ? block1 : block0;
+    const int at = half ? in1 : in_page;
+    kw = *reinterpret_cast<const words*>(block + at * (16 * D) + k_token * (D / 2) + k_part * (4 * NG));
+    const unsigned char* sp = block + P * D + (at * 32 + k_token) * NG;
+    if constexpr (NG == 4) ksc = *reinterpret_cast<const uint32_t*>(sp);
+    else ksc = *reinterpret_cast<const uint16_t*>(sp);
+    vw = *reinterpret_cast<const words*>(block + P * (D / 2) + at * (16 * D) + quad * (2 * D) + j * (4 * NG));
+    vsc = *reinterpret_cast<const uint32_t*>(block + P * (D + NG) + at * (32 * NG) + (quad >> 1) * (8 * NG) + (j * NG >> 4) * 8 + (quad & 1) * 4);
+    // tokens that do not exist have a scale of nothing: their codes may be anything, their product with zero must be zero
+    const int held = (half ? lost[1] || !there : lost[0]) ? 0 : keys - (ahead * 32 + half * 32 + quad * 4);
+    if (held < 4) vsc = held > 0 ? vsc & ((1u << (8 * held)) - 1) : 0;
     ahead += 2;
     in_page = in1 + 1;
     page = page1;
@@ -517,48 +507,39 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
       ++page;
     }
   };
+  // (quads 1 and 2 of every four change places: the eight tokens of a lane's operand are then 16 bytes side by side)
+  const int place = 8 * half + ((quad & 4) | ((quad & 1) << 1) | ((quad >> 1) & 1));
+  unsigned char* const k_to = k_lds + (tid >> 2) * KSTR + k_part * 16;
+  unsigned char* const v_to = v_lds + j * VSTR + place * 8;
   auto store_tile = [&]() {
-#pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      const int i = (NW == 8 ? tid & 255 : tid) + u * NT;
-      if (does_k) {
-        unsigned char* to = k_lds + (i >> 2) * KSTR + (i & 3) * 16;
-        auto group = [&](auto G) {
-          constexpr int g = decltype(G)::value;
-          const uint32_t sc = scale_of<g>(ksc[u]);
-          *reinterpret_cast<au32x4*>(to + g * 64) =
-              au32x4{widen2<0>(kw[u][g], sc), widen2<1>(kw[u][g], sc), widen2<2>(kw[u][g], sc), widen2<3>(kw[u][g], sc)};
-        };
-        group(std::integral_constant<int, 0>());
-        group(std::integral_constant<int, 1>());
-        if constexpr (NG == 4) {
-          group(std::integral_constant<int, 2>());
-          group(std::integral_constant<int, 3>());
-        }
+    auto group = [&](auto G) {
+      constexpr int g = decltype(G)::value;
+      const uint32_t sc = scale_of<g>(ksc);
+      *reinterpret_cast<au32x4*>(k_to + g * 64) = au32x4{widen2<0>(kw[g], sc), widen2<1>(kw[g], sc), widen2<2>(kw[g], sc), widen2<3>(kw[g], sc)};
+    };
+    group(std::integral_constant<int, 0>());
+    group(std::integral_constant<int, 1>());
+    if constexpr (NG == 4) {
+      group(std::integral_constant<int, 2>());
+      group(std::integral_constant<int, 3>());
+    }
+    const uint32_t s0 = scale_of<0>(vsc), s1 = scale_of<1>(vsc), s2 = scale_of<2>(vsc), s3 = scale_of<3>(vsc);
+    auto column = [&](auto B) {
+      constexpr int b = decltype(B)::value;
+      uint32_t x0, x1, x2, x3;          // values 2b, 2b + 1 of the four tokens
+      if constexpr (NG == 4) {
+        x0 = widen2<b>(vw[0], s0); x1 = widen2<b>(vw[1], s1); x2 = widen2<b>(vw[2], s2); x3 = widen2<b>(vw[3], s3);
+      } else {
+        x0 = widen2<b>(vw[0], s0); x1 = widen2<b + 2>(vw[0], s1); x2 = widen2<b>(vw[1], s2); x3 = widen2<b + 2>(vw[1], s3);
       }
-      if (does_v) {
-        // (quads 1 and 2 of every four change places: the eight tokens of a lane's operand are then 16 bytes side by side)
-        const int quad = i >> 4, place = (quad & 12) | ((quad & 1) << 1) | ((quad >> 1) & 1);
-        unsigned char* to = v_lds + (i & 15) * VSTR + place * 8;
-        const uint32_t s0 = scale_of<0>(vsc[u]), s1 = scale_of<1>(vsc[u]), s2 = scale_of<2>(vsc[u]), s3 = scale_of<3>(vsc[u]);
-        auto column = [&](auto B) {
-          constexpr int b = decltype(B)::value;
-          uint32_t x0, x1, x2, x3;          // values 2b, 2b + 1 of the four tokens
-          if constexpr (NG == 4) {
-            x0 = widen2<b>(vw[u][0], s0); x1 = widen2<b>(vw[u][1], s1); x2 = widen2<b>(vw[u][2], s2); x3 = widen2<b>(vw[u][3], s3);
-          } else {
-            x0 = widen2<b>(vw[u][0], s0); x1 = widen2<b + 2>(vw[u][0], s1); x2 = widen2<b>(vw[u][1], s2); x3 = widen2<b + 2>(vw[u][1], s3);
-          }
-          *reinterpret_cast<au32x2*>(to + 2 * b * 16 * VSTR) = au32x2{__builtin_amdgcn_perm(x1, x0, 0x05040100u), __builtin_amdgcn_perm(x3, x2, 0x05040100u)};
-          *reinterpret_cast<au32x2*>(to + (2 * b + 1) * 16 * VSTR) = au32x2{__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u)};
-        };
-        column(std::integral_constant<int, 0>());
-        column(std::integral_constant<int, 1>());
-        if constexpr (NG == 4) {
-          column(std::integral_constant<int, 2>());
-          column(std::integral_constant<int, 3>());
-        }
-      }
+      *reinterpret_cast<au32x2*>(v_to + 2 * b * 16 * VSTR) = au32x2{__builtin_amdgcn_perm(x1, x0, 0x05040100u), __builtin_amdgcn_perm(x3, x2, 0x05040100u)};
+      *reinterpret_cast<au32x2*>(v_to + (2 * b + 1) * 16 * VSTR) = au32x2{__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u)};
+    };
+    column(std::integral_constant<int, 0>());
+    column(std::integral_constant<int, 1>());
+    if constexpr (NG == 4) {
+      column(std::integral_constant<int, 2>());
+      column(std::integral_constant<int, 3>());
     }
   };
 
@@ -644,19 +625,19 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
   if (t.shares > 1 && lhi == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m == -INFINITY ? m : shift, sum);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const int j = 8 * (e >> 2) + 4 * lhi + (e & 3);
+    const int word = 8 * (e >> 2) + 4 * lhi + (e & 3);
     float x[2 * NG];
 #pragma unroll
     for (int d = 0; d < 2 * NG; ++d) x[d] = o[d >> 1][8 * (d & 1) + e];
     if (t.shares > 1) {
-      af32x4* to = reinterpret_cast<af32x4*>(a.part_o + at * D + j * (2 * NG));
+      af32x4* to = reinterpret_cast<af32x4*>(a.part_o + at * D + word * (2 * NG));
 #pragma unroll
       for (int d = 0; d < 2 * NG; d += 4) to[d / 4] = af32x4{x[d], x[d + 1], x[d + 2], x[d + 3]};
     } else {
       words w;
 #pragma unroll
       for (int d = 0; d < NG; ++d) w[d] = pack2_k(x[2 * d] * inv, x[2 * d + 1] * inv);
-      *reinterpret_cast<words*>(a.out + (t.seq.q0 + query) * a.out_row + head * D + j * (2 * NG)) = w;
+      *reinterpret_cast<words*>(a.out + (t.seq.q0 + query) * a.out_row + head * D + word * (2 * NG)) = w;
     }
   }
 }
@@ -735,22 +716,30 @@ __global__ __launch_bounds__(256) void join_shares_kernel(CacheAttnArgs a) {
 
 size_t plan_cache_attention(CacheAttnArgs& a) {
   const int64_t rows = (int64_t)a.max_queries * a.group, tiles = (a.max_keys + 31) / 32;
-  // rows of a workgroup, and workgroups that are on the chip at once (registers and LDS)
-  a.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-  a.target = a.rows == 16 || a.rows == 64 ? 1024 : a.rows == 256 ? 256 : 512;
-  // up to 1024 keys a workgroup takes them all, and there is nothing to join
-  a.least = a.rows <= 32 && tiles <= 32 ? 32 : 8;
+  // Rows of a workgroup.  Widening the cache costs 32 rows as much as 16, and it is shared by 128: against that, blocks of 128 leave
+  // most of the chip idle until there are about 1.2 10^8 products of a row and a key, and waste what a sequence's last block lacks.
+  // 16 against 32, a token each: one sequence of 2048 keys 9.9 and 10.6 us, 64 of 160 .. 16384 36.4 and 49.4; 40 and 64 rows a unit
+  // go either way by a tenth.  32 against 128: 64 rows a unit, 32 sequences of 8192 keys 69 and 92 us, 40 rows 42 and 48; prompts of 500, 1000 and 2000 tokens, 28 heads (7 .. 112 million) 12.4 and 23, 26 and 37, 69 and 73;
+  // 512 tokens behind 8192 (125 million) 113 and 93, four prompts of 1000 (128 million) 94 and 76, the largest chunk 599 and 489.
+  const double work = (double)a.n_queries * (a.group * a.shape.n_kv_heads) * (double)a.max_keys;
+  a.rows = rows <= 16 ? 16 : rows <= 64 || work < 1.2e8 ? 32 : 128;
+  a.target = a.rows == 16 ? 1024 : 512;         // workgroups that are on the chip at once (registers)
   a.row_blocks = (int32_t)((rows + a.rows - 1) / a.rows);
-  const int64_t units = (int64_t)a.n_seqs * a.shape.n_kv_heads * a.row_blocks, most = std::max<int64_t>(1, (tiles + a.least - 1) / a.least);
+  const int64_t row_units = (int64_t)a.n_seqs * a.shape.n_kv_heads * a.row_blocks;
+  // Tiles of a share, at least.  Up to 1024 keys one workgroup takes them all and there is nothing to join (32 sequences of 500 keys 13.9 ->
+  // 9.7 us, one of 1000 the same); a few short rows are shared out finer (one token of 2048 keys 10.4 -> 9.8, of 4096 10.8 -> 10.4).
+  a.least = a.rows == 128 ? 8 : tiles <= 32 ? 32 : row_units * ((tiles + 3) / 4) <= 256 ? 4 : 8;
+  a.row_blocks = (int32_t)((rows + a.rows - 1) / a.rows);
+  const int64_t most = std::max<int64_t>(1, (tiles + a.least - 1) / a.least);
   // (see find_share: a share is at least `least` tiles, and more than the work over `target`)
-  const int64_t blocks = most > (1 << 20) ? units + a.target + 64 : std::min(units * most, units + a.target + 64);
+  const int64_t blocks = most > (1 << 20) ? row_units + a.target + 64 : std::min(row_units * most, row_units + a.target + 64);
   a.blocks = blocks > 0x7fffffff ? 0 : (int32_t)blocks;
   a.join = most == 1 ? 0 : 1;
   if (!a.join || !a.blocks) return 0;
   // a row's parts at a time: up to sixteen, while that is not more than 512 workgroups (64 ragged sequences 40.3 -> 38.3 us against
   // 2048, 128 rows of each of eight units 42.1 -> 40.2)
   const int64_t of_block = std::min<int64_t>(rows, a.rows);
-  while (a.join < 16 && a.join < most && units * of_block * a.join * 2 <= 8192) a.join *= 2;
+  while (a.join < 16 && a.join < most && row_units * of_block * a.join * 2 <= 8192) a.join *= 2;
   a.join_groups = (int32_t)((of_block * a.join + 15) / 16);
   return (size_t)a.blocks * (size_t)a.rows * (size_t)(a.shape.head_dim + 2) * 4 + (size_t)a.n_seqs * 16;
 }
@@ -760,9 +749,7 @@ static void launch_attend(const CacheAttnArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)a.blocks);
   if (a.rows == 16) hipLaunchKernelGGL((attend_rows_kernel<NG, 1>), grid, dim3(256), 0, stream, a);
   else if (a.rows == 32) hipLaunchKernelGGL((attend_rows_kernel<NG, 2>), grid, dim3(256), 0, stream, a);
-  else if (a.rows == 64) hipLaunchKernelGGL((attend_block_kernel<NG, 2>), grid, dim3(128), 0, stream, a);
-  else if (a.rows == 128) hipLaunchKernelGGL((attend_block_kernel<NG, 4>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((attend_block_kernel<NG, 8>), grid, dim3(512), 0, stream, a);
+  else hipLaunchKernelGGL((attend_block_kernel<NG>), grid, dim3(256), 0, stream, a);
 }
 
 cs_status launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream) {

@@ -268,3 +268,136 @@ def test_nothing_to_do():
     b.run(max_keys=0, out=out)                                                         # told that there are no keys
     assert not out.any()
     assert b.run(q=b.q[:0], cu_queries=torch.zeros(2, dtype=torch.int32, device=DEV)).shape == (0, 4, 64)
+
+
+# ---- many rows.  The kernel for blocks of 128 rows is taken when a sequence may have more than 64 of them and all rows times the
+# keys they may see are many: bounds that are loose take it for short lengths too.
+MANY = dict(max_queries=200, max_keys=1 << 26)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(28, 4, 128), (8, 2, 64), (7, 1, 128), (4, 4, 128), (4, 4, 64), (32, 1, 128)])
+@pytest.mark.parametrize("page", [32, 96])
+@pytest.mark.parametrize("lens", [[(150, 150)], [(1, 1), (2, 0), (5, 33), (0, 7), (0, 0), (33, 300), (129, 130), (64, 64), (70, 31)],
+                                  [(200, 95), (3, 65), (1, 257)], [(1, 5000), (17, 3001), (90, 96)]])
+def test_blocks_of_many_rows(lens, heads, kv_heads, dim, page):
+    b = Batch(lens, heads, kv_heads, dim, page)
+    flag = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for causal in (True, False):
+        got = b.run(causal=causal, err_flag=flag, **MANY)
+        b.check(got, causal)
+        assert torch.equal(got, b.run(causal=causal, **MANY))
+    assert flag.item() == 0
+    at = 0
+    got = b.run(**MANY)
+    for q, n in lens:
+        assert not got[at:at + max(0, q - n)].any()
+        at += q
+
+
+def test_few_and_many_rows_on_either_side_of_the_rule():
+    # 70 rows a sequence; products of rows and keys just below and above 1.2e8, and one row block more or less than 64 rows
+    b = Batch([(35, 400), (9, 77)], 4, 2, 128, 64, seed=14)
+    per_key = 44 * 4
+    for most in (400, int(1.2e8) // per_key - 1, int(1.2e8) // per_key + 2, 1 << 30):
+        for queries in (35, 32, 33):
+            if queries >= 35:
+                b.check(b.run(max_keys=most, max_queries=queries))
+            else:
+                flag = torch.zeros(1, dtype=torch.int32, device=DEV)
+                got = b.run(max_keys=most, max_queries=queries, err_flag=flag)
+                assert flag.item() == 1 and torch.isfinite(got[35:].float()).all()
+
+
+def test_blocks_loud_scores_and_a_maximum_that_moves():
+    b = Batch([(2, 500), (1, 64), (20, 333)], 8, 2, 128, 64, seed=5, loud=True)
+    for scale in (0.02, 0.0, -0.02):
+        b.check(b.run(scale=scale, **MANY), scale=scale)
+    for sign in (1, -1):
+        b = Batch([(150, 640)], 2, 1, 64, 32, seed=15)
+        r = np.round(np.where(sign > 0, np.arange(640), 640 - np.arange(640)) / 20.0)
+        k = np.zeros((640, 1, 64))
+        k[:, 0] = np.exp2(np.floor(np.log2(r + 1)))[:, None]
+        v = np.random.default_rng(1).standard_normal((640, 1, 64))
+        kd, vd = (torch.from_numpy(x).to(torch.bfloat16).to(DEV) for x in (k, v))
+        B.cs_cache_write(b.dpool, kd, vd, torch.from_numpy(b.slots).to(DEV), 32)
+        b.k, b.v = ([O.held(x.double().cpu().numpy())] for x in (kd, vd))
+        b.q = torch.ones_like(b.q)
+        b.check(b.run(scale=0.25, **MANY), scale=0.25)
+
+
+def test_blocks_what_lies_behind_the_last_key_does_not_matter():
+    for n in (45, 64, 99):
+        b = Batch([(1, n), (40, 99)], 4, 2, 128, 64, seed=16)
+        a = b.run(**MANY)
+        b.check(a)
+        for fill in (0x00, 0xff, 0x7f):
+            free = torch.ones(b.dpool.shape[0] * 64, dtype=torch.bool, device=DEV)
+            free[torch.from_numpy(b.slots).to(DEV)] = False
+            pool = b.dpool.cpu().numpy().copy()
+            for slot in np.flatnonzero(free.cpu().numpy()):
+                p, o = divmod(int(slot), 64)
+                for h in range(2):
+                    for at in O.code_addresses(o, 64, 128):
+                        pool[p, h * 64 * 136 + at] = fill
+            assert torch.equal(a, b.run(pool=torch.from_numpy(pool).to(DEV), **MANY)), (n, fill)
+
+
+def test_blocks_pages_that_cannot_be():
+    b = Batch([(1, 100), (2, 64), (1, 40)], 4, 2, 64, 32, seed=10, spare_width=0)
+    flag = torch.zeros(1, dtype=torch.int32, device=DEV)
+    table = b.dtable.clone()
+    table[1, 1], table[0, 0] = b.dpool.shape[0], -7
+    got = b.run(page_table=table, err_flag=flag, causal=False, **MANY)
+    assert flag.item() == 1
+    k, v = ([x[0][32:100], x[1][:32], x[2]] for x in (b.k, b.v))
+    want, weight = O.attention(b.q.double().cpu().numpy(), k, v, [1, 2, 1], 64 ** -0.5, causal=False)
+    assert (np.abs(got.double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -9) * weight).all()
+    # a sequence told to have more keys than its pages hold, and lists of queries that cannot be
+    flag.zero_()
+    got = b.run(n_keys=torch.tensor([100, 64, 1 << 30], dtype=torch.int32, device=DEV), err_flag=flag, **MANY)
+    assert flag.item() == 1
+    b.check(got[:3], lens=[(1, 100), (2, 64)], q=b.q[:3])
+    for cu in ([0, 1, 3, 1 << 30], [0, 1, 0, 4], [-3, 1, 3, 4]):
+        flag.zero_()
+        b.run(cu_queries=torch.tensor(cu, dtype=torch.int32, device=DEV), err_flag=flag, **MANY)
+        assert flag.item() == 1, cu
+
+
+def test_blocks_a_query_of_nan_stays_one_and_its_own():
+    for lens in ([(70, 1500), (3, 50)], [(2, 6000), (3, 50)]):
+        b = Batch(lens, 4, 2, 64, 32, seed=17)
+        clean = b.run(**MANY)
+        q = b.q.clone()
+        q[1, 2, 7] = float("nan")
+        got = b.run(q=q, **MANY)
+        assert got[1, 2].isnan().all()
+        got[1, 2] = clean[1, 2]
+        assert torch.equal(got, clean)
+
+
+def test_blocks_apart_on_another_stream_and_in_a_graph():
+    b = Batch([(40, 3000), (1, 10), (3, 0)], 8, 2, 128, 32, seed=18)
+    eager = b.run(**MANY)
+    b.check(eager)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    other = b.run(stream=side, **MANY)
+    side.synchronize()
+    assert torch.equal(eager, other)
+    wide = torch.full((44, 12, 128), 9.0, dtype=torch.bfloat16, device=DEV)
+    q = torch.zeros(44, 10, 128, dtype=torch.bfloat16, device=DEV)
+    q[:, 1:9] = b.q
+    out, ws = wide[:, 2:10], torch.empty(1 << 26, dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.run(q=q[:, 1:9], out=out, workspace=ws, **MANY)
+    for lens in ([3000, 10, 0], [1, 0, 31], [2048, 33, 64], [3000, 10, 0]):
+        b.n_keys.copy_(torch.tensor(lens, dtype=torch.int32))
+        b.dtable[2, :2] = b.dtable[0, :2]
+        b.dtable[1, :2] = b.dtable[0, 2:4]
+        ws.fill_(0xff)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, b.run(**MANY)), lens
+    assert (wide[:, :2] == 9).all() and (wide[:, 10:] == 9).all()
