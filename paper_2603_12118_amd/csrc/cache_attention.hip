@@ -719,8 +719,9 @@ size_t plan_cache_attention(CacheAttnArgs& a) {
   // Rows of a workgroup.  Widening the cache costs 32 rows as much as 16, and it is shared by 128: against that, blocks of 128 leave
   // most of the chip idle until there are about 1.2 10^8 products of a row and a key, and waste what a sequence's last block lacks.
   // 16 against 32, a token each: one sequence of 2048 keys 9.9 and 10.6 us, 64 of 160 .. 16384 36.4 and 49.4; 40 and 64 rows a unit
-  // go either way by a tenth.  32 against 128: 64 rows a unit, 32 sequences of 8192 keys 69 and 92 us, 40 rows 42 and 48; prompts of 500, 1000 and 2000 tokens, 28 heads (7 .. 112 million) 12.4 and 23, 26 and 37, 69 and 73;
-  // 512 tokens behind 8192 (125 million) 113 and 93, four prompts of 1000 (128 million) 94 and 76, the largest chunk 599 and 489.
+  // go either way by a tenth.  32 against 128: 64 rows a unit, 32 sequences of 8192 keys 69 and 92 us, 40 rows 42 and 48; prompts of
+  // 500, 1000 and 2000 tokens, 28 heads (7 .. 112 million) 12.4 and 23, 26 and 37, 69 and 73; 512 tokens behind 8192 (125 million)
+  // 113 and 93, four prompts of 1000 (128 million) 94 and 76, the largest chunk 599 and 489.
   const double work = (double)a.n_queries * (a.group * a.shape.n_kv_heads) * (double)a.max_keys;
   a.rows = rows <= 16 ? 16 : rows <= 64 || work < 1.2e8 ? 32 : 128;
   a.target = a.rows == 16 ? 1024 : 512;         // workgroups that are on the chip at once (registers)
@@ -729,7 +730,6 @@ size_t plan_cache_attention(CacheAttnArgs& a) {
   // Tiles of a share, at least.  Up to 1024 keys one workgroup takes them all and there is nothing to join (32 sequences of 500 keys 13.9 ->
   // 9.7 us, one of 1000 the same); a few short rows are shared out finer (one token of 2048 keys 10.4 -> 9.8, of 4096 10.8 -> 10.4).
   a.least = a.rows == 128 ? 8 : tiles <= 32 ? 32 : row_units * ((tiles + 3) / 4) <= 256 ? 4 : 8;
-  a.row_blocks = (int32_t)((rows + a.rows - 1) / a.rows);
   const int64_t most = std::max<int64_t>(1, (tiles + a.least - 1) / a.least);
   // (see find_share: a share is at least `least` tiles, and more than the work over `target`)
   const int64_t blocks = most > (1 << 20) ? row_units + a.target + 64 : std::min(row_units * most, row_units + a.target + 64);

@@ -1,0 +1,140 @@
+"""The attention calls of the LLM task run together (paper_2603_12118_amd/consumer_layer.py), each stage against the fp64 checker.
+
+Tolerances.  QKV rows are rounded to bf16, 2^-8 of each value; the norm's root follows its values, so a normed value is off by at most
+2 * 2^-8 of itself, a rotated one by that of |a| + |b|, and the result is rounded once more: 2^-6 of |a| + |b| covers them.  The fp32
+sums of the projection (K = 128 products of order 1/8) add less than 2^-9.  What a slot holds is exact; attention: as in
+test_gpu_cache_attention.py.  The output projection: 2^-8 of the result and K 2^-24 of the sum of |products|, below 2^-12 of it."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as O
+from paper_2603_12118_amd import binding as B
+from paper_2603_12118_amd import consumer_layer as L
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def small(sequences=3, **kw):
+    return L.ConsumerLayer(hidden=128, n_heads=4, n_kv_heads=2, head_dim=64, sections=(8, 12, 12), max_position=512, n_pages=24,
+                           page_tokens=32, sequences=sequences, max_keys=256, **kw)
+
+
+def rows(n, seed):
+    return torch.randn(n, 128, generator=torch.Generator(DEV).manual_seed(seed), device=DEV, dtype=torch.bfloat16)
+
+
+def d64(t):
+    return t.double().cpu().numpy()
+
+
+def check(layer, x, positions, which, lens, out, q, a):
+    """One call's results; lens: new tokens of each sequence."""
+    h, kv, d = layer.n_heads, layer.n_kv_heads, layer.head_dim
+    qkv = (d64(x) @ d64(layer.w_qkv).T + d64(layer.b_qkv)).reshape(-1, h + 2 * kv, d)
+    half = d // 2
+    for got, raw, gain in ((d64(q), qkv[:, :h], layer.q_gain), (d64(layer.last_k), qkv[:, h:h + kv], layer.k_gain)):
+        args = (d64(positions).astype(int), layer.sections, d64(gain), 1e-6)
+        want = O.norm_rope(raw, d64(layer.cos_sin), *args)
+        y = np.abs(O.norm_rope(raw, np.broadcast_to([1.0, 0.0], layer.cos_sin.shape), *args))
+        size = np.tile(y[..., :half] + y[..., half:], 2)
+        assert (np.abs(got - want) <= 2.0 ** -6 * size + 2.0 ** -9).all()
+    at, ks, vs = 0, [], []
+    for b, n in zip(which, lens):
+        total = layer.pages.lens[b]
+        slots = layer.pages.slots(b, 0, total)
+        k, v = O.read(layer.pool.cpu().numpy(), slots, kv, d, layer.pages.page_tokens)
+        assert np.array_equal(k[total - n:], O.held(d64(layer.last_k[at:at + n])))
+        assert np.array_equal(v[total - n:], O.held(d64(layer.last_v[at:at + n])))
+        ks.append(k)
+        vs.append(v)
+        at += n
+    want, weight = O.attention(d64(q), ks, vs, lens, d ** -0.5)
+    assert (np.abs(d64(a) - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -9) * weight + 2.0 ** -126).all()
+    w, flat = d64(layer.w_out), d64(a).reshape(len(want), -1)
+    want = flat @ w.T
+    assert (np.abs(d64(out) - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -12 * (np.abs(flat) @ np.abs(w).T)).all()
+
+
+@pytest.fixture
+def spied(monkeypatch):
+    """Layers whose last written keys and values can be looked at."""
+    def forward(self, *args, _f=L.ConsumerLayer.forward):
+        write = B.cs_cache_write
+
+        def spy(pool, k, v, *rest, **kw):
+            self.last_k, self.last_v = k, v
+            return write(pool, k, v, *rest, **kw)
+        monkeypatch.setattr(L.B, "cs_cache_write", spy)
+        try:
+            return _f(self, *args)
+        finally:
+            monkeypatch.setattr(L.B, "cs_cache_write", write)
+    monkeypatch.setattr(L.ConsumerLayer, "forward", forward)
+
+
+def test_positions_of_text_and_items():
+    p, following = L.prompt_positions([2, (1, 2, 3), 1])
+    assert p.tolist() == [[0, 0, 0], [1, 1, 1], [2, 2, 2], [2, 2, 3], [2, 2, 4], [2, 3, 2], [2, 3, 3], [2, 3, 4], [5, 5, 5]] and following == 6
+
+
+def test_prompts_in_chunks_and_tokens(spied):
+    layer = small()
+    pos, following = L.prompt_positions([5, (1, 6, 7), 40, (3, 2, 2), 1])
+    pos = torch.as_tensor(pos, device=DEV)
+    x = [rows(len(pos), s) for s in range(3)]
+    # placed embeddings: an item's rows in the middle of the text
+    place = torch.arange(5, 47, device=DEV)
+    B.cs_forward_embeddings(rows(42, 9), place, x[1])
+    done = [0, 0, 0]
+    for chunks in ([17, 1, 60], [33, 50, 1], [1, 2, 3]):
+        which = [b for b in range(3)]
+        part = [x[b][done[b]:done[b] + c] for b, c in enumerate(chunks)]
+        part_pos = [pos[done[b]:done[b] + c] for b, c in enumerate(chunks)]
+        got = layer.prefill(which, part, part_pos)
+        check(layer, torch.cat(part), torch.cat(part_pos), which, chunks, *got)
+        done = [d + c for d, c in zip(done, chunks)]
+    got = layer.prefill([2, 0], [rows(1, 11), rows(2, 12)], [pos[64:65], pos[51:53]])
+    check(layer, torch.cat([rows(1, 11), rows(2, 12)]), torch.cat([pos[64:65], pos[51:53]]), [2, 0], [1, 2], *got)
+    assert layer.err.item() == 0
+    held = len(layer.pages.free)
+    layer.pages.release(1)
+    assert len(layer.pages.free) == held + 2 and layer.pages.lens[1] == 0
+    with pytest.raises(RuntimeError, match="no room"):
+        layer.prefill([1], [rows(257, 1)], [torch.zeros(257, 3, dtype=torch.int32, device=DEV)])
+
+
+def test_recorded_steps_are_the_calls():
+    recorded, eager = small(), small()
+    pos, following = L.prompt_positions([3, (1, 5, 5), 2])
+    for layer in (recorded, eager):
+        layer.prefill([0, 1, 2], [rows(30, 1), rows(21, 2), rows(1, 3)],
+                      [torch.as_tensor(pos[:n], device=DEV) for n in (30, 21, 1)])
+    step = L.DecodeStep(recorded, [following, 9, 1])
+    assert torch.equal(recorded.pool, eager.pool)          # recording ran nothing that stays
+    for i in range(40):                                    # pages begin under way
+        x = rows(3, 100 + i)
+        step.x.copy_(x)
+        got = step.run().clone()
+        at = torch.tensor([following + i, 9 + i, 1 + i], dtype=torch.int32, device=DEV)[:, None].repeat(1, 3)
+        lens = list(eager.pages.lens)
+        slots = []
+        for b in range(3):
+            eager.pages.reserve(b, lens[b] + 1)
+            slots.append(eager.pages.slots(b, lens[b], 1))
+            eager.pages.lens[b] += 1
+        want, _, _ = eager.forward(x, at, torch.as_tensor(np.concatenate(slots), device=DEV), torch.arange(4, dtype=torch.int32, device=DEV),
+                                   torch.tensor(eager.pages.lens, dtype=torch.int32, device=DEV), eager.pages.table, 1, eager.max_keys)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), i
+    assert torch.equal(recorded.pool, eager.pool) and recorded.err.item() == 0
+    for b in range(3):
+        near = L.attention_of_cached(recorded, b, step.q[b:b + 1])
+        assert (step.attended[b:b + 1].float() - near).abs().max().item() < 0.03
+
+
+def test_the_program(capsys, monkeypatch):
+    monkeypatch.setattr("sys.argv", ["consumer_layer", "--sequences", "2", "--steps", "3"])
+    L.main()
+    assert "flag 0" in capsys.readouterr().out
