@@ -49,6 +49,11 @@ double real(PyObject* o) {
   if (v == -1.0 && PyErr_Occurred()) throw Type("");
   return v;
 }
+int32_t truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Type("");
+  return v;
+}
 
 int dtype_code(const at::Tensor& x) {
   if (x.scalar_type() == at::kBFloat16) return CS_BF16;
@@ -151,7 +156,7 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (axes > 3) throw Value("sections: at most three axes");
     if (H > 1 << 20 || K > 1 << 20 || D > 1 << 20 || cs.size(1) > 1 << 20) throw Value("q, k, cos_sin: sizes");
     const int code = dtype_code(q);
-    cs_qk_config c = {sizeof(cs_qk_config), (int32_t)H, (int32_t)K, (int32_t)D, (int32_t)(2 * cs.size(1)), (int32_t)axes, PyObject_IsTrue(a[8]),
+    cs_qk_config c = {sizeof(cs_qk_config), (int32_t)H, (int32_t)K, (int32_t)D, (int32_t)(2 * cs.size(1)), (int32_t)axes, truth(a[8]),
                       {0, 0, 0}, cs.size(0), (float)real(a[7])};
     for (int64_t i = 0; i < axes; ++i) {
       PyObject* item = PySequence_GetItem(a[4], i);
@@ -251,7 +256,7 @@ PyObject* attention_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const at::Tensor out = a[11] == Py_None ? at::empty({T, H, D}, q.options()) : tensor(a[11], "out");
     const auto o = call.given(out, T, H, D, at::kBFloat16, "out");
-    const int st = cs_attention_cache(&c, pool, &b, qr.p, qr.row, o.p, o.row, (int32_t)H, (float)scale, PyObject_IsTrue(a[10]),
+    const int st = cs_attention_cache(&c, pool, &b, qr.p, qr.row, o.p, o.row, (int32_t)H, (float)scale, truth(a[10]),
                                       need ? workspace.data_ptr() : nullptr, need, static_cast<int32_t*>(flag), call.stream());
     if (st != CS_OK) return PyLong_FromLong(st);
     return THPVariable_Wrap(out);
