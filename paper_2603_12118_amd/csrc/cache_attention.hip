@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 4
           if (kv + 8 * p + i >= seen[r]) x[i] = -INFINITY;
       }
       float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      if (__any(top > m[r] + slack || (m[r] == -INFINITY && top > m[r]))) {
+      if (__any(top > m[r] + slack)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float moved = top > m[r] + slack || m[r] == -INFINITY ? fmaxf(top, m[r]) : m[r];
@@ -580,7 +580,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
     for (int jt = 0; jt < 2; ++jt)
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[jt][e]);
-    if (__any(top > m + slack || (m == -INFINITY && top > m))) {
+    if (__any(top > m + slack)) {
       top = fmaxf(top, __shfl_xor(top, 32));
       const float moved = top > m + slack || m == -INFINITY ? fmaxf(top, m) : m;
       const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(shift - moved * a.scale_log2);
