@@ -71,11 +71,12 @@ struct CacheAttnArgs {
   int32_t least;          // tiles of 32 keys that a workgroup takes at least, if there are so many
   int32_t blocks;         // workgroups of the launch: those without work end at once
   int32_t join;           // 0: no sequence can be shared out; else the threads, in sixteens, that share a row's parts
+  int32_t planned;        // the shares are worked out by a launch before
   int32_t join_groups;    // workgroups of the joining launch for a block of rows
   // parts, where a sequence's keys are shared out: [blocks, rows, head_dim] sums not yet normalised, and [blocks, rows, 2]
   // their maximum (log2 domain) and weight
   float *part_o, *part_ml;
-  int32_t* share_of;      // [n_seqs, 4] first workgroup, shares, tiles of a share: left by the first launch for the joining one
+  int32_t* share_of;      // [n_seqs, 4] first workgroup, shares, tiles of a share: left by the first launch, or by one before it, for the joining one
 };
 // Fills the plan's fields from the sizes; bytes of workspace the launch needs.
 size_t plan_cache_attention(CacheAttnArgs& a);

@@ -55,10 +55,13 @@ struct KeyTile {
   au32x2 v_scale;                        // of tokens 8p..8p+7, the group of the lane's V columns
 };
 
-// ---- who does what.  The lengths are on the GPU only, so the workgroups share the work out themselves: every wave reads
-// all lengths, and from them come the tiles a workgroup takes (`chunk`: all work over `target` workgroups), the number of
+// ---- who does what.  The lengths are on the GPU only, so the workgroups share the work out themselves: up to 64 sequences, every wave
+// reads all lengths, and from them come the tiles a workgroup takes (`chunk`: all work over `target` workgroups), the number of
 // shares of each sequence's keys, and the sequence a workgroup belongs to.  A batch of long and short sequences then fills
-// the chip as evenly as one of equal ones (64 sequences of 160 .. 16384 keys, shares by the longest: 62 us).
+// the chip as evenly as one of equal ones (64 sequences of 160 .. 16384 keys: 29 us, with shares by the longest 62).  More sequences are
+// shared out by a launch of one workgroup before, which is 2 us slower than reading all lengths in every wave for 128 sequences of 2000 keys
+// (35 us), and 512 ragged ones of up to 4000 take 67 us instead of 79.  Where no sequence can be shared out, a workgroup is a block of
+// rows and reads the lengths of its own: 1024 sequences of 500 keys 58 us instead of 110, one 7.1 instead of 7.4.
 struct Sequence {
   int q0, nq, keys, units, tiles;   // units: blocks of rows of all key/value heads
   bool cut;                         // a length on the GPU is not what the host was told
@@ -84,53 +87,115 @@ struct Share {
   Sequence seq;
   int b, chunk, shares, first;   // first: the sequence's first workgroup
 };
+// tiles a workgroup takes (more than work / target, so that the workgroups are fewer than target and one a unit)
+__device__ __forceinline__ int chunk_of(const CacheAttnArgs& a, float work) {
+  const float per = work / (float)a.target;
+  const int chunk = per > 3e7f ? 1 << 25 : (int)per + 1;
+  return chunk < a.least ? a.least : (chunk + 1) & ~1;
+}
+__device__ __forceinline__ int shares_of(const Sequence& t, int chunk) { return t.tiles > chunk ? (t.tiles + chunk - 1) / chunk : 1; }
+
 // The share of workgroup `id`; false where there is none.  Whole waves.
 __device__ __forceinline__ bool find_share(const CacheAttnArgs& a, int rows, int id, Share& s) {
   const int lane = threadIdx.x & 63, n = a.n_seqs;
-  const Sequence mine = sequence(a, lane, rows);
-  float work = (float)mine.units * (float)mine.tiles;
-  bool cut = mine.cut;
-  for (int b = 64 + lane; b < n; b += 64) {
-    const Sequence t = sequence(a, b, rows);
-    work += (float)t.units * (float)t.tiles;
-    cut |= t.cut;
-  }
-  if (id == 0 && cut && a.err) atomicOr(a.err, 1);
-  for (int m = 1; m < 64 && m < n; m <<= 1) work += __shfl_xor(work, m);
-  work = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(work)));
-  // (more than work / target, so that the workgroups are fewer than target and one a unit)
-  const float per = work / (float)a.target;
-  int chunk = per > 3e7f ? 1 << 25 : (int)per + 1;
-  chunk = chunk < a.least ? a.least : (chunk + 1) & ~1;
-  int before = 0;
-  for (int b0 = 0; b0 < n; b0 += 64) {
-    const Sequence t = b0 ? sequence(a, b0 + lane, rows) : mine;
-    const int shares = t.tiles > chunk ? (t.tiles + chunk - 1) / chunk : 1;
-    int upto = t.units * shares;
-    const int own = upto;
-    for (int m = 1; m < 64 && m < n; m <<= 1) {
+  bool found;
+  if (!a.join || a.planned) {
+    if (!a.join) {
+      const int per = a.shape.n_kv_heads * a.row_blocks;
+      s.b = id / per;
+      s.first = s.b * per;
+      s.shares = 1;
+      s.chunk = 1 << 25;
+    } else {                             // the last sequence whose first workgroup is not behind `id`, by steps of 64
+      int step = 1;
+      while ((int64_t)step * 64 < n) step *= 64;
+      s.b = 0;
+      for (; step; step >>= 6) {
+        const int64_t at = s.b + (int64_t)lane * step;
+        const uint64_t upto = __ballot(at < n && a.share_of[4 * at] <= id);
+        s.b += (__builtin_popcountll(upto) - 1) * step;
+      }
+      const int4 share = *reinterpret_cast<const int4*>(a.share_of + 4 * (int64_t)s.b);
+      s.first = share.x;
+      s.shares = share.y;
+      s.chunk = share.z;
+    }
+    s.seq = sequence(a, s.b, rows);
+    found = id - s.first < s.seq.units * s.shares;
+    if (!a.join && s.seq.cut && id == s.first && a.err && threadIdx.x == 0) atomicOr(a.err, 1);
+  } else {
+    const Sequence t = sequence(a, lane, rows);
+    float work = (float)t.units * (float)t.tiles;
+    const uint64_t cut = __ballot(t.cut);
+    if (id == 0 && cut && a.err && threadIdx.x == 0) atomicOr(a.err, 1);
+    for (int m = 1; m < n; m <<= 1) work += __shfl_xor(work, m);
+    s.chunk = chunk_of(a, __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(work))));
+    const int shares = shares_of(t, s.chunk), own = t.units * shares;
+    int upto = own;
+    for (int m = 1; m < n; m <<= 1) {
       const int x = __shfl_up(upto, m);
       upto += lane >= m ? x : 0;
     }
-    const uint64_t hit = __ballot(before + upto > id);
-    if (hit) {
-      const int f = __builtin_ctzll(hit);
-      s.b = b0 + f;
-      s.chunk = chunk;
-      s.shares = __builtin_amdgcn_readlane(shares, f);
-      s.first = before + __builtin_amdgcn_readlane(upto - own, f);
-      s.seq.q0 = __builtin_amdgcn_readlane(t.q0, f);
-      s.seq.nq = __builtin_amdgcn_readlane(t.nq, f);
-      s.seq.keys = __builtin_amdgcn_readlane(t.keys, f);
-      s.seq.units = __builtin_amdgcn_readlane(t.units, f);
-      s.seq.tiles = __builtin_amdgcn_readlane(t.tiles, f);
-      return true;
-    }
-    const int last = n - b0 < 64 ? n - b0 - 1 : 63;
-    before += __builtin_amdgcn_readlane(upto, last);
+    const uint64_t hit = __ballot(lane < n && upto > id);
+    found = hit != 0;
+    s.b = found ? __builtin_ctzll(hit) : 0;
+    s.shares = __builtin_amdgcn_readlane(shares, s.b);
+    s.first = __builtin_amdgcn_readlane(upto - own, s.b);
+    s.seq.q0 = __builtin_amdgcn_readlane(t.q0, s.b);
+    s.seq.nq = __builtin_amdgcn_readlane(t.nq, s.b);
+    s.seq.keys = __builtin_amdgcn_readlane(t.keys, s.b);
+    s.seq.units = __builtin_amdgcn_readlane(t.units, s.b);
+    s.seq.tiles = __builtin_amdgcn_readlane(t.tiles, s.b);
+    if (found && id == s.first && threadIdx.x == 0) *reinterpret_cast<int4*>(a.share_of + 4 * s.b) = make_int4(s.first, s.shares, s.chunk, 0);
   }
-  return false;
+  // (the same in every lane: into scalar registers)
+  for (int* x : {&s.b, &s.first, &s.shares, &s.chunk, &s.seq.q0, &s.seq.nq, &s.seq.keys, &s.seq.units, &s.seq.tiles}) *x = __builtin_amdgcn_readfirstlane(*x);
+  return __builtin_amdgcn_readfirstlane(found);
 }
+
+// The shares of more than 64 sequences, 1024 at a time, one workgroup.  Bound by latency (lengths, twice, and the sums between).
+__global__ __launch_bounds__(1024) void share_out_kernel(CacheAttnArgs a) {
+  __shared__ float work_of[16];
+  __shared__ int upto_of[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  float work = 0.f;
+  bool cut = false;
+  for (int64_t b = tid; b < a.n_seqs; b += 1024) {
+    const Sequence t = sequence(a, (int)b, a.rows);
+    work += (float)t.units * (float)t.tiles;
+    cut |= t.cut;
+  }
+  if (cut && a.err) atomicOr(a.err, 1);
+  for (int m = 1; m < 64; m <<= 1) work += __shfl_xor(work, m);
+  if (lane == 0) work_of[wave] = work;
+  __syncthreads();
+  work = 0.f;
+  for (int w = 0; w < 16; ++w) work += work_of[w];
+  const int chunk = chunk_of(a, work);
+  int before = 0;
+  for (int64_t b0 = 0; b0 < a.n_seqs; b0 += 1024) {
+    const int64_t b = b0 + tid;
+    Sequence t = {};
+    if (b < a.n_seqs) t = sequence(a, (int)b, a.rows);
+    const int shares = shares_of(t, chunk), own = t.units * shares;
+    int upto = own;
+    for (int m = 1; m < 64; m <<= 1) {
+      const int x = __shfl_up(upto, m);
+      upto += lane >= m ? x : 0;
+    }
+    if (lane == 63) upto_of[wave] = upto;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) upto += upto_of[w];
+      all += upto_of[w];
+    }
+    if (b < a.n_seqs) *reinterpret_cast<int4*>(a.share_of + 4 * b) = make_int4(before + upto - own, shares, chunk, 0);
+    before += all;
+    __syncthreads();
+  }
+}
+
 // The block of rows that `unit` of a sequence is: the last rows, which see the most keys, first
 struct RowBlock {
   int h, first, rows, seen;   // rows first .. of `rows`; keys its last row sees
@@ -163,7 +228,12 @@ __device__ __forceinline__ void store_row(const CacheAttnArgs& a, int q0, int h,
   *reinterpret_cast<typename Words<NG>::type*>(a.out + (q0 + query) * a.out_row + head * (32 * NG) + jc) = w;
 }
 
-// ---- few rows: 16 RT of them, a wave's keys its own
+// ---- few rows: 16 RT of them, a wave's keys its own.  The softmax keeps a running maximum and sum (fp32) a row and wave, joined at the end.
+// Bound by the memory once there are enough keys: 64 sequences of 8192 (285 MB) 57 us with their join, 5.0 TB/s.  Fewer are bound by the way to
+// a wave's first tile (arguments, lengths, page table, tile: four reads, one behind the other) and by the join: 64 of 160 .. 16384 keys
+// (119 MB) 29 + 5.5 us, one of 131072 (71 MB) 18.5 + 7.4, one of 2048 5.9 + 5.0, six of up to 4097 with 5 queries 12.3 + 4.8.  While a wave
+// works on a tile its next one is on its way: 17.8 MB over the chip, 2.8 us at 6.3 TB/s; two ahead do not fit the registers of four waves a
+// SIMD.  The loop is some 200 vector and 16 matrix instructions a tile; an eighth fewer of the former changed nothing.
 template <int NG, int RT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 4 : 2))) void attend_rows_kernel(CacheAttnArgs a) {
   constexpr int D = 32 * NG, WAVES = 4, PITCH = D + 4, ROWS = 16 * RT;
@@ -176,7 +246,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 4
   if (!find_share(a, ROWS, blockIdx.x, t)) return;           // (whole workgroups, before any barrier)
   const int rank = blockIdx.x - t.first, share = rank / t.seq.units, unit = rank - share * t.seq.units;
   const RowBlock rb = row_block(a, t.seq, unit, ROWS);
-  if (a.join && rank == 0 && tid == 0) *reinterpret_cast<int4*>(a.share_of + 4 * t.b) = make_int4(t.first, t.shares, t.chunk, 0);
 
   // ---- this wave's tiles
   int t0 = share * t.chunk, t1 = (rb.seen + 31) >> 5;
@@ -412,6 +481,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 4
 // workgroup (a thread: a quarter of a token of K, a word of four tokens of V): K as it is, V transposed, so that both products read
 // 16 bytes a lane.  S^T = K Q^T and O^T = V^T P^T with
 // v_mfma_f32_32x32x16_bf16: lane l has row l % 32 throughout, and what the exponential leaves is the second product's operand.
+// Bound by the SIMDs, whose matrix and vector instructions share less than half of their time (two waves of 16 products and 128 FMAs: alternating
+// 797 ns, interleaved 645, products alone 495, FMAs alone 473), and by the power: 2048 queries behind 14336 keys, 28 heads, 451 GFLOP,
+// 473 .. 509 us on different cards, 890 .. 950 TFLOP/s (zeros for data: 450), matrix pipe busy 40 % of the cycles, vector unit 45 %.  Within
+// 3 % of that: 256 rows a workgroup, K widened by every wave into registers without LDS, fragments asked for earlier, exponentials between
+// the products, tiles two ahead.  Three waves a SIMD spill (569 us), 64 rows a wave move accumulators about (592).
 // A column of V^T (value 2 NG j + d of a head, j = the word of a token that holds it) is row 16 d + j of the tile: the 16 lanes
 // that write one d then write neighbouring rows, and a lane's results come out 2 NG values at a time.
 template <int NG>
@@ -427,7 +501,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
   if (!find_share(a, ROWS, blockIdx.x, t)) return;          // (whole workgroups, before any barrier)
   const int rank = blockIdx.x - t.first, share = rank / t.seq.units, unit = rank - share * t.seq.units;
   const RowBlock rb = row_block(a, t.seq, unit, ROWS);
-  if (a.join && rank == 0 && tid == 0) *reinterpret_cast<int4*>(a.share_of + 4 * t.b) = make_int4(t.first, t.shares, t.chunk, 0);
   const int t0 = share * t.chunk, seen_tiles = (rb.seen + 31) >> 5;       // (chunks are even)
   if (share > 0 && t0 >= seen_tiles) return;
   const int t1 = t0 + t.chunk < seen_tiles ? t0 + t.chunk : seen_tiles;
@@ -643,7 +716,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void a
 }
 
 // ---- the shares of a row's keys, joined: 16 lanes a part, `join` parts of a row at a time, in an order that depends on
-// the lengths alone
+// the lengths alone.  Bound by latency (lengths, shares, parts, one behind the other): 4.4 .. 7.4 us, 13 where 57344 rows have two parts each.
+// A launch of its own: a counter to tell the last workgroup of a row would have to be cleared by one.
 template <int NG>
 __global__ __launch_bounds__(256) void join_shares_kernel(CacheAttnArgs a) {
   constexpr int D = 32 * NG;
@@ -653,7 +727,7 @@ __global__ __launch_bounds__(256) void join_shares_kernel(CacheAttnArgs a) {
   const int block = blockIdx.x / a.join_groups, units = a.row_blocks * a.shape.n_kv_heads, b = block / units, unit = block - b * units;
   const Sequence seq = sequence(a, b, a.rows);
   if (unit >= seq.units) return;                             // (whole workgroups, before any barrier)
-  const int4 share = *reinterpret_cast<const int4*>(a.share_of + 4 * b);
+  const int4 share = *reinterpret_cast<const int4*>(a.share_of + 4 * (int64_t)b);
   const int first = share.x, chunk = share.z;
   if (share.y == 1) return;
   const RowBlock rb = row_block(a, seq, unit, a.rows);
@@ -738,6 +812,7 @@ size_t plan_cache_attention(CacheAttnArgs& a) {
   const int64_t blocks = most > (1 << 20) ? row_units + a.target + 64 : std::min(row_units * most, row_units + a.target + 64);
   a.blocks = blocks > 0x7fffffff ? 0 : (int32_t)blocks;
   a.join = most == 1 ? 0 : 1;
+  a.planned = a.join && a.n_seqs > 64;
   if (!a.join || !a.blocks) return 0;
   // a row's parts at a time: up to sixteen, while that is not more than 512 workgroups (64 ragged sequences 40.3 -> 38.3 us against
   // 2048, 128 rows of each of eight units 42.1 -> 40.2)
@@ -758,6 +833,10 @@ static void launch_attend(const CacheAttnArgs& a, hipStream_t stream) {
 cs_status launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream) {
   const int64_t joins = (int64_t)a.n_seqs * a.shape.n_kv_heads * a.row_blocks * a.join_groups;
   if (!a.blocks || joins > 0x7fffffff) return fail(CS_ERR_UNSUPPORTED, "cs_attention_cache: too many rows");
+  if (a.planned) {
+    hipLaunchKernelGGL(share_out_kernel, dim3(1), dim3(1024), 0, stream, a);
+    CS_HIP(hipGetLastError());
+  }
   if (a.shape.head_dim == 128) launch_attend<4>(a, stream);
   else launch_attend<2>(a, stream);
   CS_HIP(hipGetLastError());

@@ -401,3 +401,47 @@ def test_blocks_apart_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, b.run(**MANY)), lens
     assert (wide[:, :2] == 9).all() and (wide[:, 10:] == 9).all()
+
+
+# ---- more sequences than lanes: their shares are worked out by a launch of its own where keys can be shared out (a bound of more than
+# 1024 keys), and are a division where they cannot
+@pytest.mark.parametrize("count", [64, 65, 130, 1025, 4100])
+def test_many_sequences(count):
+    rng = np.random.default_rng(count)
+    lens = [(int(q), int(n)) for q, n in zip(rng.choice([0, 1, 1, 1, 2], count), rng.integers(0, 5 if count > 500 else 60, count))]
+    for at, n in ((0, 0), (count // 2, 2500), (count - 1, 0)):
+        lens[at] = (1 if n else 0, n)
+    lens[7], lens[count - 3] = (1, 1300), (3, 40)
+    b = Batch(lens, 2, 1, 64, 32, seed=count)
+    flag = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = b.run(err_flag=flag)
+    b.check(got)
+    assert torch.equal(got, b.run(err_flag=flag))
+    b.check(b.run(max_keys=100000, err_flag=flag))
+    b.check(b.run(err_flag=flag, max_queries=300, max_keys=1 << 26))         # blocks of many rows
+    assert flag.item() == 0
+    short = [(q, min(n, 1000)) for q, n in lens]
+    got = b.run(max_keys=1000, err_flag=flag)                                 # one launch; two sequences are cut
+    b.check(got, lens=short)
+    assert flag.item() == 1
+    flag.zero_()
+    b.run(max_keys=2400, err_flag=flag)
+    assert flag.item() == 1
+
+
+def test_many_sequences_in_a_graph():
+    lens = [(1, 40 + 3 * i) for i in range(100)]
+    b = Batch(lens, 4, 2, 64, 32, seed=19)
+    out, ws = torch.empty_like(b.q), torch.empty(1 << 26, dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.run(out=out, workspace=ws, max_keys=4000)
+    keys = b.n_keys.clone()
+    for step in range(3):
+        b.n_keys.copy_((keys - 40 * step).clamp(min=0))
+        ws.fill_(0xff)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, b.run(max_keys=4000)), step
+        b.check(out, lens=[(1, max(0, n - 40 * step)) for _, n in lens])
