@@ -64,7 +64,8 @@ struct CacheAttnArgs {
   int32_t causal;
   CacheShape shape;
   int32_t* err;
-  // set by plan_cache_attention
+  // set by the launcher
+  int32_t more_than, at_most;   // rows of the sequences that a launch takes: the others are another's
   int32_t rows;           // rows (a row: a query and a head) a workgroup takes: 16 or 32 (their keys shared out to its waves) or 128
   int32_t row_blocks;     // blocks of so many rows that a sequence and key/value head have at most
   int32_t target;         // workgroups that fill the chip once
@@ -72,14 +73,15 @@ struct CacheAttnArgs {
   int32_t blocks;         // workgroups of the launch: those without work end at once
   int32_t join;           // 0: no sequence can be shared out; else the threads, in sixteens, that share a row's parts
   int32_t planned;        // the shares are worked out by a launch before
+  int64_t units;          // ... units that the joining launch is laid out for
   int32_t join_groups;    // workgroups of the joining launch for a block of rows
   // parts, where a sequence's keys are shared out: [blocks, rows, head_dim] sums not yet normalised, and [blocks, rows, 2]
   // their maximum (log2 domain) and weight
   float *part_o, *part_ml;
-  int32_t* share_of;      // [n_seqs, 4] first workgroup, shares, tiles of a share: left by the first launch, or by one before it, for the joining one
+  int32_t* share_of;      // [n_seqs, 4] first workgroup, shares, tiles of a share, first unit: left by the first launch, or by one before it, for the joining one
 };
-// Fills the plan's fields from the sizes; bytes of workspace the launch needs.
-size_t plan_cache_attention(CacheAttnArgs& a);
-cs_status launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);
+// Bytes of workspace the launches need, from the sizes alone.
+size_t plan_cache_attention(const CacheAttnArgs& a);
+cs_status launch_cache_attention(const CacheAttnArgs& a, void* workspace, hipStream_t s);
 
 }  // namespace cs

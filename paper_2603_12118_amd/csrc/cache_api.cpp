@@ -163,10 +163,7 @@ cs_status attention_cache(const cs_cache_config* c, const void* pool, const cs_c
   a.scale_log2 = std::max(std::fabs(scale) * 1.4426950408889634f, 1e-30f);
   a.q_sign = scale < 0 ? 0x80008000u : 0;
   a.causal = causal; a.err = err_flag;
-  a.part_o = static_cast<float*>(workspace);
-  a.part_ml = a.part_o + (size_t)a.blocks * (size_t)a.rows * (size_t)c->head_dim;
-  a.share_of = reinterpret_cast<int32_t*>(a.part_ml + (size_t)a.blocks * (size_t)a.rows * 2);
-  return launch_cache_attention(a, static_cast<hipStream_t>(stream));
+  return launch_cache_attention(a, workspace, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace
@@ -209,7 +206,7 @@ CS_CATCH_ALL("cs_cache_read")
 cs_status cs_attention_cache_query(const cs_cache_config* config, const cs_cache_batch* batch, int32_t n_heads, size_t* workspace_bytes) try {
   if (!workspace_bytes) return invalid("cs_attention_cache_query", "NULL argument");
   if (cs_status st = check_batch("cs_attention_cache_query", config, batch, n_heads)) return st;
-  CacheAttnArgs a = attention_args(config, batch, n_heads);
+  const CacheAttnArgs a = attention_args(config, batch, n_heads);
   *workspace_bytes = plan_cache_attention(a);
   return CS_OK;
 }

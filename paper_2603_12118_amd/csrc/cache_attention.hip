@@ -79,7 +79,8 @@ __device__ __forceinline__ Sequence sequence(const CacheAttnArgs& a, int b, int 
   t.cut |= t.keys != n;
   t.q0 = (int)q0;
   t.nq = (int)(q1 - q0);
-  t.units = (int)(((int64_t)t.nq * a.group + rows - 1) / rows) * a.shape.n_kv_heads;
+  const int64_t r = (int64_t)t.nq * a.group;
+  t.units = r > a.more_than && r <= a.at_most ? (int)((r + rows - 1) / rows) * a.shape.n_kv_heads : 0;
   t.tiles = (t.keys + 31) >> 5;
   return t;
 }
@@ -95,6 +96,17 @@ __device__ __forceinline__ int chunk_of(const CacheAttnArgs& a, float work) {
 }
 __device__ __forceinline__ int shares_of(const Sequence& t, int chunk) { return t.tiles > chunk ? (t.tiles + chunk - 1) / chunk : 1; }
 
+// The last sequence whose entry of share_of (0: first workgroup, 3: first unit) is not behind `id`, by steps of 64
+__device__ __forceinline__ int find_sequence(const CacheAttnArgs& a, int entry, int id) {
+  int step = 1, b = 0;
+  while ((int64_t)step * 64 < a.n_seqs) step *= 64;
+  for (; step; step >>= 6) {
+    const int64_t at = b + (int64_t)(threadIdx.x & 63) * step;
+    const uint64_t upto = __ballot(at < a.n_seqs && a.share_of[4 * at + entry] <= id);
+    b += (__builtin_popcountll(upto) - 1) * step;
+  }
+  return b;
+}
 // The share of workgroup `id`; false where there is none.  Whole waves.
 __device__ __forceinline__ bool find_share(const CacheAttnArgs& a, int rows, int id, Share& s) {
   const int lane = threadIdx.x & 63, n = a.n_seqs;
@@ -106,15 +118,8 @@ __device__ __forceinline__ bool find_share(const CacheAttnArgs& a, int rows, int
       s.first = s.b * per;
       s.shares = 1;
       s.chunk = 1 << 25;
-    } else {                             // the last sequence whose first workgroup is not behind `id`, by steps of 64
-      int step = 1;
-      while ((int64_t)step * 64 < n) step *= 64;
-      s.b = 0;
-      for (; step; step >>= 6) {
-        const int64_t at = s.b + (int64_t)lane * step;
-        const uint64_t upto = __ballot(at < n && a.share_of[4 * at] <= id);
-        s.b += (__builtin_popcountll(upto) - 1) * step;
-      }
+    } else {
+      s.b = find_sequence(a, 0, id);
       const int4 share = *reinterpret_cast<const int4*>(a.share_of + 4 * (int64_t)s.b);
       s.first = share.x;
       s.shares = share.y;
@@ -153,10 +158,10 @@ __device__ __forceinline__ bool find_share(const CacheAttnArgs& a, int rows, int
   return __builtin_amdgcn_readfirstlane(found);
 }
 
-// The shares of more than 64 sequences, 1024 at a time, one workgroup.  Bound by latency (lengths, twice, and the sums between).
+// The shares of more than 64 sequences, or of few that differ much, 1024 at a time, one workgroup.  Bound by latency (lengths, twice, and the sums between).
 __global__ __launch_bounds__(1024) void share_out_kernel(CacheAttnArgs a) {
   __shared__ float work_of[16];
-  __shared__ int upto_of[16];
+  __shared__ int upto_of[16], units_of[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   float work = 0.f;
   bool cut = false;
@@ -172,26 +177,35 @@ __global__ __launch_bounds__(1024) void share_out_kernel(CacheAttnArgs a) {
   work = 0.f;
   for (int w = 0; w < 16; ++w) work += work_of[w];
   const int chunk = chunk_of(a, work);
-  int before = 0;
+  int before = 0, units_before = 0;
   for (int64_t b0 = 0; b0 < a.n_seqs; b0 += 1024) {
     const int64_t b = b0 + tid;
     Sequence t = {};
     if (b < a.n_seqs) t = sequence(a, (int)b, a.rows);
     const int shares = shares_of(t, chunk), own = t.units * shares;
-    int upto = own;
+    int upto = own, units = t.units;
     for (int m = 1; m < 64; m <<= 1) {
-      const int x = __shfl_up(upto, m);
+      const int x = __shfl_up(upto, m), y = __shfl_up(units, m);
       upto += lane >= m ? x : 0;
+      units += lane >= m ? y : 0;
     }
-    if (lane == 63) upto_of[wave] = upto;
+    if (lane == 63) {
+      upto_of[wave] = upto;
+      units_of[wave] = units;
+    }
     __syncthreads();
-    int all = 0;
+    int all = 0, all_units = 0;
     for (int w = 0; w < 16; ++w) {
-      if (w < wave) upto += upto_of[w];
+      if (w < wave) {
+        upto += upto_of[w];
+        units += units_of[w];
+      }
       all += upto_of[w];
+      all_units += units_of[w];
     }
-    if (b < a.n_seqs) *reinterpret_cast<int4*>(a.share_of + 4 * b) = make_int4(before + upto - own, shares, chunk, 0);
+    if (b < a.n_seqs) *reinterpret_cast<int4*>(a.share_of + 4 * b) = make_int4(before + upto - own, shares, chunk, units_before + units - t.units);
     before += all;
+    units_before += all_units;
     __syncthreads();
   }
 }
@@ -724,12 +738,16 @@ __global__ __launch_bounds__(256) void join_shares_kernel(CacheAttnArgs a) {
   __shared__ __align__(16) float state_o[16][D + 4];
   __shared__ float state_m[16], state_l[16];
   const int per = 16 / a.join;                               // rows of a workgroup
-  const int block = blockIdx.x / a.join_groups, units = a.row_blocks * a.shape.n_kv_heads, b = block / units, unit = block - b * units;
+  const int block = blockIdx.x / a.join_groups, units = a.row_blocks * a.shape.n_kv_heads;
+  const int b = a.planned ? find_sequence(a, 3, block) : block / units;
+  const int4 share = *reinterpret_cast<const int4*>(a.share_of + 4 * (int64_t)b);
+  const int unit = block - (a.planned ? share.w : b * units);
   const Sequence seq = sequence(a, b, a.rows);
   if (unit >= seq.units) return;                             // (whole workgroups, before any barrier)
-  const int4 share = *reinterpret_cast<const int4*>(a.share_of + 4 * (int64_t)b);
   const int first = share.x, chunk = share.z;
   if (share.y == 1) return;
+  // (lists of queries that overlap may have more parts than there is room for: theirs are not looked at)
+  if (first < 0 || chunk < 1 || share.y != shares_of(seq, chunk) || first + (int64_t)seq.units * share.y > a.blocks) return;
   const RowBlock rb = row_block(a, seq, unit, a.rows);
   const int slot = threadIdx.x >> 4, jc = (threadIdx.x & 15) * (2 * NG);
   const int in_block = (blockIdx.x - block * a.join_groups) * per + slot / a.join;
@@ -788,8 +806,9 @@ __global__ __launch_bounds__(256) void join_shares_kernel(CacheAttnArgs a) {
   if (r < rb.rows) store_row<NG>(a, seq.q0, rb.h, r, jc, acc, ll);
 }
 
-size_t plan_cache_attention(CacheAttnArgs& a) {
-  const int64_t rows = (int64_t)a.max_queries * a.group, tiles = (a.max_keys + 31) / 32;
+// The plan of the sequences with more than `more_than` rows and at most `at_most`
+static size_t plan_rows(CacheAttnArgs& a) {
+  const int64_t rows = std::min<int64_t>((int64_t)a.max_queries * a.group, a.at_most), all_rows = a.n_queries * a.group, tiles = (a.max_keys + 31) / 32;
   // Rows of a workgroup.  Widening the cache costs 32 rows as much as 16, and it is shared by 128: against that, blocks of 128 leave
   // most of the chip idle until there are about 1.2 10^8 products of a row and a key, and waste what a sequence's last block lacks.
   // 16 against 32, a token each: one sequence of 2048 keys 9.9 and 10.6 us, 64 of 160 .. 16384 36.4 and 49.4; 40 and 64 rows a unit
@@ -803,23 +822,48 @@ size_t plan_cache_attention(CacheAttnArgs& a) {
   // instead of 19.8, chunks of 1024 behind 7168 212 instead of 187.)
   a.target = a.rows == 32 ? 512 : a.rows == 16 ? (a.shape.head_dim == 128 ? 1024 : 1280) : a.shape.head_dim == 128 ? 512 : 768;
   a.row_blocks = (int32_t)((rows + a.rows - 1) / a.rows);
-  const int64_t row_units = (int64_t)a.n_seqs * a.shape.n_kv_heads * a.row_blocks;
+  // units there may be: a sequence's last block of rows may be smaller than the others
+  const int64_t seqs = std::min<int64_t>(a.n_seqs, all_rows / (a.more_than + 1)), each = (int64_t)a.n_seqs * a.row_blocks;
+  const int64_t bound = std::min(seqs * a.row_blocks, seqs + all_rows / a.rows), row_units = bound * a.shape.n_kv_heads;
   // Tiles of a share, at least.  Up to 1024 keys one workgroup takes them all and there is nothing to join (32 sequences of 500 keys 13.9 ->
   // 9.7 us, one of 1000 the same); a few short rows are shared out finer (one token of 2048 keys 10.4 -> 9.8, of 4096 10.8 -> 10.4).
   a.least = a.rows == 128 ? 8 : tiles <= 32 ? 32 : row_units * ((tiles + 3) / 4) <= 256 ? 4 : 8;
   const int64_t most = std::max<int64_t>(1, (tiles + a.least - 1) / a.least);
   // (see find_share: a share is at least `least` tiles, and more than the work over `target`)
   const int64_t blocks = most > (1 << 20) ? row_units + a.target + 64 : std::min(row_units * most, row_units + a.target + 64);
-  a.blocks = blocks > 0x7fffffff ? 0 : (int32_t)blocks;
   a.join = most == 1 ? 0 : 1;
-  a.planned = a.join && a.n_seqs > 64;
+  // (one launch: a workgroup for every block of rows that a sequence may have)
+  const int64_t grid = a.join ? blocks : each * a.shape.n_kv_heads;
+  a.blocks = grid > 0x7fffffff ? 0 : (int32_t)grid;
   if (!a.join || !a.blocks) return 0;
+  a.planned = a.n_seqs > 64 || each > 2 * bound;
+  a.units = a.planned ? row_units : each * a.shape.n_kv_heads;
   // a row's parts at a time: up to sixteen, while that is not more than 512 workgroups (64 ragged sequences 40.3 -> 38.3 us against
   // 2048, 128 rows of each of eight units 42.1 -> 40.2)
   const int64_t of_block = std::min<int64_t>(rows, a.rows);
   while (a.join < 16 && a.join < most && row_units * of_block * a.join * 2 <= 8192) a.join *= 2;
   a.join_groups = (int32_t)((of_block * a.join + 15) / 16);
   return (size_t)a.blocks * (size_t)a.rows * (size_t)(a.shape.head_dim + 2) * 4 + (size_t)a.n_seqs * 16;
+}
+
+// A batch of prompts and tokens: sequences of few rows and of many have launches of their own, with one workspace in turn.  (The host knows the
+// number of queries and the most that a sequence has: half of n_seqs times that, or less, and the batch is taken for one.)  48 tokens behind 200
+// .. 8000 keys and 512 queries behind 3584: 181 us as blocks of 128 rows, the two apart 98.
+static int plan_parts(const CacheAttnArgs& a, CacheAttnArgs (&parts)[2]) {
+  const int few = a.group <= 16 ? 16 : 32;
+  parts[0] = a;
+  parts[0].more_than = 0;
+  parts[0].at_most = 0x7fffffff;
+  if (a.group > 32 || (int64_t)a.max_queries * a.group <= 64 || a.n_queries * 2 > (int64_t)a.n_seqs * a.max_queries) return 1;
+  parts[1] = parts[0];
+  parts[0].more_than = parts[1].at_most = few;
+  return 2;
+}
+size_t plan_cache_attention(const CacheAttnArgs& a) {
+  CacheAttnArgs parts[2];
+  size_t need = 0;
+  for (int n = plan_parts(a, parts); n--;) need = std::max(need, plan_rows(parts[n]));
+  return need;
 }
 
 template <int NG>
@@ -830,21 +874,32 @@ static void launch_attend(const CacheAttnArgs& a, hipStream_t stream) {
   else hipLaunchKernelGGL((attend_block_kernel<NG>), grid, dim3(256), 0, stream, a);
 }
 
-cs_status launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream) {
-  const int64_t joins = (int64_t)a.n_seqs * a.shape.n_kv_heads * a.row_blocks * a.join_groups;
+static cs_status launch_rows(CacheAttnArgs& a, void* workspace, hipStream_t stream) {
+  plan_rows(a);
+  const int64_t joins = a.join ? a.units * a.join_groups : 0;
   if (!a.blocks || joins > 0x7fffffff) return fail(CS_ERR_UNSUPPORTED, "cs_attention_cache: too many rows");
-  if (a.planned) {
+  a.part_o = static_cast<float*>(workspace);
+  a.part_ml = a.part_o + (size_t)a.blocks * (size_t)a.rows * (size_t)a.shape.head_dim;
+  a.share_of = reinterpret_cast<int32_t*>(a.part_ml + (size_t)a.blocks * (size_t)a.rows * 2);
+  if (a.join && a.planned) {
     hipLaunchKernelGGL(share_out_kernel, dim3(1), dim3(1024), 0, stream, a);
     CS_HIP(hipGetLastError());
   }
   if (a.shape.head_dim == 128) launch_attend<4>(a, stream);
   else launch_attend<2>(a, stream);
   CS_HIP(hipGetLastError());
-  if (a.join) {
+  if (joins) {
     if (a.shape.head_dim == 128) hipLaunchKernelGGL((join_shares_kernel<4>), dim3((unsigned)joins), dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((join_shares_kernel<2>), dim3((unsigned)joins), dim3(256), 0, stream, a);
     CS_HIP(hipGetLastError());
   }
+  return CS_OK;
+}
+cs_status launch_cache_attention(const CacheAttnArgs& a, void* workspace, hipStream_t stream) {
+  CacheAttnArgs parts[2];
+  const int n = plan_parts(a, parts);
+  for (int i = 0; i < n; ++i)
+    if (cs_status st = launch_rows(parts[i], workspace, stream)) return st;
   return CS_OK;
 }
 

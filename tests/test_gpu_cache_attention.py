@@ -445,3 +445,62 @@ def test_many_sequences_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, b.run(max_keys=4000)), step
         b.check(out, lens=[(1, max(0, n - 40 * step)) for _, n in lens])
+
+
+# ---- prompts and tokens in one batch: where the host's numbers say so, sequences of few rows and of many have launches of their own
+@pytest.mark.parametrize("heads,kv_heads,dim", [(28, 4, 128), (8, 2, 64), (4, 4, 128), (32, 1, 64), (40, 1, 64)])
+@pytest.mark.parametrize("bound", [None, 1 << 26])
+@pytest.mark.parametrize("lens", [[(100, 150), (1, 40)], [(100, 150), (2, 40)], [(1, 1300), (90, 400), (0, 9), (2, 0), (1, 33), (3, 64), (5, 1), (1, 2)],
+                                  [(66, 66)] + [(1, 13 * i) for i in range(80)]])
+def test_prompts_and_tokens_in_one_batch(lens, heads, kv_heads, dim, bound):
+    b = Batch(lens, heads, kv_heads, dim, 32, seed=20)
+    flag = torch.zeros(1, dtype=torch.int32, device=DEV)
+    kw = {} if bound is None else dict(max_keys=bound)
+    for causal in (True, False):
+        got = b.run(causal=causal, err_flag=flag, **kw)
+        b.check(got, causal)
+        assert torch.equal(got, b.run(causal=causal, **kw))
+    assert flag.item() == 0
+
+
+def test_prompts_and_tokens_with_lists_that_cannot_be():
+    lens = [(1, 1300), (90, 400), (1, 9), (2, 70), (1, 33), (3, 64)] + [(1, 50)] * 70
+    for n in (6, 76):
+        b = Batch(lens[:n], 8, 2, 64, 32, seed=21)
+        T = b.q.shape[0]
+        clean = b.run()
+        flag = torch.zeros(1, dtype=torch.int32, device=DEV)
+        good = b.cu.tolist()
+        for change in ({2: 0}, {3: T}, {1: T, 2: 0, 3: T, 4: 0}, {n: 1 << 30}, {0: -5}, {i: (T if i % 2 else 0) for i in range(n + 1)}):
+            cu = [change.get(i, x) for i, x in enumerate(good)]
+            for kw in ({}, dict(max_keys=1 << 26), dict(max_keys=1024)):
+                flag.zero_()
+                b.run(cu_queries=torch.tensor(cu, dtype=torch.int32, device=DEV), err_flag=flag, **kw)
+                assert flag.item() == 1, (n, change)
+        assert torch.equal(clean, b.run())
+
+
+def test_prompts_and_tokens_in_a_graph():
+    lens = [(80, 900), (1, 2000), (1, 1), (2, 300), (1, 0), (1, 77)]
+    b = Batch(lens, 8, 2, 128, 32, seed=22)
+    out, ws = torch.empty_like(b.q), torch.empty(1 << 27, dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.run(out=out, workspace=ws)
+    for keys in ([900, 2000, 1, 300, 0, 77], [80, 1, 1, 2, 0, 33], [40, 1999, 0, 299, 0, 76]):
+        b.n_keys.copy_(torch.tensor(keys, dtype=torch.int32))
+        ws.fill_(0xff)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, b.run()), keys
+        b.check(out, lens=[(q, n) for (q, _), n in zip(lens, keys)])
+
+
+def test_workspace_of_a_mixed_batch_is_for_its_rows():
+    import ctypes as C
+    need = C.c_size_t()
+    c = B.cs_cache_config(C.sizeof(B.cs_cache_config), 4, 128, 64, 100)
+    x = B.cs_cache_batch(C.sizeof(B.cs_cache_batch), n_seqs=64, n_queries=2048 + 63, max_queries=2048, table_width=200, max_keys=8192)
+    assert B.lib().cs_attention_cache_query(C.byref(c), C.byref(x), 28, C.byref(need)) == 0
+    assert need.value < 128 << 20
