@@ -1,4 +1,4 @@
-"""CPU checker of the LLM task's attention calls: rotation and norm, the 4-bit cache, attention over it.
+"""CPU oracle of the LLM task's attention calls: rotation and norm, the 4-bit cache, attention over it.
 
 Written from the definitions in include/cornenc.h, in numpy fp64, row by row and head by head; test infrastructure only.
 """

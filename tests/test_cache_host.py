@@ -1,4 +1,4 @@
-"""The LLM task's attention calls without a GPU: the CPU checker against brute force, and what the calls refuse before
+"""The LLM task's attention calls without a GPU: the CPU oracle against brute force, and what the calls refuse before
 anything is enqueued."""
 import ctypes as C
 
@@ -9,7 +9,7 @@ from oracle import cache_oracle as O
 from paper_2603_12118_amd import binding as B
 
 
-# ---- the checker
+# ---- the oracle
 def test_quantise_takes_the_nearest_level_and_even_codes_on_ties():
     rng = np.random.default_rng(0)
     x = np.concatenate([rng.standard_normal(64 * 32) * 10.0 ** rng.integers(-6, 6, 64).repeat(32),
@@ -52,7 +52,7 @@ def test_written_rows_read_back():
     assert not rk[[2, 5]].any() and (new != pool).sum() <= 5 * 2 * 2 * (32 + 2)
 
 
-def test_attention_of_the_checker_against_a_direct_sum():
+def test_attention_of_the_oracle_against_a_direct_sum():
     rng = np.random.default_rng(2)
     q, k, v = rng.standard_normal((5, 4, 8)), rng.standard_normal((6, 2, 8)), rng.standard_normal((6, 2, 8))
     out, weight = O.attention(q, [k, k[:2]], [v, v[:2]], [2, 3], 0.3)

@@ -1,4 +1,4 @@
-"""The 4-bit cache on the GPU against the CPU checker: every byte written, every value read."""
+"""The 4-bit cache on the GPU against the CPU oracle: every byte written, every value read."""
 import numpy as np
 import pytest
 import torch

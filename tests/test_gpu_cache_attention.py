@@ -1,4 +1,4 @@
-"""Attention over the 4-bit cache against the fp64 checker, which reads the same bytes.
+"""Attention over the 4-bit cache against the fp64 oracle, which reads the same bytes.
 
 Tolerance, per value: out = sum p v.  Probabilities are rounded to bf16 (at most 2^-8 of each), the result is too (2^-8 of
 it); scores are sums of exact products in fp32, off by at most 2 D 2^-24 sum |q k| scale, which moves a probability by that share
@@ -16,7 +16,7 @@ DEV = "cuda:0"
 
 
 class Batch:
-    """Sequences with random pages in a pool of random bytes; their keys written by the checker."""
+    """Sequences with random pages in a pool of random bytes; their keys written by the oracle."""
 
     def __init__(self, lens, heads, kv_heads, dim, page, seed=0, spare_width=2, loud=False):
         rng = np.random.default_rng(seed)
@@ -38,7 +38,7 @@ class Batch:
                 k, v = k * 3.0, v * 10.0 ** rng.integers(-6, 6, (n, 1, 1))
             ks.append(k)
             vs.append(v)
-        # (the checker's writer is slow: the bytes come from its quantiser, a page at a time where whole)
+        # (the oracle's writer is slow: the bytes come from its quantiser, a page at a time where whole)
         self.slots = np.concatenate(slots) if slots else np.zeros(0, np.int64)
         k, v = np.concatenate(ks), np.concatenate(vs)
         codes = [O.quantise(x) for x in (k, v)]

@@ -1,4 +1,4 @@
-"""The attention calls of the LLM task run together (paper_2603_12118_amd/consumer_layer.py), each stage against the fp64 checker.
+"""The attention calls of the LLM task run together (paper_2603_12118_amd/consumer_layer.py), each stage against the fp64 oracle.
 
 Tolerances.  QKV rows are rounded to bf16, 2^-8 of each value; the norm's root follows its values, so a normed value is off by at most
 2 * 2^-8 of itself, a rotated one by that of |a| + |b|, and the result is rounded once more: 2^-6 of |a| + |b| covers them.  The fp32

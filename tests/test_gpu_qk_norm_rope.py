@@ -1,4 +1,4 @@
-"""Queries and keys normed and rotated, against the fp64 checker.
+"""Queries and keys normed and rotated, against the fp64 oracle.
 
 Tolerances.  With u = 2^-24: a sum of D squares is off by at most D u of itself, its root by half that, and the few
 products behind it by 8 u, so a normed value is off by (D/2 + 8) u of itself, the rotated one by that of |a| + |b|
@@ -47,7 +47,7 @@ def packed(rng, T, H, K, D, dtype, scale=1.0):
     (1, 28, 4, 128, (16, 24, 24), False), (3, 1, 1, 64, (32,), False), (67, 8, 2, 64, (12, 10, 10), True), (130, 5, 3, 80, (8, 16, 16), False),
     (9, 4, 4, 96, (24, 24), False), (5, 3, 1, 256, (32, 48, 48), False), (33, 16, 16, 128, (24, 20, 20), True), (7, 2, 2, 16, (3, 5), False),
     (4, 6, 2, 128, (0, 16, 16), False), (2049, 2, 1, 48, (8,), False), (6, 40, 8, 128, (5, 3, 56), False), (2, 2, 1, 32, (6, 1, 1), True)])
-def test_against_the_checker(T, H, K, D, sections, interleaved, norm, dtype):
+def test_against_the_oracle(T, H, K, D, sections, interleaved, norm, dtype):
     rng = np.random.default_rng(T + D)
     qkv, q, k = packed(rng, T, H, K, D, dtype)
     before = qkv.clone()
