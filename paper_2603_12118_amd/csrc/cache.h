@@ -17,9 +17,9 @@ struct QkArgs {
   const int32_t* positions;                     // [n_rows, axes]
   int64_t n_rows, n_positions;
   int32_t n_heads, n_kv_heads, head_dim, half, axes;
-  int32_t end0, end1;                           // contiguous sections: pair j follows axis 0 below end0, 1 below end1, then 2
-  int32_t lim1, lim2;                           // interleaved: pair j % 3 == 1 below lim1 follows axis 1, == 2 below lim2 axis 2
-  int32_t interleaved;
+  // the axis pair j follows: 1 from end0 on or where j % 3 == 1 below lim1, 2 from end1 on or where j % 3 == 2 below lim2, else 0
+  int32_t end0, end1;                           // contiguous sections (the number of pairs where they are interleaved)
+  int32_t lim1, lim2;                           // interleaved ones (else 0)
   float eps;
   int32_t* err;
   int32_t parts;                                // set by the launcher: workgroup rows that share out a token's heads

@@ -76,12 +76,12 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= a.n_rows) return;
   const int lane = threadIdx.x & 63, l = lane & (LPH - 1), slot = lane / LPH;
-  int64_t pos[3] = {0, 0, 0};
+  int64_t pos[3];
+#pragma unroll
+  for (int x = 0; x < 3; ++x) pos[x] = a.positions[row * a.axes + (x < a.axes ? x : a.axes - 1)];      // (all at once, whatever the axes)
   bool bad = false;
-  for (int x = 0; x < a.axes; ++x) {
-    pos[x] = a.positions[row * a.axes + x];
-    bad |= pos[x] < 0 || pos[x] >= a.n_positions;
-  }
+#pragma unroll
+  for (int x = 0; x < 3; ++x) bad |= pos[x] < 0 || pos[x] >= a.n_positions;
   if (bad) {
     if (a.err && lane == 0 && blockIdx.y == 0) atomicOr(a.err, 1);
     return;
@@ -90,17 +90,15 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
   const bool turns = l < rot_lanes, has = l < (a.head_dim >> 4);
   const int d0 = turns ? 8 * l : 2 * a.half + 16 * (l - rot_lanes), d1 = turns ? a.half + 8 * l : d0 + 8;
   float c[8], s[8];
+  const int first = turns ? 8 * l : 0;          // (every lane loads, so that nothing waits for a branch; those that do not turn drop it)
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int j = 8 * l + i, m = j % 3;
-    const int axis = a.interleaved ? (m == 1 && j < a.lim1 ? 1 : m == 2 && j < a.lim2 ? 2 : 0) : j < a.end0 ? 0 : j < a.end1 ? 1 : 2;
-    c[i] = 1.f;
-    s[i] = 0.f;
-    if (turns) {
-      const float2 cs = *reinterpret_cast<const float2*>(a.cos_sin + ((axis == 0 ? pos[0] : axis == 1 ? pos[1] : pos[2]) * a.half + j) * 2);
-      c[i] = cs.x;
-      s[i] = cs.y;
-    }
+    const int j = first + i, m = j % 3;
+    const bool second = (j >= a.end0) | ((m == 1) & (j < a.lim1)), third = (j >= a.end1) | ((m == 2) & (j < a.lim2));
+    const int64_t at = third ? pos[2] : second ? pos[1] : pos[0];
+    const float2 cs = *reinterpret_cast<const float2*>(a.cos_sin + (at * a.half + j) * 2);
+    c[i] = turns ? cs.x : 1.f;
+    s[i] = turns ? cs.y : 0.f;
   }
   const int heads = a.n_heads + a.n_kv_heads, steps = (heads + HEADS - 1) / HEADS;
   for (int step = blockIdx.y; step < steps; step += a.parts) {
@@ -109,7 +107,12 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
     float x[8] = {}, y[8] = {};
     const void* src = is_q ? a.q : a.k;
     const int64_t at = is_q ? row * a.q_row + (int64_t)h * a.head_dim : row * a.k_row + (int64_t)(h - a.n_heads) * a.head_dim;
+    float g0[8] = {}, g1[8] = {};
     if (live) {
+      if (a.norm) {                     // (asked for with the values, not behind their sum)
+        load8<false, false>(is_q ? a.q_gain : a.k_gain, d0, g0);
+        load8<false, false>(is_q ? a.q_gain : a.k_gain, d1, g1);
+      }
       load8<BF16, true>(src, at + d0, x);
       load8<BF16, true>(src, at + d1, y);
     }
@@ -120,16 +123,10 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
 #pragma unroll
       for (int m = 1; m < LPH; m <<= 1) sum += __shfl_xor(sum, m);
       const float r = rsqrtf(sum / (float)a.head_dim + a.eps);
-      if (live) {
-        const float* g = is_q ? a.q_gain : a.k_gain;
-        float g0[8], g1[8];
-        load8<false, false>(g, d0, g0);
-        load8<false, false>(g, d1, g1);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[i] *= r * g0[i];
-          y[i] *= r * g1[i];
-        }
+      for (int i = 0; i < 8; ++i) {
+        x[i] *= r * g0[i];
+        y[i] *= r * g1[i];
       }
     }
     if (!live) continue;
@@ -218,6 +215,12 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheRows a) {
   if (row >= a.n_rows) return;      // (whole groups of lanes)
   const int c = threadIdx.x % LANES, h = blockIdx.y;
   const int64_t slot = a.slots[row];
+  float x[8], y[8];
+  load8<BF16, false>(a.k, row * a.k_row + h * D + 8 * c, x);
+  load8<BF16, false>(a.v, row * a.v_row + h * D + 8 * c, y);
+  int kb, vb;
+  bool ko, vo;
+  const uint32_t kw = quantise8(x, kb, ko), vw = quantise8(y, vb, vo);        // (in front of the slot's branch: the rows come while the slot does)
   if (slot < 0 || slot >= a.shape.slots) {
     if (slot != -1 && a.err && c == 0 && h == 0) atomicOr(a.err, 1);
     return;
@@ -225,12 +228,6 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheRows a) {
   const int64_t page = (int64_t)__umul64hi((uint64_t)slot, a.shape.page_recip), P = a.shape.page_tokens;
   const int o = (int)(slot - page * P);
   unsigned char* block = a.pool + (page * a.shape.n_kv_heads + h) * a.shape.head_bytes;
-  float x[8], y[8];
-  load8<BF16, false>(a.k, row * a.k_row + h * D + 8 * c, x);
-  load8<BF16, false>(a.v, row * a.v_row + h * D + 8 * c, y);
-  int kb, vb;
-  bool ko, vo;
-  const uint32_t kw = quantise8(x, kb, ko), vw = quantise8(y, vb, vo);
   *reinterpret_cast<uint32_t*>(block + Place<D>::k(o, c)) = kw;
   unsigned char* vp = block + Place<D>::v(P, o, c);
   if constexpr (D == 128) {

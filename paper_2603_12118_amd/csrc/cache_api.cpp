@@ -130,9 +130,14 @@ cs_status qk_norm_rope(const cs_qk_config* c, const void* q, int64_t q_row, cons
   a.norm = norm; a.q_gain = q_gain; a.k_gain = k_gain; a.cos_sin = cos_sin; a.positions = positions;
   a.n_rows = n_rows; a.n_positions = c->n_positions;
   a.n_heads = c->n_heads; a.n_kv_heads = c->n_kv_heads; a.head_dim = c->head_dim; a.half = half; a.axes = c->axes;
-  a.end0 = c->sections[0]; a.end1 = c->sections[0] + c->sections[1];
-  a.lim1 = 3 * c->sections[1]; a.lim2 = 3 * c->sections[2];
-  a.interleaved = c->interleaved; a.eps = c->eps; a.err = err_flag;
+  if (c->interleaved) {
+    a.end0 = a.end1 = half;
+    a.lim1 = 3 * c->sections[1]; a.lim2 = 3 * c->sections[2];
+  } else {
+    a.end0 = c->sections[0]; a.end1 = c->sections[0] + c->sections[1];
+    a.lim1 = a.lim2 = 0;
+  }
+  a.eps = c->eps; a.err = err_flag;
   return launch_qk_norm_rope(a, dtype, static_cast<hipStream_t>(stream));
 }
 
