@@ -2,8 +2,8 @@
 //
 // All three are bound by memory: a few operations a value.  Every access is 16 bytes a lane, and a lane keeps its values
 // in registers from the load to the store.  What is read once, or written and not read again here, goes past the caches
-// (ONCE) where that measured faster, in loops of calls on tensors that the caches do not hold: rotation of 16384 x 32 heads of 128, bf16,
-// loads 58.9 -> 50.9 us, stores too 55.6; values out of the cache, 65536 rows of 4 heads of 128, stores 41.1 -> 25.7; rows
+// (ONCE) where that measured faster, in loops of calls on tensors that the caches do not hold (before later steps): rotation of 16384 x 32 heads
+// of 128, bf16, loads 58.9 -> 50.9 us, stores too 55.6; values out of the cache, 65536 rows of 4 heads of 128, stores 41.1 -> 25.7; rows
 // into the cache: loads of 16384 rows of 8 heads 29.5 -> 32.0 with their reading back, so they are plain.
 #include "cache.h"
 
@@ -68,8 +68,9 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const float (&x)[
 // ---- norm and rotation.  A lane holds sixteen values of a head: pairs 8l .. 8l+7, both members, so that the rotation
 // needs no other lane; lanes behind the rotary part hold sixteen values that pass.  A head is LPH lanes (head_dim / 16 of
 // them with values), a wave takes one token, 64 / LPH of its heads at a time: the angles are read once a token.
-// 16384 rows of 32 heads of 128, bf16 (277 MB): 50.5 us, 5.5 TB/s; 1125 rows of 10 heads of 64, fp32: 5.6 us; one row: 3.9 us, a
-// launch and three reads one behind the other (positions, angles, gains).
+// 16384 rows of 32 heads of 128, bf16 (277 MB): 47.5 us, 5.8 TB/s; 1125 rows of 10 heads of 64, fp32: 4.7 us; one row: 3.2 us, a
+// launch and three reads one behind the other (positions, angles, values).  What does not depend on one another is asked for at once: positions and
+// angles one by one, and gains behind the sum, took 51.9, 5.5 and 4.3 us.
 template <bool BF16, int LPH>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
   constexpr int HEADS = 64 / LPH;               // heads of a wave at a time
@@ -165,8 +166,8 @@ cs_status launch_qk_norm_rope(const QkArgs& args, int dtype, hipStream_t stream)
 
 // ---- the cache.  D / 8 lanes hold a row of one head, eight values each: a lane's K codes are one word, a group of 32
 // values is four neighbouring lanes.  Rows go to slots in any order, so a row's codes are pieces of 4 bytes in two blocks; the rows of a
-// workgroup, mostly neighbours, fill whole lines between them.  16384 rows of 8 heads of 128, bf16, in (67 MB + 18 MB): 14.4 us,
-// 5.9 TB/s, and out again 13.9; 65536 rows of 4 heads out (36 + 134 MB): 25.7 us, 6.6 TB/s; 48 rows 3 us, the launch.
+// workgroup, mostly neighbours, fill whole lines between them.  16384 rows of 8 heads of 128, bf16, in (67 MB + 18 MB): 13.9 us,
+// 6.1 TB/s, and out again 14.0; 65536 rows of 4 heads out (36 + 134 MB): 25.7 us, 6.6 TB/s; 48 rows 3 us, the launch.
 // Where the words of chunk c (values 8c .. 8c+7) of token `o` are in a block (see cs_cache_config).
 template <int D>
 struct Place {

@@ -245,7 +245,7 @@ __device__ __forceinline__ void store_row(const CacheAttnArgs& a, int q0, int h,
 // ---- few rows: 16 RT of them, a wave's keys its own.  The softmax keeps a running maximum and sum (fp32) a row and wave, joined at the end.
 // Bound by the memory once there are enough keys: 64 sequences of 8192 (285 MB) 57 us with their join, 5.0 TB/s.  Fewer are bound by the way to
 // a wave's first tile (arguments, lengths, page table, tile: four reads, one behind the other) and by the join: 64 of 160 .. 16384 keys
-// (119 MB) 29 + 5.5 us, one of 131072 (71 MB) 18.5 + 7.4, one of 2048 5.9 + 5.0, six of up to 4097 with 5 queries 12.3 + 4.8.  While a wave
+// (119 MB) 30 + 5.4 us, one of 131072 (71 MB) 18.2 + 7.3, one of 2048 5.5 + 5.0, six of up to 4097 with 5 queries 12.9 + 4.5.  While a wave
 // works on a tile its next one is on its way: 17.8 MB over the chip, 2.8 us at 6.3 TB/s; two ahead do not fit the registers of four waves a
 // SIMD.  The loop is some 200 vector and 16 matrix instructions a tile; an eighth fewer of the former changed nothing.
 template <int NG, int RT>
