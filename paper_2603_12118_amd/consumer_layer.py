@@ -36,11 +36,11 @@ def prompt_positions(parts):
 
 
 class PagePool:
-    """The pages of the sequences that a layer serves, kept on the host; `table` is their copy on the GPU."""
+    """The pages of the sequences that a layer serves, kept on the host; `table` is their copy on the GPU (-1: no page)."""
 
     def __init__(self, n_pages: int, page_tokens: int, sequences: int, width: int, device):
         self.page_tokens, self.free = page_tokens, list(range(n_pages))[::-1]
-        self.owned, self.lens = [[] for _ in range(sequences)], [0] * sequences
+        self.owned, self.lens, self.releases = [[] for _ in range(sequences)], [0] * sequences, [0] * sequences
         self.table = torch.full((sequences, width), -1, dtype=torch.int32, device=device)
 
     def reserve(self, b: int, tokens: int) -> None:
@@ -59,8 +59,11 @@ class PagePool:
         return np.asarray(self.owned[b], np.int64)[t // self.page_tokens] * self.page_tokens + t % self.page_tokens
 
     def release(self, b: int) -> None:
+        """Sequence b has ended: its pages are another's to take.  Recorded steps leave it out (DecodeStep.take)."""
         self.free += self.owned[b][::-1]
         self.owned[b], self.lens[b] = [], 0
+        self.releases[b] += 1
+        self.table[b] = -1
 
 
 class ConsumerLayer:
@@ -112,26 +115,40 @@ class ConsumerLayer:
 
 class DecodeStep:
     """One token of every sequence of a layer, recorded once: fill `x`, call `run`, read `out`.  Lengths, positions and slots stay on the
-    GPU and advance in the recording; the host only sees to it that the pages are there."""
+    GPU and advance in the recording; the host only sees to it that the pages are there.  A sequence that was released is left out: its row of
+    `x` goes nowhere, its rows of `out` and `attended` are zeros, until `take` hands the step the sequence that is in its place."""
 
     def __init__(self, layer: ConsumerLayer, next_position):
+        """next_position: of every sequence the position of its next token, or None where the step is to leave it out."""
         self.layer, n, dev = layer, len(layer.pages.lens), layer.device
+        if len(next_position) != n:
+            raise ValueError(f"next_position: expected {n}, one a sequence")
         self.x = torch.zeros(n, layer.hidden, dtype=torch.bfloat16, device=dev)
-        self.n_keys = torch.tensor(layer.pages.lens, dtype=torch.int32, device=dev)
-        self.positions = torch.tensor(next_position, dtype=torch.int32, device=dev)[:, None].repeat(1, 3)
+        self.n_keys, self.ahead = (torch.zeros(n, dtype=torch.int32, device=dev) for _ in range(2))       # ahead: tokens a step adds, 0 or 1
+        self.live, self.positions = torch.zeros(n, dtype=torch.bool, device=dev), torch.zeros(n, 3, dtype=torch.int32, device=dev)
+        self.serves, self.releases = [False] * n, [0] * n
         self.cu = torch.arange(n + 1, dtype=torch.int32, device=dev)
         # (a warm-up pass runs the calls once outside the recording, on a length of zero and no slot: it changes no cache)
-        self.slots = torch.full((n,), -1, dtype=torch.int64, device=dev)
+        self.slots, self.no_slot = torch.full((n,), -1, dtype=torch.int64, device=dev), torch.full((n,), -1, dtype=torch.int64, device=dev)
         self._pass(torch.zeros_like(self.n_keys))
+        for b, position in enumerate(next_position):
+            self.take(b, position)
         torch.cuda.synchronize()
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):
             P = layer.pages.page_tokens
             page = layer.pages.table.gather(1, (self.n_keys // P).long()[:, None])[:, 0].long()
-            self.slots.copy_(page * P + self.n_keys % P)
-            self.n_keys += 1
+            torch.where(self.live, torch.add(self.n_keys % P, page, alpha=P), self.no_slot, out=self.slots)
+            self.n_keys += self.ahead
             self.out, self.q, self.attended = self._pass(self.n_keys)
-            self.positions += 1
+            self.positions += self.ahead[:, None]
+
+    def take(self, b: int, next_position) -> None:
+        """From now on the step serves sequence b as the layer holds it, its next token at `next_position`, or leaves it out (None)."""
+        pages = self.layer.pages
+        self.serves[b], self.releases[b] = next_position is not None, pages.releases[b]
+        self.live[b] = self.ahead[b] = self.serves[b]
+        self.n_keys[b], self.positions[b] = (pages.lens[b], next_position) if self.serves[b] else (0, 0)
 
     def _pass(self, n_keys):
         layer = self.layer
@@ -140,8 +157,12 @@ class DecodeStep:
     def run(self):
         pages = self.layer.pages
         for b in range(len(pages.lens)):
-            pages.reserve(b, pages.lens[b] + 1)
-            pages.lens[b] += 1
+            if self.serves[b] and self.releases[b] != pages.releases[b]:
+                self.take(b, None)
+        for b in range(len(pages.lens)):
+            if self.serves[b]:
+                pages.reserve(b, pages.lens[b] + 1)
+                pages.lens[b] += 1
         self.graph.replay()
         return self.out
 

@@ -1,0 +1,20 @@
+"""The host's side of a layer's sequences (paper_2603_12118_amd/consumer_layer.py), with tensors on the CPU."""
+import numpy as np
+
+from paper_2603_12118_amd.consumer_layer import PagePool
+
+
+def pool(n_pages=6, sequences=2, width=4, **kw):
+    return PagePool(n_pages, 32, sequences, width, "cpu", **kw)
+
+
+def test_a_released_sequence_has_no_pages_anywhere():
+    p = pool()
+    p.reserve(0, 70)
+    p.lens[0] = 70
+    p.release(0)
+    assert p.owned[0] == [] and p.lens[0] == 0 and sorted(p.free) == list(range(6))
+    assert (p.table == -1).all()                              # (the GPU must not find another sequence's pages there)
+    p.reserve(1, 90)
+    assert p.table.tolist() == [[-1] * 4, p.owned[1] + [-1]]
+    assert np.array_equal(p.slots(1, 31, 3), [p.owned[1][0] * 32 + 31, p.owned[1][1] * 32, p.owned[1][1] * 32 + 1])

@@ -1,0 +1,128 @@
+"""Sequences that come and go under a recorded step (paper_2603_12118_amd/consumer_layer.py): every step against the same calls made one
+by one on a second layer, bit for bit, and what a step may not touch unchanged."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_12118_amd import binding as B
+from paper_2603_12118_amd import consumer_layer as L
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def small(sequences=3, **kw):
+    args = dict(hidden=128, n_heads=4, n_kv_heads=2, head_dim=64, sections=(8, 12, 12), max_position=512, n_pages=24, page_tokens=32,
+                sequences=sequences, max_keys=256) | kw
+    return L.ConsumerLayer(**args)
+
+
+def rows(n, seed):
+    return torch.randn(n, 128, generator=torch.Generator(DEV).manual_seed(seed), device=DEV, dtype=torch.bfloat16)
+
+
+def text(first, n):
+    return torch.arange(first, first + n, dtype=torch.int32, device=DEV)[:, None].repeat(1, 3)
+
+
+def one_by_one(layer, x, at):
+    """A step of the sequences with a position in `at` (None: left out), without a recording."""
+    pages, slots = layer.pages, []
+    for b, position in enumerate(at):
+        slots.append(np.array([-1]))
+        if position is not None:
+            pages.reserve(b, pages.lens[b] + 1)
+            slots[b] = pages.slots(b, pages.lens[b], 1)
+            pages.lens[b] += 1
+    positions = torch.tensor([p or 0 for p in at], dtype=torch.int32, device=DEV)[:, None].repeat(1, 3)
+    keys = torch.tensor([0 if p is None else n for p, n in zip(at, pages.lens)], dtype=torch.int32, device=DEV)
+    return layer.forward(x, positions, torch.as_tensor(np.concatenate(slots), device=DEV), torch.arange(len(at) + 1, dtype=torch.int32, device=DEV), keys,
+                         pages.table, 1, layer.max_keys)
+
+
+def everything(layer):
+    """What every slot of the pool holds."""
+    slots = torch.arange(layer.pool.shape[0] * layer.pages.page_tokens, device=DEV)
+    return torch.cat(B.cs_cache_read(layer.pool, slots, layer.n_kv_heads, layer.head_dim, layer.pages.page_tokens, dtype=torch.float32), 1)
+
+
+def both(lens, **kw):
+    """Two layers alike, each sequence with `lens` text tokens."""
+    pair = small(len(lens), **kw), small(len(lens), **kw)
+    for layer in pair:
+        layer.prefill(range(len(lens)), [rows(n, b) for b, n in enumerate(lens)], [text(0, n) for n in lens])
+    return pair
+
+
+def same_step(step, layer, seed, at):
+    """One step of the recording and of `layer`: the same bits, and only the slots of the new tokens touched."""
+    recorded, x = step.layer, rows(len(at), seed)
+    before = everything(recorded)
+    step.x.copy_(x)
+    got = step.run().clone()
+    want, _, _ = one_by_one(layer, x, at)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    assert recorded.pages.lens == layer.pages.lens and recorded.pages.owned == layer.pages.owned
+    assert torch.equal(recorded.pages.table, layer.pages.table) and torch.equal(recorded.pool, layer.pool)
+    untouched = torch.ones(len(before), dtype=torch.bool, device=DEV)
+    for b, position in enumerate(at):
+        if position is None:
+            assert not got[b].any() and not step.attended[b].any()
+        else:
+            untouched[recorded.pages.slots(b, recorded.pages.lens[b] - 1, 1)] = False
+    assert torch.equal(everything(recorded)[untouched], before[untouched])
+    assert recorded.err.item() == 0
+
+
+def test_a_released_sequence_is_left_out_until_another_is_taken():
+    recorded, layer = both([70, 96, 20])
+    step = L.DecodeStep(recorded, [70, 96, 20])
+    for i in range(2):
+        same_step(step, layer, 100 + i, [70 + i, 96 + i, 20 + i])
+    for x in (recorded, layer):
+        x.pages.release(0)
+    for i in range(2, 14):                                    # sequence 2 moves on to a page that sequence 0 had
+        same_step(step, layer, 100 + i, [None, 96 + i, 20 + i])
+    for x in (recorded, layer):                               # another sequence in its place, in chunks, steps of the others in between
+        x.prefill([0], [rows(40, 7)], [text(0, 40)])
+    same_step(step, layer, 120, [None, 110, 34])
+    for x in (recorded, layer):
+        x.prefill([0], [rows(50, 8)], [text(40, 50)])
+    same_step(step, layer, 121, [None, 111, 35])
+    step.take(0, 90)
+    for i in range(40):
+        same_step(step, layer, 130 + i, [90 + i, 112 + i, 36 + i])
+    for b in range(3):
+        near = L.attention_of_cached(recorded, b, step.q[b:b + 1])
+        assert (step.attended[b:b + 1].float() - near).abs().max().item() < 0.03
+
+
+def test_a_released_sequence_that_was_full():
+    recorded, layer = both([256, 40])                         # every column of its table in use
+    step = L.DecodeStep(recorded, [None, 40])
+    same_step(step, layer, 100, [None, 40])
+    for x in (recorded, layer):
+        x.pages.release(0)
+    same_step(step, layer, 101, [None, 41])
+    recorded, layer = both([254, 40])
+    step = L.DecodeStep(recorded, [254, 40])
+    for i in range(2):
+        same_step(step, layer, 110 + i, [254 + i, 40 + i])
+    for x in (recorded, layer):
+        x.pages.release(0)
+    for i in range(2, 5):
+        same_step(step, layer, 110 + i, [None, 40 + i])
+
+
+def test_a_step_of_its_sequences_alone():
+    recorded, layer = both([5, 33, 64])
+    step = L.DecodeStep(recorded, [None, 33, None])
+    for i in range(3):
+        same_step(step, layer, 100 + i, [None, 33 + i, None])
+    step.take(2, 64)
+    same_step(step, layer, 103, [None, 36, 64])
+    step.take(1, None)
+    same_step(step, layer, 104, [None, None, 65])
+    with pytest.raises(ValueError):
+        L.DecodeStep(recorded, [5, 33])
