@@ -116,7 +116,8 @@ class ConsumerLayer:
 class DecodeStep:
     """One token of every sequence of a layer, recorded once: fill `x`, call `run`, read `out`.  Lengths, positions and slots stay on the
     GPU and advance in the recording; the host only sees to it that the pages are there.  A sequence that was released is left out: its row of
-    `x` goes nowhere, its rows of `out` and `attended` are zeros, until `take` hands the step the sequence that is in its place."""
+    `x` goes nowhere, its rows of `out` and `attended` are zeros, until `take` hands the step the sequence that is in its place.  One that was
+    given tokens by other calls has to be taken again, too: until then `run` refuses."""
 
     def __init__(self, layer: ConsumerLayer, next_position):
         """next_position: of every sequence the position of its next token, or None where the step is to leave it out."""
@@ -126,7 +127,7 @@ class DecodeStep:
         self.x = torch.zeros(n, layer.hidden, dtype=torch.bfloat16, device=dev)
         self.n_keys, self.ahead = (torch.zeros(n, dtype=torch.int32, device=dev) for _ in range(2))       # ahead: tokens a step adds, 0 or 1
         self.live, self.positions = torch.zeros(n, dtype=torch.bool, device=dev), torch.zeros(n, 3, dtype=torch.int32, device=dev)
-        self.serves, self.releases = [False] * n, [0] * n
+        self.serves, self.releases, self.lens = [False] * n, [0] * n, [0] * n
         self.cu = torch.arange(n + 1, dtype=torch.int32, device=dev)
         # (a warm-up pass runs the calls once outside the recording, on a length of zero and no slot: it changes no cache)
         self.slots, self.no_slot = torch.full((n,), -1, dtype=torch.int64, device=dev), torch.full((n,), -1, dtype=torch.int64, device=dev)
@@ -146,7 +147,7 @@ class DecodeStep:
     def take(self, b: int, next_position) -> None:
         """From now on the step serves sequence b as the layer holds it, its next token at `next_position`, or leaves it out (None)."""
         pages = self.layer.pages
-        self.serves[b], self.releases[b] = next_position is not None, pages.releases[b]
+        self.serves[b], self.releases[b], self.lens[b] = next_position is not None, pages.releases[b], pages.lens[b]
         self.live[b] = self.ahead[b] = self.serves[b]
         self.n_keys[b], self.positions[b] = (pages.lens[b], next_position) if self.serves[b] else (0, 0)
 
@@ -159,10 +160,13 @@ class DecodeStep:
         for b in range(len(pages.lens)):
             if self.serves[b] and self.releases[b] != pages.releases[b]:
                 self.take(b, None)
+            if self.serves[b] and self.lens[b] != pages.lens[b]:
+                raise RuntimeError(f"sequence {b} has {pages.lens[b]} tokens, {self.lens[b]} of them known to the step: take({b}, its next position)")
         for b in range(len(pages.lens)):
             if self.serves[b]:
                 pages.reserve(b, pages.lens[b] + 1)
                 pages.lens[b] += 1
+                self.lens[b] += 1
         self.graph.replay()
         return self.out
 

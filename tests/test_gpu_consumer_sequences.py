@@ -126,3 +126,23 @@ def test_a_step_of_its_sequences_alone():
     same_step(step, layer, 104, [None, None, 65])
     with pytest.raises(ValueError):
         L.DecodeStep(recorded, [5, 33])
+
+
+def test_tokens_given_by_other_calls_are_taken_over():
+    recorded, layer = both([30, 62])
+    step = L.DecodeStep(recorded, [30, 62])
+    same_step(step, layer, 100, [30, 62])
+    for x in (recorded, layer):                               # more of sequence 1's prompt, behind the recording
+        x.prefill([1], [rows(7, 5)], [text(63, 7)])
+    held, lens, owned = recorded.pool.clone(), list(recorded.pages.lens), [list(o) for o in recorded.pages.owned]
+    with pytest.raises(RuntimeError, match="sequence 1 has 70 tokens"):
+        step.run()
+    torch.cuda.synchronize()
+    assert torch.equal(recorded.pool, held) and recorded.pages.lens == lens and recorded.pages.owned == owned
+    step.take(1, 70)
+    for i in range(3):
+        same_step(step, layer, 101 + i, [31 + i, 70 + i])
+    other = L.DecodeStep(recorded, [34, 73])                  # a second recording moves the same sequences
+    same_step(other, layer, 110, [34, 73])
+    with pytest.raises(RuntimeError, match="sequence 0 has"):
+        step.run()
