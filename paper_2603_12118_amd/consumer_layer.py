@@ -45,14 +45,21 @@ class PagePool:
 
     def reserve(self, b: int, tokens: int) -> None:
         """Pages for `tokens` tokens of sequence b in all."""
-        need = -(-tokens // self.page_tokens) - len(self.owned[b])
-        if need > len(self.free) or tokens > self.table.shape[1] * self.page_tokens:
-            raise RuntimeError(f"no room for {tokens} tokens of sequence {b}")
-        if need > 0:
-            new = [self.free.pop() for _ in range(need)]
-            at = len(self.owned[b])
-            self.table[b, at:at + need] = torch.tensor(new, dtype=torch.int32, device=self.table.device)
-            self.owned[b] += new
+        self.reserve_all({b: tokens})
+
+    def reserve_all(self, tokens) -> None:
+        """Pages for tokens[b] tokens in all of every sequence b of a dict; none for any of them where there is no room for one."""
+        new, left = {}, len(self.free)
+        for b, n in tokens.items():
+            new[b] = max(0, -(-n // self.page_tokens) - len(self.owned[b]))
+            left -= new[b]
+            if left < 0 or n > self.table.shape[1] * self.page_tokens:
+                raise RuntimeError(f"no room for {n} tokens of sequence {b}")
+        for b, n in new.items():
+            if n:
+                pages, at = [self.free.pop() for _ in range(n)], len(self.owned[b])
+                self.table[b, at:at + n] = torch.tensor(pages, dtype=torch.int32, device=self.table.device)
+                self.owned[b] += pages
 
     def slots(self, b: int, first: int, tokens: int) -> np.ndarray:
         t = np.arange(first, first + tokens)
@@ -98,19 +105,22 @@ class ConsumerLayer:
         return out, q, a
 
     def prefill(self, which, rows, positions):
-        """New tokens of the sequences `which`: rows[i] [n, hidden] bf16 and positions[i] int32 [n, 3] on the GPU.  Returns what forward does."""
-        slots, keys = [], []
+        """New tokens of the sequences `which`: rows[i] [n, hidden] bf16 and positions[i] int32 [n, 3] on the GPU.  Returns what forward does.
+        Where there is no room, or a call refuses its tensors, no sequence is longer than before."""
+        parts, after = [], {}
         for b, x in zip(which, rows):
-            first, n = self.pages.lens[b], x.shape[0]
-            self.pages.reserve(b, first + n)
-            slots.append(self.pages.slots(b, first, n))
-            self.pages.lens[b] = first + n
-            keys.append(first + n)
-        lens = [x.shape[0] for x in rows]
+            first = after.get(b, self.pages.lens[b])
+            parts.append((b, first, x.shape[0]))
+            after[b] = first + x.shape[0]
+        self.pages.reserve_all(after)
+        lens, keys = [x.shape[0] for x in rows], [first + n for _, first, n in parts]
         dev = dict(device=self.device)
-        return self.forward(torch.cat(rows), torch.cat(positions), torch.as_tensor(np.concatenate(slots), **dev),
-                            torch.as_tensor(np.cumsum([0] + lens, dtype=np.int32), **dev), torch.tensor(keys, dtype=torch.int32, **dev),
-                            self.pages.table[torch.tensor(which, **dev)], max(lens), max(keys))
+        got = self.forward(torch.cat(rows), torch.cat(positions), torch.as_tensor(np.concatenate([self.pages.slots(*x) for x in parts]), **dev),
+                           torch.as_tensor(np.cumsum([0] + lens, dtype=np.int32), **dev), torch.tensor(keys, dtype=torch.int32, **dev),
+                           self.pages.table[torch.tensor(which, **dev)], max(lens), max(keys))
+        for b, n in after.items():
+            self.pages.lens[b] = n
+        return got
 
 
 class DecodeStep:
@@ -162,12 +172,12 @@ class DecodeStep:
                 self.take(b, None)
             if self.serves[b] and self.lens[b] != pages.lens[b]:
                 raise RuntimeError(f"sequence {b} has {pages.lens[b]} tokens, {self.lens[b]} of them known to the step: take({b}, its next position)")
-        for b in range(len(pages.lens)):
-            if self.serves[b]:
-                pages.reserve(b, pages.lens[b] + 1)
-                pages.lens[b] += 1
-                self.lens[b] += 1
+        served = [b for b in range(len(pages.lens)) if self.serves[b]]
+        pages.reserve_all({b: pages.lens[b] + 1 for b in served})
         self.graph.replay()
+        for b in served:
+            pages.lens[b] += 1
+            self.lens[b] += 1
         return self.out
 
 

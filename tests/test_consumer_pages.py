@@ -1,5 +1,6 @@
 """The host's side of a layer's sequences (paper_2603_12118_amd/consumer_layer.py), with tensors on the CPU."""
 import numpy as np
+import pytest
 
 from paper_2603_12118_amd.consumer_layer import PagePool
 
@@ -18,3 +19,15 @@ def test_a_released_sequence_has_no_pages_anywhere():
     p.reserve(1, 90)
     assert p.table.tolist() == [[-1] * 4, p.owned[1] + [-1]]
     assert np.array_equal(p.slots(1, 31, 3), [p.owned[1][0] * 32 + 31, p.owned[1][1] * 32, p.owned[1][1] * 32 + 1])
+
+
+def test_room_for_all_or_for_none():
+    p = pool()
+    p.reserve_all({0: 40, 1: 64})
+    owned, table = [list(o) for o in p.owned], p.table.clone()
+    for tokens in ({0: 96, 1: 128}, {1: 65, 0: 129}, {0: 41, 1: 129}):       # 1 + 2 of two pages left; more than four columns
+        with pytest.raises(RuntimeError, match="no room"):
+            p.reserve_all(tokens)
+        assert p.owned == owned and len(p.free) == 2 and (p.table == table).all()
+    p.reserve_all({0: 64, 1: 128})
+    assert p.free == [] and p.table[1].tolist() == p.owned[1]

@@ -146,3 +146,38 @@ def test_tokens_given_by_other_calls_are_taken_over():
     same_step(other, layer, 110, [34, 73])
     with pytest.raises(RuntimeError, match="sequence 0 has"):
         step.run()
+
+
+def test_no_room_for_one_moves_none():
+    recorded, layer = both([40, 64], n_pages=5)                # one page left
+    step = L.DecodeStep(recorded, [40, 64])
+    held, lens = recorded.pool.clone(), [40, 64]
+    for given in ([20, 40], [30, 40], [40, 1], [1, 250]):
+        with pytest.raises(RuntimeError, match="no room"):
+            recorded.prefill([0, 1], [rows(n, 5) for n in given], [text(lens[b], n) for b, n in enumerate(given)])
+        assert recorded.pages.lens == lens and recorded.pages.owned == layer.pages.owned
+    with pytest.raises((ValueError, RuntimeError)):            # positions that are not the rows'
+        recorded.prefill([0], [rows(3, 5)], [text(40, 2)])
+    assert recorded.pages.lens == lens
+    torch.cuda.synchronize()
+    assert torch.equal(recorded.pool, held)
+    for i in range(24):
+        same_step(step, layer, 100 + i, [40 + i, 64 + i])
+    held = recorded.pool.clone()
+    with pytest.raises(RuntimeError, match="no room"):         # sequence 0 would begin a page
+        step.run()
+    torch.cuda.synchronize()
+    assert recorded.pages.lens == [64, 88] and torch.equal(recorded.pool, held)
+    for x in (recorded, layer):
+        x.pages.release(0)
+    for i in range(24, 30):
+        same_step(step, layer, 100 + i, [None, 64 + i])
+
+
+def test_a_sequence_named_twice_goes_on():
+    twice, layer = both([10, 20])
+    got, _, _ = twice.prefill([1, 0, 1], [rows(5, 1), rows(3, 2), rows(40, 3)], [text(20, 5), text(10, 3), text(25, 40)])
+    assert twice.pages.lens == [13, 65]
+    for b, n, seed, at in ((1, 5, 1, 20), (0, 3, 2, 10), (1, 40, 3, 25)):
+        layer.prefill([b], [rows(n, seed)], [text(at, n)])
+    assert torch.equal(everything(twice), everything(layer)) and twice.err.item() == 0
