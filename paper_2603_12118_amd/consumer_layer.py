@@ -38,7 +38,9 @@ def prompt_positions(parts):
 class PagePool:
     """The pages of the sequences that a layer serves, kept on the host; `table` is their copy on the GPU (-1: no page)."""
 
-    def __init__(self, n_pages: int, page_tokens: int, sequences: int, width: int, device):
+    def __init__(self, n_pages: int, page_tokens: int, sequences: int, width: int, device, max_tokens=None):
+        """width: pages a sequence may have; max_tokens: tokens, where they end inside the last page."""
+        self.max_tokens = width * page_tokens if max_tokens is None else min(max_tokens, width * page_tokens)
         self.page_tokens, self.free = page_tokens, list(range(n_pages))[::-1]
         self.owned, self.lens, self.releases = [[] for _ in range(sequences)], [0] * sequences, [0] * sequences
         self.table = torch.full((sequences, width), -1, dtype=torch.int32, device=device)
@@ -53,7 +55,7 @@ class PagePool:
         for b, n in tokens.items():
             new[b] = max(0, -(-n // self.page_tokens) - len(self.owned[b]))
             left -= new[b]
-            if left < 0 or n > self.table.shape[1] * self.page_tokens:
+            if left < 0 or n > self.max_tokens:
                 raise RuntimeError(f"no room for {n} tokens of sequence {b}")
         for b, n in new.items():
             if n:
@@ -86,7 +88,7 @@ class ConsumerLayer:
         pairs = sum(sections)
         angles = torch.arange(max_position, dtype=torch.float64)[:, None] * theta ** (-torch.arange(pairs, dtype=torch.float64) / pairs)
         self.cos_sin = torch.stack((angles.cos(), angles.sin()), -1).float().to(device)
-        self.pages = PagePool(n_pages, page_tokens, sequences, -(-max_keys // page_tokens), device)
+        self.pages = PagePool(n_pages, page_tokens, sequences, -(-max_keys // page_tokens), device, max_keys)
         self.pool = torch.zeros(n_pages, B.cs_cache_query(n_kv_heads, head_dim, page_tokens)[0], dtype=torch.uint8, device=device)
         self.err = torch.zeros(1, dtype=torch.int32, device=device)
         self.device = device

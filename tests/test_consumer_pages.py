@@ -31,3 +31,11 @@ def test_room_for_all_or_for_none():
         assert p.owned == owned and len(p.free) == 2 and (p.table == table).all()
     p.reserve_all({0: 64, 1: 128})
     assert p.free == [] and p.table[1].tolist() == p.owned[1]
+
+
+def test_a_limit_inside_the_last_page():
+    p = pool(max_tokens=100)
+    p.reserve(0, 100)
+    with pytest.raises(RuntimeError, match="no room for 101 tokens"):
+        p.reserve(1, 101)
+    assert pool(max_tokens=1000).max_tokens == pool().max_tokens == 128

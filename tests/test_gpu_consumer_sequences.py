@@ -181,3 +181,16 @@ def test_a_sequence_named_twice_goes_on():
     for b, n, seed, at in ((1, 5, 1, 20), (0, 3, 2, 10), (1, 40, 3, 25)):
         layer.prefill([b], [rows(n, seed)], [text(at, n)])
     assert torch.equal(everything(twice), everything(layer)) and twice.err.item() == 0
+
+
+def test_no_more_keys_than_attention_is_told_of():
+    recorded, layer = both([240, 30], max_keys=250)            # 250 tokens end inside the eighth page
+    step = L.DecodeStep(recorded, [240, 30])
+    for i in range(10):
+        same_step(step, layer, 100 + i, [240 + i, 30 + i])
+    with pytest.raises(RuntimeError, match="no room for 251 tokens of sequence 0"):
+        step.run()
+    with pytest.raises(RuntimeError, match="no room for 251 tokens of sequence 1"):
+        recorded.prefill([1], [rows(211, 5)], [text(40, 211)])
+    torch.cuda.synchronize()
+    assert recorded.pages.lens == [250, 40] and recorded.err.item() == 0 and torch.equal(recorded.pool, layer.pool)
