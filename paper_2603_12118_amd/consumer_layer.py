@@ -139,7 +139,7 @@ class DecodeStep:
         self.x = torch.zeros(n, layer.hidden, dtype=torch.bfloat16, device=dev)
         self.n_keys, self.ahead = (torch.zeros(n, dtype=torch.int32, device=dev) for _ in range(2))       # ahead: tokens a step adds, 0 or 1
         self.live, self.positions = torch.zeros(n, dtype=torch.bool, device=dev), torch.zeros(n, 3, dtype=torch.int32, device=dev)
-        self.serves, self.releases, self.lens = [False] * n, [0] * n, [0] * n
+        self.serves, self.releases, self.lens, self.next = [False] * n, [0] * n, [0] * n, [0] * n
         self.cu = torch.arange(n + 1, dtype=torch.int32, device=dev)
         # (a warm-up pass runs the calls once outside the recording, on a length of zero and no slot: it changes no cache)
         self.slots, self.no_slot = torch.full((n,), -1, dtype=torch.int64, device=dev), torch.full((n,), -1, dtype=torch.int64, device=dev)
@@ -161,7 +161,8 @@ class DecodeStep:
         pages = self.layer.pages
         self.serves[b], self.releases[b], self.lens[b] = next_position is not None, pages.releases[b], pages.lens[b]
         self.live[b] = self.ahead[b] = self.serves[b]
-        self.n_keys[b], self.positions[b] = (pages.lens[b], next_position) if self.serves[b] else (0, 0)
+        self.next[b] = next_position if self.serves[b] else 0
+        self.n_keys[b], self.positions[b] = pages.lens[b] if self.serves[b] else 0, self.next[b]
 
     def _pass(self, n_keys):
         layer = self.layer
@@ -175,11 +176,15 @@ class DecodeStep:
             if self.serves[b] and self.lens[b] != pages.lens[b]:
                 raise RuntimeError(f"sequence {b} has {pages.lens[b]} tokens, {self.lens[b]} of them known to the step: take({b}, its next position)")
         served = [b for b in range(len(pages.lens)) if self.serves[b]]
+        for b in served:                                      # (the calls would leave its rows as they are and set the flag)
+            if not 0 <= self.next[b] < len(self.layer.cos_sin):
+                raise RuntimeError(f"sequence {b}: position {self.next[b]} is not in the rotary table of {len(self.layer.cos_sin)}")
         pages.reserve_all({b: pages.lens[b] + 1 for b in served})
         self.graph.replay()
         for b in served:
             pages.lens[b] += 1
             self.lens[b] += 1
+            self.next[b] += 1
         return self.out
 
 

@@ -194,3 +194,16 @@ def test_no_more_keys_than_attention_is_told_of():
         recorded.prefill([1], [rows(211, 5)], [text(40, 211)])
     torch.cuda.synchronize()
     assert recorded.pages.lens == [250, 40] and recorded.err.item() == 0 and torch.equal(recorded.pool, layer.pool)
+
+
+def test_no_position_behind_the_table():
+    recorded, layer = both([20, 30], max_position=64)
+    step = L.DecodeStep(recorded, [20, 60])                    # (an item's grid may stand far ahead of its number of tokens)
+    for i in range(4):
+        same_step(step, layer, 100 + i, [20 + i, 60 + i])
+    with pytest.raises(RuntimeError, match="sequence 1: position 64"):
+        step.run()
+    torch.cuda.synchronize()
+    assert recorded.pages.lens == [24, 34] and recorded.err.item() == 0 and torch.equal(recorded.pool, layer.pool)
+    step.take(1, None)
+    same_step(step, layer, 104, [24, None])
