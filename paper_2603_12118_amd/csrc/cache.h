@@ -7,6 +7,9 @@ namespace cs {
 // n / d for n < 2^32 and 2 <= d <= 2^31 as a product with recip64(d)
 inline uint64_t recip64(uint64_t d) { return ~0ull / d + 1; }
 
+// Workgroups of 256 threads that a launch may have: HIP refuses more than 2^32 - 1 threads along a dimension of the grid.
+constexpr int64_t MAX_GROUPS = 0xffffffffll / 256;
+
 struct QkArgs {
   const void *q, *k;
   void *q_out, *k_out;

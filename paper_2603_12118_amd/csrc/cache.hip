@@ -8,6 +8,7 @@
 #include "cache.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace cs {
 
@@ -144,12 +145,18 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
   }
 }
 
-cs_status launch_qk_norm_rope(const QkArgs& args, int dtype, hipStream_t stream) {
-  QkArgs a = args;
+// p, `elements` of them further on
+template <class T>
+static T* moved(T* p, int64_t elements, int dtype) {
+  typedef std::conditional_t<std::is_const<T>::value, const unsigned char, unsigned char> bytes;
+  return p ? static_cast<bytes*>(p) + elements * (dtype == CS_BF16 ? 2 : 4) : nullptr;
+}
+
+// as many rows as a grid may have
+static cs_status launch_qk_rows(QkArgs a, int dtype, hipStream_t stream) {
   const int lanes = a.head_dim <= 64 ? 4 : a.head_dim <= 128 ? 8 : 16;
   const int steps = (a.n_heads + a.n_kv_heads + 64 / lanes - 1) / (64 / lanes);
   const int64_t blocks = (a.n_rows + 3) / 4;
-  if (blocks > 0x7fffffff) return fail(CS_ERR_UNSUPPORTED, "cs_qk_norm_rope: too many rows");
   // few tokens: their heads are shared out so that every wave has one step
   a.parts = (int)std::min<int64_t>(steps, std::max<int64_t>(1, 2048 / blocks));
   const dim3 grid((unsigned)blocks, (unsigned)a.parts);
@@ -161,6 +168,19 @@ cs_status launch_qk_norm_rope(const QkArgs& args, int dtype, hipStream_t stream)
   else if (b) hipLaunchKernelGGL((qk_norm_rope_kernel<true, 16>), grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL((qk_norm_rope_kernel<false, 16>), grid, dim3(256), 0, stream, a);
   CS_HIP(hipGetLastError());
+  return CS_OK;
+}
+cs_status launch_qk_norm_rope(const QkArgs& args, int dtype, hipStream_t stream) {
+  for (int64_t first = 0; first < args.n_rows; first += MAX_GROUPS * 4) {
+    QkArgs a = args;
+    a.n_rows = std::min<int64_t>(args.n_rows - first, MAX_GROUPS * 4);
+    a.q = moved(args.q, first * args.q_row, dtype);
+    a.k = moved(args.k, first * args.k_row, dtype);
+    a.q_out = moved(args.q_out, first * args.q_out_row, dtype);
+    a.k_out = moved(args.k_out, first * args.k_out_row, dtype);
+    a.positions = args.positions + first * args.axes;
+    if (cs_status st = launch_qk_rows(a, dtype, stream)) return st;
+  }
   return CS_OK;
 }
 
@@ -276,32 +296,45 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheRows a) {
   store8<BF16, true>(a.v, row * a.v_row + h * D + 8 * c, y);
 }
 
-cs_status launch_cache_write(const CacheRows& a, int dtype, hipStream_t stream) {
-  const int D = a.shape.head_dim;
-  const int64_t blocks = (a.n_rows + 2048 / D - 1) / (2048 / D);
-  if (blocks > 0x7fffffff) return fail(CS_ERR_UNSUPPORTED, "cs_cache_write: too many rows");
-  const dim3 grid((unsigned)blocks, (unsigned)a.shape.n_kv_heads);
-  const bool b = dtype == CS_BF16;
-  if (D == 128 && b) hipLaunchKernelGGL((cache_write_kernel<true, 128>), grid, dim3(256), 0, stream, a);
-  else if (D == 128) hipLaunchKernelGGL((cache_write_kernel<false, 128>), grid, dim3(256), 0, stream, a);
-  else if (b) hipLaunchKernelGGL((cache_write_kernel<true, 64>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((cache_write_kernel<false, 64>), grid, dim3(256), 0, stream, a);
-  CS_HIP(hipGetLastError());
+static int64_t blocks_of(const CacheRows& a) { return (a.n_rows + 2048 / a.shape.head_dim - 1) / (2048 / a.shape.head_dim); }
+// as many rows at a time as a grid may have
+template <class F>
+static cs_status by_grids(const CacheRows& all, int dtype, F launch) {
+  const int64_t most = MAX_GROUPS * (2048 / all.shape.head_dim);
+  for (int64_t first = 0; first < all.n_rows; first += most) {
+    CacheRows a = all;
+    a.n_rows = std::min(all.n_rows - first, most);
+    a.k = moved(all.k, first * all.k_row, dtype);
+    a.v = moved(all.v, first * all.v_row, dtype);
+    a.slots = all.slots + first;
+    launch(a);
+    CS_HIP(hipGetLastError());
+  }
   return CS_OK;
 }
 
-cs_status launch_cache_read(const CacheRows& a, int dtype, hipStream_t stream) {
-  const int D = a.shape.head_dim;
-  const int64_t blocks = (a.n_rows + 2048 / D - 1) / (2048 / D);
-  if (blocks > 0x7fffffff) return fail(CS_ERR_UNSUPPORTED, "cs_cache_read: too many rows");
-  const dim3 grid((unsigned)blocks, (unsigned)a.shape.n_kv_heads);
-  const bool b = dtype == CS_BF16;
-  if (D == 128 && b) hipLaunchKernelGGL((cache_read_kernel<true, 128>), grid, dim3(256), 0, stream, a);
-  else if (D == 128) hipLaunchKernelGGL((cache_read_kernel<false, 128>), grid, dim3(256), 0, stream, a);
-  else if (b) hipLaunchKernelGGL((cache_read_kernel<true, 64>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((cache_read_kernel<false, 64>), grid, dim3(256), 0, stream, a);
-  CS_HIP(hipGetLastError());
-  return CS_OK;
+cs_status launch_cache_write(const CacheRows& rows, int dtype, hipStream_t stream) {
+  const int D = rows.shape.head_dim;
+  return by_grids(rows, dtype, [&](const CacheRows& a) {
+    const dim3 grid((unsigned)blocks_of(a), (unsigned)a.shape.n_kv_heads);
+    const bool b = dtype == CS_BF16;
+    if (D == 128 && b) hipLaunchKernelGGL((cache_write_kernel<true, 128>), grid, dim3(256), 0, stream, a);
+    else if (D == 128) hipLaunchKernelGGL((cache_write_kernel<false, 128>), grid, dim3(256), 0, stream, a);
+    else if (b) hipLaunchKernelGGL((cache_write_kernel<true, 64>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((cache_write_kernel<false, 64>), grid, dim3(256), 0, stream, a);
+  });
+}
+
+cs_status launch_cache_read(const CacheRows& rows, int dtype, hipStream_t stream) {
+  const int D = rows.shape.head_dim;
+  return by_grids(rows, dtype, [&](const CacheRows& a) {
+    const dim3 grid((unsigned)blocks_of(a), (unsigned)a.shape.n_kv_heads);
+    const bool b = dtype == CS_BF16;
+    if (D == 128 && b) hipLaunchKernelGGL((cache_read_kernel<true, 128>), grid, dim3(256), 0, stream, a);
+    else if (D == 128) hipLaunchKernelGGL((cache_read_kernel<false, 128>), grid, dim3(256), 0, stream, a);
+    else if (b) hipLaunchKernelGGL((cache_read_kernel<true, 64>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((cache_read_kernel<false, 64>), grid, dim3(256), 0, stream, a);
+  });
 }
 
 }  // namespace cs
