@@ -73,7 +73,7 @@ struct CacheAttnArgs {
   int32_t row_blocks;     // blocks of so many rows that a sequence and key/value head have at most
   int32_t target;         // workgroups that fill the chip once
   int32_t least;          // tiles of 32 keys that a workgroup takes at least, if there are so many
-  int32_t blocks;         // workgroups of the launch: those without work end at once
+  int32_t blocks;         // workgroups of the launch: those without work end at once (0: more than a grid may have, here or in the joining launch)
   int32_t join;           // 0: no sequence can be shared out; else the threads, in sixteens, that share a row's parts
   int32_t planned;        // the shares are worked out by a launch before
   int64_t units;          // ... units that the joining launch is laid out for
@@ -83,8 +83,8 @@ struct CacheAttnArgs {
   float *part_o, *part_ml;
   int32_t* share_of;      // [n_seqs, 4] first workgroup, shares, tiles of a share, first unit: left by the first launch, or by one before it, for the joining one
 };
-// Bytes of workspace the launches need, from the sizes alone.
-size_t plan_cache_attention(const CacheAttnArgs& a);
+// Bytes of workspace the launches need, from the sizes alone; CS_ERR_UNSUPPORTED where one of them would be too large.
+cs_status plan_cache_attention(const CacheAttnArgs& a, size_t& bytes);
 cs_status launch_cache_attention(const CacheAttnArgs& a, void* workspace, hipStream_t s);
 
 }  // namespace cs

@@ -156,7 +156,8 @@ cs_status attention_cache(const cs_cache_config* c, const void* pool, const cs_c
       !aligned4(b->page_table) || !aligned4(err_flag))
     return invalid(who, "NULL or misaligned lengths, page table or flag");
   CacheAttnArgs a = attention_args(c, b, n_heads);
-  const size_t need = plan_cache_attention(a);
+  size_t need = 0;
+  if (cs_status st = plan_cache_attention(a, need)) return st;
   if (need && (!workspace || !aligned16(workspace))) return invalid(who, "NULL or misaligned workspace");
   if (workspace_bytes < need)
     return fail(CS_ERR_WORKSPACE, std::string(who) + ": needs " + std::to_string(need) + " bytes of workspace, got " + std::to_string(workspace_bytes));
@@ -212,8 +213,7 @@ cs_status cs_attention_cache_query(const cs_cache_config* config, const cs_cache
   if (!workspace_bytes) return invalid("cs_attention_cache_query", "NULL argument");
   if (cs_status st = check_batch("cs_attention_cache_query", config, batch, n_heads)) return st;
   const CacheAttnArgs a = attention_args(config, batch, n_heads);
-  *workspace_bytes = plan_cache_attention(a);
-  return CS_OK;
+  return plan_cache_attention(a, *workspace_bytes);
 }
 CS_CATCH_ALL("cs_attention_cache_query")
 

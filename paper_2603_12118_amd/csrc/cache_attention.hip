@@ -825,6 +825,8 @@ static size_t plan_rows(CacheAttnArgs& a) {
   // units there may be: a sequence's last block of rows may be smaller than the others
   const int64_t seqs = std::min<int64_t>(a.n_seqs, all_rows / (a.more_than + 1)), each = (int64_t)a.n_seqs * a.row_blocks;
   const int64_t bound = std::min(seqs * a.row_blocks, seqs + all_rows / a.rows), row_units = bound * a.shape.n_kv_heads;
+  a.blocks = 0;
+  if (row_units > MAX_GROUPS) return 0;                      // (every launch has at least as many)
   // Tiles of a share, at least.  Up to 1024 keys one workgroup takes them all and there is nothing to join (32 sequences of 500 keys 13.9 ->
   // 9.7 us, one of 1000 the same); a few short rows are shared out finer (one token of 2048 keys 10.4 -> 9.8, of 4096 10.8 -> 10.4).
   a.least = a.rows == 128 ? 8 : tiles <= 32 ? 32 : row_units * ((tiles + 3) / 4) <= 256 ? 4 : 8;
@@ -833,8 +835,8 @@ static size_t plan_rows(CacheAttnArgs& a) {
   const int64_t blocks = most > (1 << 20) ? row_units + a.target + 64 : std::min(row_units * most, row_units + a.target + 64);
   a.join = most == 1 ? 0 : 1;
   // (one launch: a workgroup for every block of rows that a sequence may have)
-  const int64_t grid = a.join ? blocks : each * a.shape.n_kv_heads;
-  a.blocks = grid > 0x7fffffff ? 0 : (int32_t)grid;
+  const int64_t grid = a.join ? blocks : each > MAX_GROUPS ? each : each * a.shape.n_kv_heads;
+  a.blocks = grid > MAX_GROUPS ? 0 : (int32_t)grid;
   if (!a.join || !a.blocks) return 0;
   a.planned = a.n_seqs > 64 || each > 2 * bound;
   a.units = a.planned ? row_units : each * a.shape.n_kv_heads;
@@ -843,6 +845,10 @@ static size_t plan_rows(CacheAttnArgs& a) {
   const int64_t of_block = std::min<int64_t>(rows, a.rows);
   while (a.join < 16 && a.join < most && row_units * of_block * a.join * 2 <= 8192) a.join *= 2;
   a.join_groups = (int32_t)((of_block * a.join + 15) / 16);
+  if (a.units * a.join_groups > MAX_GROUPS) {
+    a.blocks = 0;
+    return 0;
+  }
   return (size_t)a.blocks * (size_t)a.rows * (size_t)(a.shape.head_dim + 2) * 4 + (size_t)a.n_seqs * 16;
 }
 
@@ -859,11 +865,15 @@ static int plan_parts(const CacheAttnArgs& a, CacheAttnArgs (&parts)[2]) {
   parts[0].more_than = parts[1].at_most = few;
   return 2;
 }
-size_t plan_cache_attention(const CacheAttnArgs& a) {
+cs_status plan_cache_attention(const CacheAttnArgs& a, size_t& bytes) {
   CacheAttnArgs parts[2];
   size_t need = 0;
-  for (int n = plan_parts(a, parts); n--;) need = std::max(need, plan_rows(parts[n]));
-  return need;
+  for (int n = a.n_seqs && a.n_queries && a.max_queries ? plan_parts(a, parts) : 0; n--;) {
+    need = std::max(need, plan_rows(parts[n]));
+    if (!parts[n].blocks) return fail(CS_ERR_UNSUPPORTED, "cs_attention_cache: more rows and sequences than a launch takes");
+  }
+  bytes = need;
+  return CS_OK;
 }
 
 template <int NG>
@@ -877,7 +887,6 @@ static void launch_attend(const CacheAttnArgs& a, hipStream_t stream) {
 static cs_status launch_rows(CacheAttnArgs& a, void* workspace, hipStream_t stream) {
   plan_rows(a);
   const int64_t joins = a.join ? a.units * a.join_groups : 0;
-  if (!a.blocks || joins > 0x7fffffff) return fail(CS_ERR_UNSUPPORTED, "cs_attention_cache: too many rows");
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = a.part_o + (size_t)a.blocks * (size_t)a.rows * (size_t)a.shape.head_dim;
   a.share_of = reinterpret_cast<int32_t*>(a.part_ml + (size_t)a.blocks * (size_t)a.rows * 2);
