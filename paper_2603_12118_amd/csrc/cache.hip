@@ -99,8 +99,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
     const bool second = (j >= a.end0) | ((m == 1) & (j < a.lim1)), third = (j >= a.end1) | ((m == 2) & (j < a.lim2));
     const int64_t at = third ? pos[2] : second ? pos[1] : pos[0];
     const float2 cs = *reinterpret_cast<const float2*>(a.cos_sin + (at * a.half + j) * 2);
-    c[i] = turns ? cs.x : 1.f;
-    s[i] = turns ? cs.y : 0.f;
+    c[i] = cs.x;
+    s[i] = cs.y;
   }
   const int heads = a.n_heads + a.n_kv_heads, steps = (heads + HEADS - 1) / HEADS;
   for (int step = blockIdx.y; step < steps; step += a.parts) {
@@ -132,16 +132,18 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a) {
       }
     }
     if (!live) continue;
-    float u[8], v[8];
+    if (turns) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      u[i] = x[i] * c[i] - y[i] * s[i];
-      v[i] = y[i] * c[i] + x[i] * s[i];
+      for (int i = 0; i < 8; ++i) {
+        const float u = x[i] * c[i] - y[i] * s[i];
+        y[i] = y[i] * c[i] + x[i] * s[i];
+        x[i] = u;
+      }
     }
     const int64_t to = is_q ? row * a.q_out_row + (int64_t)h * a.head_dim : row * a.k_out_row + (int64_t)(h - a.n_heads) * a.head_dim;
     void* dst = is_q ? a.q_out : a.k_out;
-    store8<BF16, false>(dst, to + d0, u);
-    store8<BF16, false>(dst, to + d1, v);
+    store8<BF16, false>(dst, to + d0, x);
+    store8<BF16, false>(dst, to + d1, y);
   }
 }
 

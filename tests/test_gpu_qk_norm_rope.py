@@ -144,3 +144,29 @@ def test_no_rows():
     cs, pos = torch.from_numpy(table(4, 32)).to(DEV), torch.zeros(0, 1, dtype=torch.int32, device=DEV)
     qo, ko = B.cs_qk_norm_rope(q[:0], k[:0], cs, pos, (32,))
     assert qo.shape == (0, 4, 64) and ko.shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,sections", [(64, (16,)), (128, (8, 4, 4)), (80, (8, 16, 8)), (256, (32, 16, 16)), (48, (8,))])
+def test_values_behind_the_rotary_part_pass_alone(D, sections, dtype):
+    # whatever one of them is, an infinity or NaN, the others are not touched by it, and zeros keep their signs
+    rng = np.random.default_rng(D)
+    _, q, k = packed(rng, 4, 3, 2, D, dtype)
+    rot = 2 * sum(sections)
+    cs = torch.from_numpy(table(50, rot // 2)).to(DEV)
+    pos = torch.from_numpy(rng.integers(0, 50, (4, len(sections))).astype(np.int32)).to(DEV)
+    for x in (q, k):
+        for i, value in enumerate((float("inf"), float("-inf"), float("nan"), 3e38)):
+            x[i, 1, rot + 8] = value
+            x[i, 0, rot + 1], x[i, 0, rot + 9] = -0.0, value
+            x[i, 1, D - 1] = -0.0
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    for got, x in zip(B.cs_qk_norm_rope(q, k, cs, pos, sections), (q, k)):
+        assert torch.equal(got[..., rot:].contiguous().view(bits), x[..., rot:].contiguous().view(bits))
+        assert got[..., :rot].isfinite().all()
+    # normed by an infinite mean: zeros, and NaN where the infinity was
+    g = torch.ones(D, device=DEV)
+    for got in B.cs_qk_norm_rope(q[:2], k[:2], cs, pos[:2], sections, q_gain=g, k_gain=g):
+        want = torch.zeros_like(got)
+        want[:, 1, rot + 8], want[:, 0, rot + 9] = float("nan"), float("nan")
+        assert torch.equal(got[:, :2].isnan(), want[:, :2].isnan()) and not got[:, :2].nan_to_num().any()
