@@ -170,3 +170,42 @@ def test_values_behind_the_rotary_part_pass_alone(D, sections, dtype):
         want = torch.zeros_like(got)
         want[:, 1, rot + 8], want[:, 0, rot + 9] = float("nan"), float("nan")
         assert torch.equal(got[:, :2].isnan(), want[:, :2].isnan()) and not got[:, :2].nan_to_num().any()
+
+
+# ---- waves that take several steps of heads (a wave takes HEADS = 8 heads of 128 or 16 of 64 a step; rows beyond 2048 workgroups of
+# four share no row's heads out, and from 1024 on in fewer parts than steps): even and uneven parts, heads that end inside a step
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("T,H,K,D,sections,interleaved", [
+    (8195, 28, 4, 128, (16, 24, 24), False),              # four steps, one part
+    (4099, 40, 8, 128, (64,), False),                     # six steps, one part
+    (2731, 40, 8, 128, (24, 20, 20), True),               # six steps, two parts
+    (4093, 33, 2, 128, (10, 6, 16), False),               # five steps, two parts, the last step three heads; half of a head passes
+    (2050, 16, 16, 128, (64,), False),                    # four steps, three parts
+    (3001, 60, 10, 64, (32,), False),                     # five steps, two parts, the last step six heads
+    (4100, 9, 2, 256, (32, 48, 48), False)])              # three steps of four heads, one part
+def test_several_steps_a_wave(T, H, K, D, sections, interleaved, norm, dtype):
+    HEADS = 64 // (4 if D <= 64 else 8 if D <= 128 else 16)
+    steps, parts = -(-(H + K) // HEADS), max(1, 2048 // -(-T // 4))
+    assert steps > parts
+    rng = np.random.default_rng(T)
+    qkv, q, k = packed(rng, T, H, K, D, dtype)
+    n, half = 50, sum(sections)
+    cs, pos = table(n, half), rng.integers(0, n, (T, len(sections))).astype(np.int32)
+    gains = [(1 + 0.2 * rng.standard_normal(D)).astype(np.float32) for _ in range(2)] if norm else [None, None]
+    dg = [None if g is None else torch.from_numpy(g).to(DEV) for g in gains]
+    args = dict(q_gain=dg[0], k_gain=dg[1], eps=1e-5, interleaved=interleaved)
+    dcs, dpos = torch.from_numpy(cs).to(DEV), torch.from_numpy(pos).to(DEV)
+    before = qkv.clone()
+    qo, ko = B.cs_qk_norm_rope(q, k, dcs, dpos, sections, **args)
+    # (rows of every residue of a workgroup's four, at both ends and in between: the oracle is slow)
+    some = np.unique(np.concatenate([np.arange(40), np.arange(T // 2, T // 2 + 40), np.arange(T - 40, T)]))
+    for got, x, gain in ((qo, q, gains[0]), (ko, k, gains[1])):
+        check(got[some], x[some].double().cpu().numpy(), cs, pos[some], sections, gain, 1e-5, interleaved, dtype)
+    # ... and the rest against the same call on few rows at a time, where every wave has one step
+    for a in range(0, T, 64):
+        one = B.cs_qk_norm_rope(q[a:a + 64], k[a:a + 64], dcs, dpos[a:a + 64], sections, **args)
+        assert torch.equal(qo[a:a + 64], one[0]) and torch.equal(ko[a:a + 64], one[1])
+    assert torch.equal(qkv, before)
+    B.cs_qk_norm_rope(q, k, dcs, dpos, sections, q_out=q, k_out=k, **args)
+    assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(qkv[:, H + K:], before[:, H + K:])
