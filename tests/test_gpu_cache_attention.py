@@ -504,3 +504,122 @@ def test_workspace_of_a_mixed_batch_is_for_its_rows():
     x = B.cs_cache_batch(C.sizeof(B.cs_cache_batch), n_seqs=64, n_queries=2048 + 63, max_queries=2048, table_width=200, max_keys=8192)
     assert B.lib().cs_attention_cache_query(C.byref(c), C.byref(x), 28, C.byref(need)) == 0
     assert need.value < 128 << 20
+
+
+# ---- the kernel for blocks of 128 rows, on batches whose sequences fill such blocks: what the host says is cut to the queries there are,
+# so each test asks the plan (by its workspace, with keys enough for every share) whether that kernel runs
+LONG = 1 << 26
+
+
+def runs_blocks_of_128(b, max_queries, more_than=0):
+    import ctypes as C
+    need, T, heads = C.c_size_t(), b.q.shape[0], b.q.shape[1]
+    group, n = heads // b.kv_heads, len(b.lens)
+    c = B.cs_cache_config(C.sizeof(B.cs_cache_config), b.kv_heads, b.dim, b.page, b.dpool.shape[0])
+    x = B.cs_cache_batch(C.sizeof(B.cs_cache_batch), n_seqs=n, n_queries=T, max_queries=max_queries, table_width=b.dtable.shape[1], max_keys=LONG)
+    assert B.lib().cs_attention_cache_query(C.byref(c), C.byref(x), heads, C.byref(need)) == 0
+    seqs = min(n, T * group // (more_than + 1))
+    blocks = min(seqs * -(-max_queries * group // 128), seqs + T * group // 128) * b.kv_heads + (512 if b.dim == 128 else 768) + 64
+    return need.value == blocks * 128 * (b.dim + 2) * 4 + n * 16
+
+
+def check_lost(b, got, causal, lost):
+    """lost[b]: keys of the sequence that are in no page."""
+    at = 0
+    for (nq, n), k, v, gone in zip(b.lens, b.k, b.v, lost):
+        q = b.q[at:at + nq].double().cpu().numpy()
+        kk, vv = (np.repeat(x, q.shape[1] // b.kv_heads, 1).transpose(1, 0, 2) for x in (k, v))
+        seen = np.broadcast_to(~gone, (nq, n)) & (np.arange(n) <= np.arange(n - nq, n)[:, None] if causal else True)
+        s = np.where(seen, b.dim ** -0.5 * (q.transpose(1, 0, 2) @ kk.transpose(0, 2, 1)), -np.inf)
+        top = s.max(-1, keepdims=True)
+        p = np.where(seen, np.exp(s - np.where(np.isfinite(top), top, 0.0)), 0.0)
+        p /= np.maximum(p.sum(-1, keepdims=True), 1e-300)
+        want, weight = ((p @ x).transpose(1, 0, 2) for x in (vv, np.abs(vv)))
+        g = got[at:at + nq].double().cpu().numpy()
+        assert np.isfinite(g).all()
+        assert (np.abs(g - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -9) * weight + 2.0 ** -126).all()
+        assert not g[~seen.any(-1)].any()
+        at += nq
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 2, 64), (28, 4, 128), (6, 3, 128)])
+@pytest.mark.parametrize("page", [32, 64, 96])
+def test_full_blocks_with_pages_that_cannot_be(page, heads, kv_heads, dim):
+    b = Batch([(45, 300), (40, 128), (41, 77), (45, 3000)], heads, kv_heads, dim, page, seed=23, spare_width=0)
+    assert runs_blocks_of_128(b, 45)
+    flag = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for causal in (True, False):
+        b.check(b.run(causal=causal, max_keys=LONG, err_flag=flag), causal)
+    assert flag.item() == 0
+    pages = [-(-n // page) for _, n in b.lens]
+    beyond, first, last = b.dpool.shape[0], [0] * 4, [p - 1 for p in pages]
+    # pages of 32 are halves of a tile: the first, the second, both; the page of the last keys; all pages; some of those shared out
+    for change in ({(0, 0): -7}, {(0, 1): beyond}, {(0, 2): -1, (0, 3): beyond + 5}, {(0, last[0]): -1, (2, last[2]): beyond},
+                   {(2, p): -1 for p in range(pages[2])}, {(3, p): beyond for p in range(1, pages[3], 2)}, {(3, 0): -1, (1, 0): 1 << 30}):
+        table = b.table.copy()
+        lost = [np.zeros(n, bool) for _, n in b.lens]
+        for (s, p), bad in change.items():
+            table[s, p] = bad
+            lost[s][p * page:(p + 1) * page] = True
+        dtable = torch.from_numpy(table).to(DEV)
+        for causal in (True, False):
+            flag.zero_()
+            got = b.run(page_table=dtable, causal=causal, max_keys=LONG, err_flag=flag)
+            assert flag.item() == 1
+            check_lost(b, got, causal, lost)
+
+
+def test_full_blocks_a_query_of_nan_stays_one_and_its_own():
+    for lens in ([(70, 6000), (66, 50)], [(70, 1500), (66, 700)]):
+        b = Batch(lens, 4, 2, 64, 32, seed=24)
+        assert runs_blocks_of_128(b, 70)
+        clean = b.run(max_keys=LONG)
+        b.check(clean)
+        for at, head in ((1, 2), (69, 0), (70 + 65, 3)):
+            q = b.q.clone()
+            q[at, head, 7] = float("nan")
+            got = b.run(q=q, max_keys=LONG)
+            seen = lens[at >= 70][1] - lens[at >= 70][0] + (at - 70 if at >= 70 else at) + 1
+            assert got[at, head].isnan().all() if seen > 0 else not got[at, head].any()
+            got[at, head] = clean[at, head]
+            assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("n", [45, 64, 70, 97, 99, 1000])
+def test_full_blocks_what_lies_behind_the_last_key_does_not_matter(n):
+    b = Batch([(40, n), (40, 99)], 4, 2, 128, 64, seed=25)
+    assert runs_blocks_of_128(b, 40)
+    a = b.run(max_keys=LONG)
+    b.check(a)
+    b.check(b.run(max_keys=LONG, causal=False), causal=False)
+    for fill in (0x00, 0xff, 0x7f):
+        free = torch.ones(b.dpool.shape[0] * 64, dtype=torch.bool, device=DEV)
+        free[torch.from_numpy(b.slots).to(DEV)] = False
+        pool = b.dpool.cpu().numpy().copy()
+        for slot in np.flatnonzero(free.cpu().numpy()):
+            p, o = divmod(int(slot), 64)
+            for h in range(2):
+                for at in O.code_addresses(o, 64, 128):
+                    pool[p, h * 64 * 136 + at] = fill
+        assert torch.equal(a, b.run(pool=torch.from_numpy(pool).to(DEV), max_keys=LONG)), fill
+
+
+@pytest.mark.parametrize("count", [64, 65, 130, 1025])
+def test_full_blocks_among_many_sequences(count):
+    rng = np.random.default_rng(count)
+    lens = [(int(q), int(n)) for q, n in zip(rng.choice([0, 1, 1, 1, 2], count), rng.integers(0, 5 if count > 500 else 60, count))]
+    lens[0], lens[7], lens[count // 2], lens[count - 1] = (40, 300), (1, 1300), (33, 2500), (9, 9)
+    b = Batch(lens, 4, 2, 64, 32, seed=count)
+    assert runs_blocks_of_128(b, 40, more_than=16)            # (sequences of up to 16 rows have a launch of their own)
+    flag = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for causal in (True, False):
+        got = b.run(causal=causal, max_keys=LONG, err_flag=flag)
+        b.check(got, causal)
+        assert torch.equal(got, b.run(causal=causal, max_keys=LONG))
+    assert flag.item() == 0
+    # ... and prompts alone
+    b = Batch([(int(q), int(n)) for q, n in zip(rng.integers(33, 40, min(count, 130)), rng.integers(0, 90, min(count, 130)))], 4, 2, 64, 32, seed=count + 1)
+    most = max(q for q, _ in b.lens)
+    assert runs_blocks_of_128(b, most)
+    b.check(b.run(max_keys=LONG, err_flag=flag))
+    assert flag.item() == 0
