@@ -27,10 +27,13 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
-def _build_calls() -> None:
-    """The extension module of binding.py's hot calls: host code only, linked to the library beside it and to torch."""
+def build_calls() -> str:
+    """The extension module of binding.py's hot calls: host code only, linked to the library beside it and to torch (whose C++ headers,
+    like Python's and g++, nothing else here needs).  Without it the library's other calls run, and these say what is missing."""
     import sysconfig
     import torch
+    if os.path.exists(CALLS):                  # (one that does not compile any more is not to answer for the library of now)
+        os.remove(CALLS)
     root = os.path.dirname(torch.__file__)
     libs = os.path.join(root, "lib")
     include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), "/opt/rocm/include",
@@ -42,6 +45,7 @@ def _build_calls() -> None:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("g++ failed on calls.cpp:\n" + r.stderr)
+    return CALLS
 
 
 def build_library(verbose: bool = False) -> str:
@@ -51,9 +55,9 @@ def build_library(verbose: bool = False) -> str:
                        capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr)
-    _build_calls()
     return LIB
 
 
 if __name__ == "__main__":
     print(build_library(verbose=True))
+    print(build_calls())
