@@ -334,7 +334,8 @@ cs_status cs_qk_norm_rope(const cs_qk_config* config, const void* q, int64_t q_r
  *   e = floor(log2 amax) - 2, one more where amax >= 1.75 * 2^floor(log2 amax), kept within [-125, 125],
  * and a value becomes the nearest multiple (ties to the even code).  Every step is exact, so what a row is held as is defined
  * to the bit.  A NaN is held as 0 and an infinity as the largest finite value; both set bit 1 of *err_flag.
- * 4.25 bits a value.  Layout, with D = head_dim (64 or 128), P = page_tokens (a multiple of 32), NG = D/32: the block of
+ * 4.25 bits a value; normally distributed values are off by 11 % (rms), and attention over them by as much or more: see that
+ * the layer bears it.  Layout, with D = head_dim (64 or 128), P = page_tokens (a multiple of 32), NG = D/32: the block of
  * page p and head h starts at byte (p * n_kv_heads + h) * P * (D + 2 NG) of the pool and holds, byte offsets in it,
  *   K codes of dims d, d+1 (d even: low bits) of token o:   o D/2 + ((d % 32 / 8) NG + d / 32) 4 + d % 8 / 2
  *   V codes:  P D/2 + (o / 4) 2 D + d / (D/16) * 4 NG + o % 4 * NG + d % (D/16) / 2

@@ -4,7 +4,7 @@
 
 namespace cs {
 
-// n / d for n < 2^32 and 2 <= d <= 2^31 as a product with recip64(d)
+// n / d as a product with recip64(d), for n d < 2^64 (a slot times the tokens of a page: a pool of 2^44 slots would be a petabyte)
 inline uint64_t recip64(uint64_t d) { return ~0ull / d + 1; }
 
 // Workgroups of 256 threads that a launch may have: HIP refuses more than 2^32 - 1 threads along a dimension of the grid.

@@ -1,10 +1,12 @@
 // Queries and keys normed and rotated in one pass; the 4-bit cache written and read.
 //
 // All three are bound by memory: a few operations a value.  Every access is 16 bytes a lane, and a lane keeps its values
-// in registers from the load to the store.  What is read once, or written and not read again here, goes past the caches
-// (ONCE) where that measured faster, in loops of calls on tensors that the caches do not hold (before later steps): rotation of 16384 x 32 heads
-// of 128, bf16, loads 58.9 -> 50.9 us, stores too 55.6; values out of the cache, 65536 rows of 4 heads of 128, stores 41.1 -> 25.7; rows
-// into the cache: loads of 16384 rows of 8 heads 29.5 -> 32.0 with their reading back, so they are plain.
+// in registers from the load to the store.  Lanes of bf16 rows lie side by side; those of fp32 rows, and of values that pass
+// the rotation, 32 bytes apart or 64, so that an instruction takes part of each line and the next one the rest.
+// What is read once, or written and not read again here, goes past the caches (ONCE) where that measured faster.  Loops of calls on
+// tensors that the caches do not hold, each as it was when the choice was made: rotation of 16384 x 32 heads of 128, bf16, loads
+// 58.9 -> 50.9 us (stores too: 55.6); values out of the cache, 65536 rows of 4 heads of 128, stores 41.1 -> 25.7; rows into
+// the cache, loads of 16384 rows of 8 heads 29.5 -> 32.0 with their reading back, so they are plain.
 #include "cache.h"
 
 #include <algorithm>

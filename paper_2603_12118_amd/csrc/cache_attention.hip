@@ -6,6 +6,10 @@
 // exponential is the B operand of O^T = V^T P^T as it stands.  A code times its power of two is exact in bf16, and the
 // conversion instruction does it two codes at a time, so the cache is widened in registers between its load and the matrix
 // instruction and what crosses the memory bus is 4.25 bits a value.
+//
+// Probabilities are rounded to bf16, the type the second product takes; their sum is that of the unrounded ones, in fp32 like scores,
+// maxima, accumulators and parts.  The roundings are to nearest and independent, and cost 0.0018 .. 0.0023 of the result's norm where the
+// rounding of the result alone costs 0.0016 .. 0.0017; probabilities in two bf16 parts would double the second product.
 #include "cache.h"
 
 #include <algorithm>
@@ -322,7 +326,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 4
     next_bad = id < 0 || id >= a.shape.n_pages;
     bad |= next_bad;
     const unsigned char* block = a.pool + ((int64_t)(next_bad ? 0 : id) * a.shape.n_kv_heads + rb.h) * a.shape.head_bytes;
-    // (codes are read once: past the caches 64 sequences of 8192 keys 65.4 -> 57.4 us, ragged ones 38.6 -> 36.4)
+    // (past the caches, right for codes that one workgroup reads: 64 sequences of 8192 keys 63.9 -> 57.4 us, ragged ones 38.6 -> 36.3.  Where several
+    // blocks of rows read the same codes that costs nothing to 7 %: prompts of 500 and 1000 tokens 12.0 and 24.6 us either way, 8 x 8 drafts
+    // 21.9 -> 23.5, 32 x 8 behind 8192 keys 65.7 -> 67.5; one token of 2048 keys 10.0 -> 10.4.)
     const unsigned char* kp = block + in_page * (16 * D) + k_off;
     next.k[0] = __builtin_nontemporal_load(reinterpret_cast<const words*>(kp));
     next.k[1] = __builtin_nontemporal_load(reinterpret_cast<const words*>(kp + 2 * D));
@@ -854,7 +860,7 @@ static size_t plan_rows(CacheAttnArgs& a) {
 
 // A batch of prompts and tokens: sequences of few rows and of many have launches of their own, with one workspace in turn.  (The host knows the
 // number of queries and the most that a sequence has: half of n_seqs times that, or less, and the batch is taken for one.)  48 tokens behind 200
-// .. 8000 keys and 512 queries behind 3584: 181 us as blocks of 128 rows, the two apart 98.
+// .. 8000 keys and 512 queries behind 3584: 181 us as blocks of 128 rows, the two apart 101.
 static int plan_parts(const CacheAttnArgs& a, CacheAttnArgs (&parts)[2]) {
   const int few = a.group <= 16 ? 16 : 32;
   parts[0] = a;
