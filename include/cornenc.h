@@ -367,7 +367,8 @@ cs_status cs_cache_read(const cs_cache_config* config, const void* pool, const i
  *  q, out      dev bf16, head h of row t at [t * row + h * head_dim]; pointers and rows multiples of 16 bytes; out must not overlap q
  *  workspace   dev, 16-byte aligned, at least what cs_attention_cache_query reports; contents are scratch
  * Errors (nothing enqueued): CS_ERR_INVALID_ARG, CS_ERR_WORKSPACE, CS_ERR_UNSUPPORTED: among others, of the query too, where n_seqs, n_queries and
- * max_queries make more blocks of rows, of all key/value heads, than a grid has workgroups (2^24 - 1).
+ * max_queries make more blocks of rows, of all key/value heads, than a grid has workgroups (2^24 - 1).  No sequence, no query or max_queries == 0 is a
+ * no-op; rows of out that no sequence has are not written.
  * Scores, softmax statistics and sums are fp32; probabilities are rounded to bf16 for the second product.  Results are
  * deterministic, and do not depend on the order of pages. */
 typedef struct {
