@@ -15,6 +15,9 @@
  *                          into the LLM's input-embedding buffer
  *   cs_attention_cache     the consumer's attention over a 4-bit cache, with the calls that
  *                          fill it (cs_qk_norm_rope, cs_cache_write)
+ *   cs_norm_residual, cs_linear_packed, cs_moe
+ *                          the rest of one of the consumer's layers: norms, products with packed
+ *                          weights, experts
  *
  * The paper does not describe the inside of an encoder.  Two towers are built:
  * a Qwen2.5-VL-style vision transformer (RMSNorm, 2-D/3-D rotary, window and
@@ -387,6 +390,100 @@ cs_status cs_attention_cache_query(const cs_cache_config* config, const cs_cache
 cs_status cs_attention_cache(const cs_cache_config* config, const void* pool, const cs_cache_batch* batch, const void* q, int64_t q_row,
                              void* out, int64_t out_row, int32_t n_heads, float scale, int32_t causal, void* workspace,
                              size_t workspace_bytes, int32_t* err_flag, void* stream);
+
+/* ---- the LLM task's layer behind its attention -------------------------------------------------------------------
+ * What one of the LLM task's layers does with the attention's output: a norm before and after each block, and the block,
+ * dense or a mixture of experts, on the few rows of a decode step, on batches of them and on chunks of a prompt.
+ *
+ *   cs_norm_residual    the residual stream takes a block's output and the next block's input is normed from it
+ *   cs_weights_pack     weights laid out once, in 4 bits or bf16; cs_weights_read: the values they are held as
+ *   cs_linear_packed    a product with packed weights
+ *   cs_moe              router, experts, shared experts and their weighted sum
+ *
+ * All enqueue on `stream`, allocate nothing and wait for nothing; a recorded graph replays them on whatever the tensors hold.
+ * Rows are row-major with consecutive values; rows may lie apart where a row pitch (in elements) is passed.  Pointers
+ * and rows: multiples of 16 bytes unless said otherwise.  Results are deterministic.  A NaN or infinity stays in its row.
+ *
+ * cs_norm_residual, per row:
+ *   z = N_post(x) where post_gain is given, x otherwise;   z = z * gate where a gate is
+ *   r = residual_scale * residual + block_scale * z;       y = N_pre(r)
+ * with N(v) = v * gain / sqrt(mean(v^2) + eps) (CS_NORM_RMS) or (v - mean(v)) * gain / sqrt(var(v) + eps) (CS_NORM_LAYER), plus bias
+ * where one is given.  fp32 throughout, y from the unrounded r, one rounding each to the type of r (the residual's) and of y (x's).
+ *  config     host.  width a multiple of 8, at most 16384; gate 0 (none), 1 (one row for all) or 2 (a row each); dtype of x, gate and y,
+ *             residual_dtype of residual and r (CS_F32 or CS_BF16 each)
+ *  r may be residual and y may be x (same pointer and row), other overlaps are caller errors.
+ *  gains, biases  dev fp32 [width]; pre_gain is needed, the others may be NULL (post_bias only with post_gain)
+ * Errors (nothing enqueued): CS_ERR_INVALID_ARG, CS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op. */
+typedef enum { CS_NORM_RMS = 0, CS_NORM_LAYER = 1 } cs_norm;
+typedef struct {
+  uint32_t struct_size;
+  int32_t norm;                /* cs_norm, of both */
+  int32_t width;
+  int32_t dtype, residual_dtype;
+  int32_t gate;
+  float eps, residual_scale, block_scale;
+} cs_norm_config;
+cs_status cs_norm_residual(const cs_norm_config* config, const void* x, int64_t x_row, const void* residual, int64_t residual_row,
+                           const void* gate, int64_t gate_row, const float* post_gain, const float* post_bias, const float* pre_gain,
+                           const float* pre_bias, void* r, int64_t r_row, void* y, int64_t y_row, int64_t n_rows, void* stream);
+
+/* Packed weights: `matrices` matrices of n rows of k values, y = x W^T.  CS_WEIGHTS_BF16 holds them as bf16.  CS_WEIGHTS_E2M1 holds 32
+ * consecutive values of a row as codes of 4 bits and a shared power of two, exactly as the cache does (cs_cache_config): 4.25 bits a
+ * value, normally distributed weights off by 11 % (rms) each, so a product of them by 11 % of its norm: see that the model bears
+ * it.  A NaN is held as 0 and an infinity as the largest finite value there; both set bit 1 of *err_flag.
+ *  k a multiple of 32; the bytes (cs_weights_query) are the caller's device memory, and their layout this library's own. */
+typedef enum { CS_WEIGHTS_E2M1 = 0, CS_WEIGHTS_BF16 = 1 } cs_weights_format;
+typedef struct {
+  uint32_t struct_size;
+  int32_t format;
+  int64_t matrices;
+  int32_t n, k;
+} cs_weights_config;
+cs_status cs_weights_query(const cs_weights_config* config, size_t* bytes);      /* host-only */
+/* Row j of matrix m at w + (m * w_matrix + j * w_row) elements of `dtype` (CS_F32 or CS_BF16). */
+cs_status cs_weights_pack(const cs_weights_config* config, const void* w, int64_t w_row, int64_t w_matrix, int32_t dtype, void* packed,
+                          int32_t* err_flag, void* stream);
+cs_status cs_weights_read(const cs_weights_config* config, const void* packed, void* w, int64_t w_row, int64_t w_matrix, int32_t dtype,
+                          void* stream);
+
+/* out[t, j] = sum_k x[t, k] W[j, k] + bias[j], one matrix (config.matrices == 1).  Exact products of what the weights are held as,
+ * sums in fp32, one rounding to out_dtype.  Laid out for up to a few hundred rows and right for any number.
+ *  x    dev bf16 rows, at most 2^22 elements apart        out  dev rows of out_dtype (CS_F32 or CS_BF16); out and its rows aligned to an element
+ *  bias dev fp32 [n] or NULL, 4-byte aligned              workspace  dev, as cs_linear_packed_query reports; contents are scratch
+ * Errors (nothing enqueued): CS_ERR_INVALID_ARG, CS_ERR_WORKSPACE, CS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op. */
+cs_status cs_linear_packed_query(const cs_weights_config* config, int64_t n_rows, size_t* workspace_bytes);   /* host-only */
+cs_status cs_linear_packed(const cs_weights_config* config, const void* packed, const void* x, int64_t x_row, const float* bias, void* out,
+                           int64_t out_row, int32_t out_dtype, int64_t n_rows, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A mixture-of-experts layer.  Per row t with live[t] (all, where live is NULL):
+ *   logit[e] = x[t] . router[e]                          (fp64, so that the choice does not hang on a rounding)
+ *   score = softmax(logit) or sigmoid(logit);  the `top` experts with the largest logit (choice_bias given: score + choice_bias), the
+ *   best first, the lowest number of equal ones; a NaN is below every number
+ *   weight[i] = score of the i-th, divided by their sum where renormalise is 1, times scale
+ *   y[t] = sum_i weight[i] F_{e_i}(x[t]) + the sum of F_e(x[t]) over the shared experts e = n_experts ..
+ *   F_e(x) = D_e (silu(g) * u),  (g, u) = U_e x: rows 0 .. inter - 1 of U_e are g's, the others u's
+ * Sums in fp32; silu(g) * u is rounded to bf16 for the second product (half a step of 2^-8 each, which averages out over inter), y once.
+ * A row that is not live gets y = 0, experts -1 and weights 0, and costs its experts nothing.
+ *  config     host.  hidden and inter multiples of 32, n_experts <= 1024, top <= 32 and n_experts, top + n_shared <= 64
+ *  up, down   packed weights of n_experts + n_shared matrices [2 inter, hidden] and [hidden, inter] of config.format
+ *  x, y       dev bf16 rows, x's at most 2^17 elements apart; y must not overlap x
+ *  router     dev bf16 [n_experts, hidden];  choice_bias dev fp32 [n_experts] or NULL;  live dev uint8 [n_rows] (any alignment) or NULL
+ *  experts, weights   dev int32, fp32 [n_rows, top]
+ *  workspace  dev, as cs_moe_query reports; contents are scratch
+ * Errors (nothing enqueued): CS_ERR_INVALID_ARG, CS_ERR_WORKSPACE, CS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op. */
+typedef enum { CS_SCORE_SOFTMAX = 0, CS_SCORE_SIGMOID = 1 } cs_score;
+typedef struct {
+  uint32_t struct_size;
+  int32_t format;
+  int32_t hidden, inter;
+  int32_t n_experts, n_shared, top;
+  int32_t score, renormalise;
+  float scale;
+} cs_moe_config;
+cs_status cs_moe_query(const cs_moe_config* config, int64_t n_rows, size_t* workspace_bytes);   /* host-only */
+cs_status cs_moe(const cs_moe_config* config, const void* x, int64_t x_row, const void* router, const float* choice_bias,
+                 const uint8_t* live, const void* up, const void* down, void* y, int64_t y_row, int32_t* experts, float* weights,
+                 int64_t n_rows, void* workspace, size_t workspace_bytes, void* stream);
 
 /* cs_xchannel: the same hand-off between TWO PROCESSES on one GPU, as the paper's executors are
  * (separate processes joined by a per-GPU Sidecar, Sec. 2.1 "Data Plane"; the sender writes the tensor

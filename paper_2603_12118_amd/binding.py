@@ -18,6 +18,9 @@ LIB_PATH = os.path.join(_HERE, "libcornenc.so")
 CS_F32, CS_BF16 = 0, 1
 CS_ARCH_VIT, CS_ARCH_AUDIO, CS_ARCH_VIT_CLS = 0, 1, 2
 CS_ORDER_RASTER, CS_ORDER_MERGE_MAJOR = 0, 1
+CS_NORM_RMS, CS_NORM_LAYER = 0, 1
+CS_WEIGHTS_E2M1, CS_WEIGHTS_BF16 = 0, 1
+CS_SCORE_SOFTMAX, CS_SCORE_SIGMOID = 0, 1
 CS_SLOT_FREE, CS_SLOT_WRITING, CS_SLOT_READY = 0, 1, 2
 CS_ERR_INVALID_ARG, CS_ERR_SHAPE, CS_ERR_WORKSPACE, CS_ERR_UNSUPPORTED, CS_ERR_BUSY, CS_ERR_NO_MEMORY, CS_ERR_TIMEOUT = 1, 2, 3, 5, 8, 9, 10
 CS_XSLOT_FREE, CS_XSLOT_WRITING, CS_XSLOT_PUBLISHING, CS_XSLOT_READY, CS_XSLOT_DRAINING = 0, 1, 2, 3, 4
@@ -59,6 +62,20 @@ class cs_cache_batch(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("n_seqs", C.c_int32), ("n_queries", C.c_int64), ("max_queries", C.c_int32),
                 ("table_width", C.c_int32), ("max_keys", C.c_int64), ("cu_queries", C.c_void_p), ("n_keys", C.c_void_p),
                 ("page_table", C.c_void_p)]
+
+
+class cs_norm_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in ("norm", "width", "dtype", "residual_dtype", "gate")] + [
+        (n, C.c_float) for n in ("eps", "residual_scale", "block_scale")]
+
+
+class cs_weights_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("format", C.c_int32), ("matrices", C.c_int64), ("n", C.c_int32), ("k", C.c_int32)]
+
+
+class cs_moe_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "format", "hidden", "inter", "n_experts", "n_shared", "top", "score", "renormalise")] + [("scale", C.c_float)]
 
 
 class cs_tensor(C.Structure):
@@ -123,6 +140,15 @@ def lib() -> C.CDLL:
         L.cs_cache_read.argtypes = [cfgp, vp, vp, i64, vp, i64, vp, i64, C.c_int32, vp, vp]
         L.cs_attention_cache_query.argtypes = [cfgp, batchp, C.c_int32, C.POINTER(C.c_size_t)]
         L.cs_attention_cache.argtypes = [cfgp, vp, batchp, vp, i64, vp, i64, C.c_int32, C.c_float, C.c_int32, vp, C.c_size_t, vp, vp]
+        wp, sizep, i32 = C.POINTER(cs_weights_config), C.POINTER(C.c_size_t), C.c_int32
+        L.cs_norm_residual.argtypes = [C.POINTER(cs_norm_config), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, i64, vp]
+        L.cs_weights_query.argtypes = [wp, sizep]
+        L.cs_weights_pack.argtypes = [wp, vp, i64, i64, i32, vp, vp, vp]
+        L.cs_weights_read.argtypes = [wp, vp, vp, i64, i64, i32, vp]
+        L.cs_linear_packed_query.argtypes = [wp, i64, sizep]
+        L.cs_linear_packed.argtypes = [wp, vp, vp, i64, vp, vp, i64, i32, i64, vp, C.c_size_t, vp]
+        L.cs_moe_query.argtypes = [C.POINTER(cs_moe_config), i64, sizep]
+        L.cs_moe.argtypes = [C.POINTER(cs_moe_config), vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp, i64, vp, C.c_size_t, vp]
         L.cs_mfma_ceiling.argtypes = [vp, C.c_size_t, C.c_int32, C.c_int32, C.POINTER(C.c_double), vp]
         L.cs_encoder_step_kernel.argtypes = [vp, C.c_int32, i64, C.c_char_p, C.c_size_t]
         L.cs_encoder_batch_kernel.argtypes = [vp, C.c_int32, i64, C.c_char_p, C.c_size_t]
@@ -141,7 +167,8 @@ def lib() -> C.CDLL:
                   "cs_channel_describe", "cs_xchannel_create", "cs_xchannel_open", "cs_xchannel_acquire",
                   "cs_xchannel_publish", "cs_xchannel_wait", "cs_xchannel_forward", "cs_xchannel_release",
                   "cs_xchannel_describe", "cs_qk_norm_rope", "cs_cache_query", "cs_cache_write", "cs_cache_read",
-                  "cs_attention_cache_query", "cs_attention_cache"):
+                  "cs_attention_cache_query", "cs_attention_cache", "cs_norm_residual", "cs_weights_query", "cs_weights_pack", "cs_weights_read",
+                  "cs_linear_packed_query", "cs_linear_packed", "cs_moe_query", "cs_moe"):
             getattr(L, f).restype = C.c_int
         _lib = L
     return _lib
@@ -607,6 +634,129 @@ def cs_attention_cache(q, pool, page_table, n_keys, cu_queries, max_queries: int
                                       workspace, err_flag)
     r = _calls().attention_cache(q, pool, page_table, n_keys, cu_queries, max_queries, max_keys, n_kv_heads, page_tokens, scale, causal, out,
                                  workspace, err_flag)
+    if type(r) is int:
+        _check(r)
+    return r
+
+
+# ---- the LLM task's layer behind its attention: rows are [T, width] with consecutive values; rows may lie apart.
+_NORMS = {"rms": CS_NORM_RMS, "layer": CS_NORM_LAYER}
+_FORMATS = {"e2m1": CS_WEIGHTS_E2M1, "bf16": CS_WEIGHTS_BF16}
+_SCORES = {"softmax": CS_SCORE_SOFTMAX, "sigmoid": CS_SCORE_SIGMOID}
+
+
+def _named(table, name: str, what: str) -> int:
+    if name not in table:
+        raise ValueError(f"{what}: expected one of {', '.join(table)}, got {name!r}")
+    return table[name]
+
+
+def cs_norm_residual(x, residual, pre_gain, pre_bias=None, post_gain=None, post_bias=None, gate=None, residual_scale: float = 1.0,
+                     block_scale: float = 1.0, norm: str = "rms", eps: float = 1e-6, r=None, y=None, stream=None):
+    """r = residual_scale residual + block_scale gate N_post(x), y = N_pre(r): what a block gave (x [T, width], bf16 or fp32) goes into the
+    residual stream (its own type), and the next block's input comes out.  norm "rms" or "layer"; gains and biases fp32 [width];
+    without post_gain x is taken as it is; gate [width] or [T, width] of x's type.  Returns (r, y), new tensors unless given (residual and x
+    themselves to work in place)."""
+    if stream is not None:
+        with _on(stream):
+            return cs_norm_residual(x, residual, pre_gain, pre_bias, post_gain, post_bias, gate, residual_scale, block_scale, norm, eps, r, y)
+    got = _calls().norm_residual(x, residual, pre_gain, pre_bias, post_gain, post_bias, gate, residual_scale, block_scale,
+                                 _named(_NORMS, norm, "norm"), eps, r, y)
+    if type(got) is int:
+        _check(got)
+    return got
+
+
+class PackedWeights:
+    """Matrices [matrices, n, k] as cs_weights_pack laid them out: `data`, a uint8 tensor, in `format` "e2m1" or "bf16"."""
+
+    __slots__ = ("data", "format", "matrices", "n", "k", "call")
+
+    def __init__(self, data, format: str, matrices: int, n: int, k: int):
+        self.data, self.format, self.matrices, self.n, self.k = data, format, matrices, n, k
+        self.call = (data, _named(_FORMATS, format, "format"), matrices, n, k)
+
+
+def _weights(packed, what: str):
+    if type(packed) is not PackedWeights:
+        raise TypeError(f"{what}: expected PackedWeights, what cs_weights_pack returns")
+    return packed.call
+
+
+def cs_weights_query(format: str, n: int, k: int, matrices: int = 1) -> int:
+    """Host-only: bytes that packed weights take."""
+    c = cs_weights_config(C.sizeof(cs_weights_config), _named(_FORMATS, format, "format"), matrices, n, k)
+    size = C.c_size_t()
+    _check(lib().cs_weights_query(C.byref(c), C.byref(size)))
+    return size.value
+
+
+def cs_weights_pack(w, format: str = "e2m1", err_flag=None, stream=None) -> PackedWeights:
+    """Weights [n, k] or [matrices, n, k], bf16 or fp32, laid out once for cs_linear_packed and cs_moe: in 4 bits with a power of two for
+    each 32 values along k ("e2m1"), or in bf16."""
+    import torch
+    if stream is not None:
+        with _on(stream):
+            return cs_weights_pack(w, format, err_flag)
+    if not isinstance(w, torch.Tensor):
+        raise TypeError("w: expected a tensor")
+    w3 = w[None] if w.dim() == 2 else w
+    if w3.dim() != 3:
+        raise ValueError("w: expected [n, k] or [matrices, n, k]")
+    matrices, n, k = w3.shape
+    p = PackedWeights(torch.empty(cs_weights_query(format, n, k, matrices), dtype=torch.uint8, device=w.device), format, matrices, n, k)
+    r = _calls().weights(*p.call, w3, False, err_flag)
+    if r is not None:
+        _check(r)
+    return p
+
+
+def cs_weights_read(packed: PackedWeights, dtype=None, out=None, stream=None):
+    """The values that packed weights are held as -> [matrices, n, k] of dtype (bf16 unless given; exact in either)."""
+    import torch
+    if stream is not None:
+        with _on(stream):
+            return cs_weights_read(packed, dtype, out)
+    call = _weights(packed, "packed")
+    if out is None:
+        out = torch.empty(packed.matrices, packed.n, packed.k, dtype=torch.bfloat16 if dtype is None else dtype, device=packed.data.device)
+    elif dtype is not None and out.dtype != dtype:
+        raise ValueError("out: not of dtype")
+    r = _calls().weights(*call, out, True, None)
+    if r is not None:
+        _check(r)
+    return out
+
+
+def cs_linear_packed(x, weights: PackedWeights, bias=None, dtype=None, out=None, workspace=None, stream=None):
+    """x [T, k] bf16 times packed weights of one matrix, plus bias (fp32 [n]) -> [T, n] of dtype (bf16 unless given, or out's).  A
+    workspace of fewer bytes than needed (or None) is replaced by a new one."""
+    import torch
+    if stream is not None:
+        with _on(stream):
+            return cs_linear_packed(x, weights, bias, dtype, out, workspace)
+    if dtype is None:
+        dtype = torch.bfloat16 if out is None else out.dtype
+    code = CS_BF16 if dtype is torch.bfloat16 else CS_F32 if dtype is torch.float32 else -1
+    if code < 0:
+        raise TypeError("out must be bf16 or fp32")
+    r = _calls().linear_packed(x, *_weights(weights, "weights"), bias, code, out, workspace)
+    if type(r) is int:
+        _check(r)
+    return r
+
+
+def cs_moe(x, router, up: PackedWeights, down: PackedWeights, top: int, score: str = "softmax", renormalise: bool = True, scale: float = 1.0,
+           choice_bias=None, live=None, y=None, experts=None, weights=None, workspace=None, stream=None):
+    """A mixture-of-experts layer over x [T, hidden] bf16: router [experts, hidden] bf16, up and down packed [experts + shared, 2 inter,
+    hidden] and [experts + shared, hidden, inter]; the shared ones are every row's.  score "softmax" or "sigmoid", choice_bias fp32
+    [experts] steers the choice only, rows that are not `live` (bool [T]) are left out.  Returns (y [T, hidden] bf16, experts int32
+    [T, top], weights fp32 [T, top]), new tensors unless given; workspace as for cs_linear_packed."""
+    if stream is not None:
+        with _on(stream):
+            return cs_moe(x, router, up, down, top, score, renormalise, scale, choice_bias, live, y, experts, weights, workspace)
+    r = _calls().moe(x, router, *_weights(up, "up"), *_weights(down, "down"), top, _named(_SCORES, score, "score"), renormalise, scale, choice_bias, live, y, experts,
+                     weights, workspace)
     if type(r) is int:
         _check(r)
     return r

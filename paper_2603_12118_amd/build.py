@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcornenc.so")
 CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["api.cpp", "plan.cpp", "channel.cpp", "xchannel.cpp", "gemm.hip", "attention.hip", "elementwise.hip", "probe.hip",
-           "cache_api.cpp", "cache.hip", "cache_attention.hip"]
+           "cache_api.cpp", "cache.hip", "cache_attention.hip", "block_api.cpp", "block.hip", "packed.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
 

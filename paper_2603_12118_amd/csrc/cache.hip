@@ -8,65 +8,12 @@
 // 58.9 -> 50.9 us (stores too: 55.6); values out of the cache, 65536 rows of 4 heads of 128, stores 41.1 -> 25.7; rows into
 // the cache, loads of 16384 rows of 8 heads 29.5 -> 32.0 with their reading back, so they are plain.
 #include "cache.h"
+#include "rows.h"
 
 #include <algorithm>
 #include <type_traits>
 
 namespace cs {
-
-typedef unsigned int cu32x4 __attribute__((ext_vector_type(4)));
-typedef float cf32x2 __attribute__((ext_vector_type(2)));
-typedef float cf32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 cbf16x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ uint32_t pack2_c(float a, float b) {
-  const cf32x2 v = {a, b};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, cbf16x2));
-}
-
-template <bool ONCE, class T>
-__device__ __forceinline__ T fetch(const T* p) {
-  if constexpr (ONCE) return __builtin_nontemporal_load(p);
-  else return *p;
-}
-template <bool ONCE, class T>
-__device__ __forceinline__ void put(T v, T* p) {
-  if constexpr (ONCE) __builtin_nontemporal_store(v, p);
-  else *p = v;
-}
-// eight consecutive values of either type
-template <bool BF16, bool ONCE>
-__device__ __forceinline__ void load8(const void* base, int64_t at, float (&x)[8]) {
-  if constexpr (BF16) {
-    const cu32x4 u = fetch<ONCE>(reinterpret_cast<const cu32x4*>(static_cast<const bf16_t*>(base) + at));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-  } else {
-    const cf32x4* p = reinterpret_cast<const cf32x4*>(static_cast<const float*>(base) + at);
-    const cf32x4 a = fetch<ONCE>(p), b = fetch<ONCE>(p + 1);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = a[i];
-      x[4 + i] = b[i];
-    }
-  }
-}
-template <bool BF16, bool ONCE>
-__device__ __forceinline__ void store8(void* base, int64_t at, const float (&x)[8]) {
-  if constexpr (BF16) {
-    cu32x4 u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = pack2_c(x[2 * i], x[2 * i + 1]);
-    put<ONCE>(u, reinterpret_cast<cu32x4*>(static_cast<bf16_t*>(base) + at));
-  } else {
-    cf32x4* p = reinterpret_cast<cf32x4*>(static_cast<float*>(base) + at);
-    put<ONCE>(cf32x4{x[0], x[1], x[2], x[3]}, p);
-    put<ONCE>(cf32x4{x[4], x[5], x[6], x[7]}, p + 1);
-  }
-}
 
 // ---- norm and rotation.  A lane holds sixteen values of a head: pairs 8l .. 8l+7, both members, so that the rotation
 // needs no other lane; lanes behind the rotary part hold sixteen values that pass.  A head is LPH lanes (head_dim / 16 of
@@ -204,35 +151,6 @@ struct Place {
   static __device__ __forceinline__ int64_t v_scale(int64_t page, int o, int g) { return page * (D + NG) + (o >> 3) * (8 * NG) + g * 8 + (o & 7); }
 };
 
-// largest magnitude of the group's values as bits (NaN above infinity above every number)
-__device__ __forceinline__ uint32_t group_max_bits(const float (&x)[8]) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
-  m = max(m, (uint32_t)__shfl_xor((int)m, 1));
-  return max(m, (uint32_t)__shfl_xor((int)m, 2));
-}
-
-// Eight codes of a lane's values and the group's scale byte.  The byte: adding a quarter to the mantissa carries into the
-// exponent from 1.75 on.  The conversion instruction divides by the scale exactly, rounds to nearest even and saturates.
-__device__ __forceinline__ uint32_t quantise8(float (&x)[8], int& byte, bool& odd_values) {
-  uint32_t m = group_max_bits(x);
-  odd_values = m >= 0x7f800000u;
-  if (odd_values) {               // (the four lanes of a group take this together)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] != x[i] ? 0.f : fminf(fmaxf(x[i], -3.4028234663852886e38f), 3.4028234663852886e38f);
-    m = group_max_bits(x);
-  }
-  byte = (int)((m + 0x200000u) >> 23) - 2;
-  byte = byte < 2 ? 2 : byte > 252 ? 252 : byte;
-  const float scale = __uint_as_float((uint32_t)byte << 23);
-  uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
-}
-
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void cache_write_kernel(CacheRows a) {
   constexpr int LANES = D / 8;
@@ -266,13 +184,6 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheRows a) {
     block[Place<D>::v_scale(P, o, c >> 2)] = (unsigned char)vb;
     if ((ko || vo) && a.err) atomicOr(a.err, 2);
   }
-}
-
-__device__ __forceinline__ void values8(uint32_t w, int byte, float (&x)[8]) {
-  const float scale = __uint_as_float((uint32_t)byte << 23);
-  const cf32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
-  const cf32x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-  x[0] = p0.x; x[1] = p0.y; x[2] = p1.x; x[3] = p1.y; x[4] = p2.x; x[5] = p2.y; x[6] = p3.x; x[7] = p3.y;
 }
 
 template <bool BF16, int D>

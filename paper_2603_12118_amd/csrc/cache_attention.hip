@@ -11,6 +11,7 @@
 // maxima, accumulators and parts.  The roundings are to nearest and independent, and cost 0.0018 .. 0.0023 of the result's norm where the
 // rounding of the result alone costs 0.0016 .. 0.0017; probabilities in two bf16 parts would double the second product.
 #include "cache.h"
+#include "rows.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -32,17 +33,6 @@ __device__ __forceinline__ uint32_t pack2_k(float a, float b) {
   const af32x2 v = {a, b};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, abf16x2));
 }
-// codes 2 SEL, 2 SEL + 1 of a word, times 2^(byte - 127) where the byte is in bits 23..30 of `scale`: two bf16
-template <int SEL>
-__device__ __forceinline__ uint32_t widen2(uint32_t w, uint32_t scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, __uint_as_float(scale), SEL));
-}
-// byte B of w in bits 23..30
-template <int B>
-__device__ __forceinline__ uint32_t scale_of(uint32_t w) {
-  return (B == 3 ? w >> 1 : w << (23 - 8 * B)) & 0x7f800000u;
-}
-
 // eight values of a query, their signs turned where `sign` has the sign bits of a pair
 __device__ __forceinline__ abf16x8 load_q(const bf16_t* p, uint32_t sign) {
   au32x4 w = *reinterpret_cast<const au32x4*>(p);

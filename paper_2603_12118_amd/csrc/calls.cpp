@@ -10,6 +10,7 @@
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -263,8 +264,166 @@ PyObject* attention_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// rows [rows, width] of a given type; rows may lie apart
+Call::Rows matrix(const Call& call, const at::Tensor& x, int64_t n, int64_t width, at::ScalarType type, const char* name) {
+  if (x.dim() != 2 || x.size(0) != n || x.size(1) != width || x.scalar_type() != type || x.device() != call.device || (n > 0 && width > 1 && x.stride(1) != 1))
+    throw Value(std::string(name) + ": expected [" + std::to_string(n) + ", " + std::to_string(width) +
+                "] of its type with consecutive values, on the GPU");
+  return {x.data_ptr(), n > 1 || x.stride(0) >= width ? x.stride(0) : width};
+}
+void two(const at::Tensor& x, const char* name) {
+  if (x.dim() != 2) throw Value(std::string(name) + ": expected [rows, width]");
+}
+// a size that a configuration holds in 32 bits
+int32_t size32(int64_t v, const char* name) {
+  if (v > 0x7fffffff) throw Value(std::string(name) + ": sizes");
+  return (int32_t)v;
+}
+at::Tensor workspace_of(const Call& call, PyObject* given, size_t need, const at::Tensor& like) {
+  at::Tensor w;
+  if (!need) return w;
+  if (given != Py_None) w = tensor(given, "workspace");
+  if (!w.defined() || w.nbytes() < need) return at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+  if (w.device() != call.device || !w.is_contiguous()) throw Value("workspace: expected a contiguous tensor on the GPU");
+  return w;
+}
+
+// (x, residual, pre_gain, pre_bias, post_gain, post_bias, gate, residual_scale, block_scale, norm code, eps, r, y) -> (r, y)
+PyObject* norm_residual(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject* {
+    const at::Tensor &x = tensor(a[0], "x"), &res = tensor(a[1], "residual");
+    two(x, "x");
+    const Call call(x, "x");
+    const c10::DeviceGuard on(call.device);
+    const int64_t T = x.size(0), W = x.size(1);
+    const int code = dtype_code(x), rcode = dtype_code(res);
+    cs_norm_config c = {sizeof(cs_norm_config), number32(a[9]), size32(W, "x"), code, rcode, 0, (float)real(a[10]), (float)real(a[7]), (float)real(a[8])};
+    const auto xr = matrix(call, x, T, W, x.scalar_type(), "x"), rr = matrix(call, res, T, W, res.scalar_type(), "residual");
+    Call::Rows gate = {nullptr, 0};
+    if (a[6] != Py_None) {
+      const at::Tensor& g = tensor(a[6], "gate");
+      c.gate = g.dim() == 1 ? 1 : 2;
+      if (c.gate == 1) gate = {call.flat(g, x.scalar_type(), W, "gate"), 0};
+      else gate = matrix(call, g, T, W, x.scalar_type(), "gate");
+    }
+    void *pg = call.flat(a[2], at::kFloat, W, "pre_gain"), *pb = call.optional(a[3], at::kFloat, W, "pre_bias");
+    void *og = call.optional(a[4], at::kFloat, W, "post_gain"), *ob = call.optional(a[5], at::kFloat, W, "post_bias");
+    const at::Tensor r = a[11] == Py_None ? at::empty({T, W}, res.options()) : tensor(a[11], "r");
+    const at::Tensor y = a[12] == Py_None ? at::empty({T, W}, x.options()) : tensor(a[12], "y");
+    const auto rw = matrix(call, r, T, W, res.scalar_type(), "r"), yw = matrix(call, y, T, W, x.scalar_type(), "y");
+    const int st = cs_norm_residual(&c, xr.p, xr.row, rr.p, rr.row, gate.p, gate.row, static_cast<float*>(og), static_cast<float*>(ob),
+                                    static_cast<float*>(pg), static_cast<float*>(pb), rw.p, rw.row, yw.p, yw.row, T, call.stream());
+    if (st != CS_OK) return PyLong_FromLong(st);
+    PyObject *u = THPVariable_Wrap(r), *v = u ? THPVariable_Wrap(y) : nullptr, *both = v ? PyTuple_Pack(2, u, v) : nullptr;
+    Py_XDECREF(u);
+    Py_XDECREF(v);
+    return both;
+  });
+}
+
+// packed weights: (bytes tensor, format code, matrices, n, k) of the five arguments from `a` on
+cs_weights_config weights_of(const Call& call, PyObject* const* a, void*& p, const char* name) {
+  const cs_weights_config c = {sizeof(cs_weights_config), number32(a[1]), number(a[2]), number32(a[3]), number32(a[4])};
+  size_t bytes = 0;
+  if (cs_weights_query(&c, &bytes)) throw Value(std::string(name) + ": " + cs_last_error());
+  p = call.flat(a[0], at::kByte, (int64_t)bytes, name);
+  return c;
+}
+
+// (x, packed, format, matrices, n, k, bias, out dtype code, out, workspace) -> out
+PyObject* linear_packed(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&]() -> PyObject* {
+    const at::Tensor& x = tensor(a[0], "x");
+    two(x, "x");
+    if (x.scalar_type() != at::kBFloat16) throw Type("x must be bf16");
+    const Call call(x, "x");
+    const c10::DeviceGuard on(call.device);
+    const int64_t T = x.size(0);
+    void* packed;
+    const cs_weights_config c = weights_of(call, a + 1, packed, "weights");
+    const auto xr = matrix(call, x, T, c.k, at::kBFloat16, "x");
+    void* bias = call.optional(a[6], at::kFloat, c.n, "bias");
+    const int code = number32(a[7]);
+    const at::ScalarType type = code == CS_BF16 ? at::kBFloat16 : at::kFloat;
+    size_t need = 0;
+    if (const int st = cs_linear_packed_query(&c, T, &need)) return PyLong_FromLong(st);
+    const at::Tensor out = a[8] == Py_None ? at::empty({T, c.n}, x.options().dtype(type)) : tensor(a[8], "out");
+    const auto o = matrix(call, out, T, c.n, type, "out");
+    const at::Tensor workspace = workspace_of(call, a[9], need, x);
+    const int st = cs_linear_packed(&c, packed, xr.p, xr.row, static_cast<float*>(bias), o.p, o.row, code, T, need ? workspace.data_ptr() : nullptr, need,
+                                    call.stream());
+    if (st != CS_OK) return PyLong_FromLong(st);
+    return THPVariable_Wrap(out);
+  });
+}
+
+// (x, router, up x 5, down x 5, top, score code, renormalise, scale, choice_bias, live, y, experts, weights, workspace) -> (y, experts, weights)
+PyObject* moe(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 22, [&]() -> PyObject* {
+    const at::Tensor &x = tensor(a[0], "x"), &router = tensor(a[1], "router");
+    two(x, "x");
+    two(router, "router");
+    if (x.scalar_type() != at::kBFloat16) throw Type("x must be bf16");
+    const Call call(x, "x");
+    const c10::DeviceGuard on(call.device);
+    const int64_t T = x.size(0), H = x.size(1), E = router.size(0);
+    void *up, *down;
+    const cs_weights_config u = weights_of(call, a + 2, up, "up"), d = weights_of(call, a + 7, down, "down");
+    if (u.format != d.format || u.matrices != d.matrices || u.matrices < E || u.k != H || d.n != H || u.n != 2 * (int64_t)d.k)
+      throw Value("up, down: expected [experts, 2 inter, hidden] and [experts, hidden, inter] of one format, the router's and shared ones");
+    const int64_t top = number32(a[12]);
+    if (top <= 0 || top > E) throw Value("top: expected 1 .. experts");
+    const cs_moe_config c = {sizeof(cs_moe_config), u.format, size32(H, "x"), d.k, size32(E, "router"), (int32_t)(u.matrices - E), (int32_t)top, number32(a[13]),
+                             truth(a[14]), (float)real(a[15])};
+    const auto xr = matrix(call, x, T, H, at::kBFloat16, "x");
+    void *rp = call.flat(router, at::kBFloat16, E * H, "router"), *bias = call.optional(a[16], at::kFloat, E, "choice_bias"), *live = nullptr;
+    if (a[17] != Py_None) {
+      const at::Tensor& l = tensor(a[17], "live");
+      live = call.flat(l, l.scalar_type() == at::kByte ? at::kByte : at::kBool, T, "live");
+    }
+    size_t need = 0;
+    if (const int st = cs_moe_query(&c, T, &need)) return PyLong_FromLong(st);
+    const at::Tensor y = a[18] == Py_None ? at::empty({T, H}, x.options()) : tensor(a[18], "y");
+    const at::Tensor experts = a[19] == Py_None ? at::empty({T, top}, x.options().dtype(at::kInt)) : tensor(a[19], "experts");
+    const at::Tensor weights = a[20] == Py_None ? at::empty({T, top}, x.options().dtype(at::kFloat)) : tensor(a[20], "weights");
+    const auto yw = matrix(call, y, T, H, at::kBFloat16, "y");
+    void *ep = call.flat(experts, at::kInt, T * top, "experts"), *wp = call.flat(weights, at::kFloat, T * top, "weights");
+    const at::Tensor workspace = workspace_of(call, a[21], need, x);
+    const int st = cs_moe(&c, xr.p, xr.row, rp, static_cast<float*>(bias), static_cast<uint8_t*>(live), up, down, yw.p, yw.row, static_cast<int32_t*>(ep),
+                          static_cast<float*>(wp), T, need ? workspace.data_ptr() : nullptr, need, call.stream());
+    if (st != CS_OK) return PyLong_FromLong(st);
+    PyObject *p = THPVariable_Wrap(y), *q = p ? THPVariable_Wrap(experts) : nullptr, *r = q ? THPVariable_Wrap(weights) : nullptr;
+    PyObject* all = r ? PyTuple_Pack(3, p, q, r) : nullptr;
+    Py_XDECREF(p);
+    Py_XDECREF(q);
+    Py_XDECREF(r);
+    return all;
+  });
+}
+
+// (packed, format, matrices, n, k, w, read, err_flag) -> None: w [matrices, n, k] is packed, or filled with what is held
+PyObject* weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject* {
+    const at::Tensor& w = tensor(a[5], "w");
+    const Call call(w, "w");
+    const c10::DeviceGuard on(call.device);
+    void* packed;
+    const cs_weights_config c = weights_of(call, a, packed, "weights");
+    const int code = dtype_code(w);
+    if (w.dim() != 3 || w.size(0) != c.matrices || w.size(1) != c.n || w.size(2) != c.k || (c.k > 1 && w.stride(2) != 1) || w.stride(0) < 0)
+      throw Value("w: expected [matrices, n, k] with consecutive values");
+    const int64_t row = c.n > 1 || w.stride(1) >= c.k ? w.stride(1) : c.k;
+    void* flag = call.optional(a[7], at::kInt, 1, "err_flag");
+    const int st = truth(a[6]) ? cs_weights_read(&c, packed, w.data_ptr(), row, w.stride(0), code, call.stream())
+                               : cs_weights_pack(&c, w.data_ptr(), row, w.stride(0), code, packed, static_cast<int32_t*>(flag), call.stream());
+    Py_INCREF(Py_None);
+    return status_or(st, Py_None);
+  });
+}
+
 #define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {CALL(qk_norm_rope), CALL(cache_write), CALL(cache_read), CALL(attention_cache), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {CALL(qk_norm_rope), CALL(cache_write), CALL(cache_read), CALL(attention_cache), CALL(norm_residual), CALL(linear_packed), CALL(moe), CALL(weights),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
