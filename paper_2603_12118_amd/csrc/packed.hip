@@ -7,6 +7,7 @@
 #include "block.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.h"
 
@@ -15,6 +16,24 @@ namespace cs {
 typedef __bf16 pbf16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void plds_void;
 
+constexpr uint32_t PAST = 0x80000000u;                 // bytes a resource may address: offsets of rows and tiles are below
+#ifdef __HIP_DEVICE_COMPILE__   // (the builtins' resource type does not exist in the host pass)
+typedef __amdgpu_buffer_rsrc_t Resource;
+__device__ __forceinline__ Resource resource(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, PAST, 0x00020000); }
+// `at` a lane's, `all` every lane's: PAST puts a load behind the bound
+__device__ __forceinline__ cu32x4 fetch16(Resource r, uint32_t at, uint32_t all) { return __builtin_bit_cast(cu32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, __builtin_amdgcn_readfirstlane(all), 0)); }
+__device__ __forceinline__ uint32_t fetch4(Resource r, uint32_t at, uint32_t all) { return __builtin_amdgcn_raw_buffer_load_b32(r, at, __builtin_amdgcn_readfirstlane(all), 0); }
+__device__ __forceinline__ void fetch_lds16(Resource r, uint32_t at, uint32_t all, unsigned char* lds) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (plds_void*)(uintptr_t)lds, 16, at, __builtin_amdgcn_readfirstlane(all), 0, 0);
+}
+#else
+struct Resource {};
+__device__ Resource resource(const void* p);
+__device__ cu32x4 fetch16(Resource r, uint32_t at, uint32_t all);
+__device__ uint32_t fetch4(Resource r, uint32_t at, uint32_t all);
+__device__ void fetch_lds16(Resource r, uint32_t at, uint32_t all, unsigned char* lds);
+#endif
+
 template <int FMT>
 struct Held;                          // a block of a tile (16 rows, 128 values along k), as a lane holds it
 template <>
@@ -22,9 +41,18 @@ struct Held<CS_WEIGHTS_E2M1> {
   cu32x4 codes;
   uint32_t scales;
   __device__ __forceinline__ void load(const unsigned char* tile, int blocks, int b, int lane, int) {
-    codes = __builtin_nontemporal_load(reinterpret_cast<const cu32x4*>(tile + (int64_t)b * 1024 + lane * 16));
-    scales = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(tile + (int64_t)blocks * 1024 + b * 64 + (lane & 15) * 4));
+    codes = *reinterpret_cast<const cu32x4*>(tile + (int64_t)b * 1024 + lane * 16);
+    scales = *reinterpret_cast<const uint32_t*>(tile + (int64_t)blocks * 1024 + b * 64 + (lane & 15) * 4);
   }
+  // the same through a resource; nothing where there are no steps
+  __device__ __forceinline__ void fetch(Resource r, int blocks, int b, int lane, int steps) {
+    codes = fetch16(r, lane * 16, steps > 0 ? (uint32_t)b * 1024 : PAST);
+    scales = fetch4(r, (lane & 15) * 4, steps > 0 ? (uint32_t)blocks * 1024 + (uint32_t)b * 64 : PAST);
+  }
+  __device__ __forceinline__ pbf16x8 at(int s) const {      // s: known when compiled
+    return s == 0 ? step<0>() : s == 1 ? step<1>() : s == 2 ? step<2>() : step<3>();
+  }
+  __device__ __forceinline__ void cut(int) {}               // (codes are finite: times zeros they are zeros)
   template <int S>
   __device__ __forceinline__ pbf16x8 step() const {
     const uint32_t scale = scale_of<S>(scales), w = codes[S];
@@ -36,8 +64,19 @@ struct Held<CS_WEIGHTS_BF16> {
   cu32x4 v[4];
   __device__ __forceinline__ void load(const unsigned char* tile, int, int b, int lane, int steps) {
 #pragma unroll
+    for (int s = 0; s < 4; ++s)             // (a step that is not there: the one before, used with zeros)
+      v[s] = *reinterpret_cast<const cu32x4*>(tile + (int64_t)b * 4096 + min(s, steps - 1) * 1024 + lane * 16);
+  }
+  __device__ __forceinline__ void fetch(Resource r, int, int b, int lane, int steps) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) v[s] = fetch16(r, lane * 16, s < steps ? (uint32_t)(b * 4096 + s * 1024) : PAST);
+  }
+  __device__ __forceinline__ pbf16x8 at(int s) const { return __builtin_bit_cast(pbf16x8, v[s]); }
+  // as if the steps from `steps` on were zeros (an infinity among what stands in their place would make a NaN)
+  __device__ __forceinline__ void cut(int steps) {
+#pragma unroll
     for (int s = 0; s < 4; ++s)
-      if (s < steps) v[s] = __builtin_nontemporal_load(reinterpret_cast<const cu32x4*>(tile + (int64_t)b * 4096 + s * 1024 + lane * 16));
+      if (s >= steps) v[s] = cu32x4{0, 0, 0, 0};
   }
   template <int S>
   __device__ __forceinline__ pbf16x8 step() const { return __builtin_bit_cast(pbf16x8, v[S]); }
@@ -68,47 +107,40 @@ __device__ __forceinline__ cf32x4 mfma(pbf16x8 w, pbf16x8 x, cf32x4 c) { return 
 template <int FMT, int RT, int U>
 __device__ __forceinline__ void direct_product(cf32x4 (&acc)[RT], const unsigned char* const (&tile)[RT], int blocks, int k, int b0, int b1,
                                                const bf16_t* xl, bool live, int lane) {
-  int b = b0;
-  const int full = min(b1, k / 128);
-  for (; b + U <= full; b += U) {
+  const int last = min(4 * b1, k / 32);       // steps
+  auto group = [&](int b, auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
     Held<FMT> w[U][RT];
     cu32x4 x[U][4];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      const int bb = WHOLE ? b + u : min(b + u, b1 - 1);
 #pragma unroll
-      for (int j = 0; j < RT; ++j) w[u][j].load(tile[j], blocks, b + u, lane, 4);
+      for (int j = 0; j < RT; ++j) w[u][j].load(tile[j], blocks, bb, lane, WHOLE ? 4 : min(4, last - 4 * bb));
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         x[u][s] = cu32x4{0, 0, 0, 0};
-        if (live) x[u][s] = *reinterpret_cast<const cu32x4*>(xl + (int64_t)(b + u) * 128 + s * 32);
+        if (live && (WHOLE || 4 * (b + u) + s < last)) x[u][s] = *reinterpret_cast<const cu32x4*>(xl + (int64_t)(b + u) * 128 + s * 32);
       }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      if constexpr (!WHOLE) {
+#pragma unroll
+        for (int j = 0; j < RT; ++j) w[u][j].cut(last - 4 * (b + u));
+      }
       all_steps([&](auto t) {
         constexpr int S = decltype(t)::value;
 #pragma unroll
         for (int j = 0; j < RT; ++j) acc[j] = mfma(w[u][j].template step<S>(), __builtin_bit_cast(pbf16x8, x[u][S]), acc[j]);
       });
-  }
-  for (; b < b1; ++b) {
-    const int steps = min(4, (k - 128 * b) / 32);
-    Held<FMT> w[RT];
-    cu32x4 x[4];
-#pragma unroll
-    for (int j = 0; j < RT; ++j) w[j].load(tile[j], blocks, b, lane, steps);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      x[s] = cu32x4{0, 0, 0, 0};
-      if (live && s < steps) x[s] = *reinterpret_cast<const cu32x4*>(xl + (int64_t)b * 128 + s * 32);
     }
-    each_step(steps, [&](auto t) {
-      constexpr int S = decltype(t)::value;
-#pragma unroll
-      for (int j = 0; j < RT; ++j) acc[j] = mfma(w[j].template step<S>(), __builtin_bit_cast(pbf16x8, x[S]), acc[j]);
-    });
-  }
+  };
+  int b = b0;
+  for (; 4 * (b + U) <= last; b += U) group(b, std::true_type());
+  if (b < b1) group(b, std::false_type());
 }
 
 // four neighbouring columns of a row; `whole`: all of them are there and the place is aligned to them
@@ -160,7 +192,7 @@ __global__ __launch_bounds__(1024) void linear_direct_kernel(LinearArgs a, int w
 #pragma unroll
   for (int j = 0; j < RT; ++j) acc[j] = cf32x4{0.f, 0.f, 0.f, 0.f};
   const int b0 = (int)((int64_t)a.shape.blocks * wave / waves), b1 = (int)((int64_t)a.shape.blocks * (wave + 1) / waves);
-  direct_product<FMT, RT, FMT == CS_WEIGHTS_E2M1 ? 4 / RT : 2 / RT>(acc, tile, a.shape.blocks, a.shape.k, b0, b1, a.x + (live ? t : 0) * a.x_row + 8 * g, live, lane);
+  direct_product<FMT, RT, 2>(acc, tile, a.shape.blocks, a.shape.k, b0, b1, a.x + (live ? t : 0) * a.x_row + 8 * g, live, lane);
 #pragma unroll
   for (int j = 0; j < RT; ++j) part[wave][j][lane] = acc[j];
   __syncthreads();
@@ -171,97 +203,162 @@ __global__ __launch_bounds__(1024) void linear_direct_kernel(LinearArgs a, int w
   if (live && left > 0) store4<BF16>(a.out, t * a.out_row + n, v + bias4(a.bias, n, a.shape.n), left, whole_rows && left >= 4);
 }
 
-// ---- more rows: four waves share the rows' operands in LDS, chunks of NB blocks along k, each asked for while the one before is used,
-// and each wave has RT tiles of the weights (and, WM > 1, every WM-th part of the rows).  A chunk's rows lie as the lanes take them: piece (tile of 16
-// rows, step) is 1 KB in lane order, written and read without conflicts.
-template <int FMT, int MT, int WM, int RT, int NB>
+// One row: a wave's part of it waits in LDS as the lanes take it, 16 bytes for each quarter, the same for all 16 columns of the product (of which one
+// is used): no lane is masked and no operand cleared.  A wave writes and reads its own part only.
+template <int FMT, bool BF16>
+__global__ __launch_bounds__(1024) void linear_row_kernel(LinearArgs a, int whole_rows) {
+  constexpr int U = FMT == CS_WEIGHTS_E2M1 ? 4 : 2;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  __shared__ cf32x4 part[16][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, g = lane >> 4;
+  const unsigned char* tile = a.packed + (int64_t)blockIdx.x * a.shape.tile_bytes;
+  const int blocks = a.shape.blocks, b0 = (int)((int64_t)blocks * wave / waves), b1 = (int)((int64_t)blocks * (wave + 1) / waves);
+  for (int c = 16 * b0 + lane; c < 16 * b1; c += 64) {       // (asked for ahead of the weights: loads come back in order)
+    cu32x4 v = {0, 0, 0, 0};
+    if (8 * c < a.shape.k) v = *reinterpret_cast<const cu32x4*>(a.x + 8 * c);
+    *reinterpret_cast<cu32x4*>(lds + 16 * c) = v;
+  }
+  cf32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  const int last = a.shape.k / 32;
+  for (int b = b0; b < b1; b += U) {
+    Held<FMT> w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int bb = min(b + u, b1 - 1);
+      w[u].load(tile, blocks, bb, lane, min(4, last - 4 * bb));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (b + u < b1) {
+        w[u].cut(last - 4 * (b + u));
+        all_steps([&](auto t) {
+          constexpr int S = decltype(t)::value;
+          acc = mfma(w[u].template step<S>(), *reinterpret_cast<const pbf16x8*>(lds + (b + u) * 256 + S * 64 + g * 16), acc);
+        });
+      }
+  }
+  part[wave][lane] = acc;
+  __syncthreads();
+  if (wave) return;
+  for (int w = 1; w < waves; ++w) acc += part[w][lane];
+  const int n = blockIdx.x * 16 + 4 * g, left = a.shape.n - n;
+  if ((lane & 15) == 0 && left > 0) store4<BF16>(a.out, n, acc + bias4(a.bias, n, a.shape.n), left, whole_rows && left >= 4);
+}
+
+// ---- more rows: four waves share the rows' operands in LDS, and each wave has RT tiles of the weights (and, WM > 1, every WM-th part of
+// the rows).  The rows come in stages of SS steps, NS of them in turn: while one is used, NS - 1 are on their way; the weights, which come from
+// farther, are asked for WD blocks ahead, into registers.  A piece (step, tile of 16 rows) is 1 KB, 64 bytes a row, and neighbouring lanes ask for
+// neighbouring 16 bytes of a row (lanes that ask for different rows take an address each: 16 bytes a clock, not 64).  The four
+// chunks of row t lie turned by t / 4, so that the 16 rows of a chunk are read from different banks.
+// Both are buffer loads with a bound: what lies behind the last step is asked for behind the bound, and is zeros that cost no memory.  So
+// the number of loads under way is always the same, the waits are constants, and no step of the loop is conditional.
+template <int FMT, int MT, int WM, int RT, int SS, int NS, int WD>
 struct Staged {
   static constexpr int MTW = MT / WM;                  // tiles of rows of a wave
-  static constexpr int UNITS = MT * NB * 4;            // pieces of a chunk
-  static constexpr int PER_WAVE = (UNITS + 3) / 4;
-  static constexpr int LDS = 2 * UNITS * 1024;
-
-  // off: the lane's byte offset from x of (row, 8 (lane / 16)) in tile m of its turn; loads of chunk c
-  template <class Off>
-  static __device__ __forceinline__ void stage(const bf16_t* x, Off&& off, int c, int last_step, unsigned char* lds, int wave) {
-#ifdef __HIP_DEVICE_COMPILE__   // (the builtin's resource type does not exist in the host pass)
-    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(x), 0, 0xFFFFFFFFu, 0x00020000);
-#pragma unroll
-    for (int i = 0; i < PER_WAVE; ++i) {
-      const int u = i * 4 + wave;                      // step u / MT of the chunk, tile u % MT
-      const int step = c * NB * 4 + u / MT;
-      if (u < UNITS && step < last_step)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (plds_void*)(uintptr_t)(lds + u * 1024), 16, off(u % MT) + (uint32_t)step * 64, 0, 0, 0);
-    }
-#endif
-  }
+  static constexpr int UNITS = MT * SS;                // pieces of a stage
+  static constexpr int XL = (UNITS + 3) / 4;           // loads of a wave for a stage (a wave without a piece fetches one again)
+  static constexpr int WL = RT * (FMT == CS_WEIGHTS_E2M1 ? 2 : 4);
+  static constexpr int PB = 4 / SS;                    // stages of a block
+  static_assert((SS == 2 || SS == 4) && WD <= 3, "what the loop is written for");
+  static constexpr int LDS = NS * UNITS * 1024;
 
   // acc[j][m] += blocks [b0, b1) of tile[j] times tile m of the wave's rows.  All waves of the workgroup call it alike.
+  // off(m): the byte offset from x of row lane / 4 of tile m.
   template <class Off>
   static __device__ __forceinline__ void product(cf32x4 (&acc)[RT][MTW], const unsigned char* const (&tile)[RT], int blocks, int k, int b0, int b1,
                                                  const bf16_t* x, Off&& off, unsigned char* lds, int lane, int wave, int wm) {
-    const int chunks = (b1 - b0 + NB - 1) / NB, last_step = min(4 * b1, k / 32);
-    const int c_full = (last_step / 4 - b0) / NB;      // chunks that have all their steps
-    Held<FMT> cur[RT][NB], next[RT][NB];
-    auto weights = [&](Held<FMT> (&w)[RT][NB], int c) {
+    const int last = min(4 * b1, k / 32);              // steps
+    const Resource rx = resource(x);
+    Resource rw[RT];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int b = b0 + c * NB + i;
-        if (b < b1) {
-          const int steps = min(4, k / 32 - 4 * b);
+    for (int j = 0; j < RT; ++j) rw[j] = resource(tile[j]);
+    uint32_t offs[XL];
+    int place[XL];
 #pragma unroll
-          for (int j = 0; j < RT; ++j) w[j][i].load(tile[j], blocks, b, lane, steps);
-        }
+    for (int i = 0; i < XL; ++i) {
+      int u = i * 4 + wave;                            // step u / MT of the stage, tile u % MT
+      u = u < UNITS ? u : UNITS - 1;
+      offs[i] = off(u % MT) + (((lane & 3) ^ (lane >> 4)) << 4);
+      place[i] = u;
+    }
+    auto stage = [&](int first, int slot) {            // the stage from step `first` on, into the slot
+#pragma unroll
+      for (int i = 0; i < XL; ++i) {
+        const int step = first + place[i] / MT;
+        fetch_lds16(rx, offs[i], step < last ? (uint32_t)step * 64 : PAST, lds + (slot * UNITS + place[i]) * 1024);
       }
     };
-    // (pieces count steps from b0)
-    const bf16_t* xs = x + (int64_t)b0 * 128;
-    const int steps_here = last_step - 4 * b0;
-    if (chunks > 0) {
-      stage(xs, off, 0, steps_here, lds, wave);
-      weights(cur, 0);
-    }
-    for (int c = 0; c < chunks; ++c) {
-      const unsigned char* from = lds + (c & 1) * UNITS * 1024 + wm * MTW * 1024 + lane * 16;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's pieces of the chunk, and its weights
-      __syncthreads();                                   // everyone's; and nobody reads the other half any more
-      if (c + 1 < chunks) {
-        stage(xs, off, c + 1, steps_here, lds + (~c & 1) * UNITS * 1024, wave);
-        weights(next, c + 1);
-      }
-      auto use = [&](int i, auto t) {
-        constexpr int S = decltype(t)::value;
-        pbf16x8 f[MTW];
+    Held<FMT> w[WD + 1][RT];
+    auto weights = [&](Held<FMT> (&h)[RT], int b) {
 #pragma unroll
-        for (int m = 0; m < MTW; ++m) f[m] = *reinterpret_cast<const pbf16x8*>(from + ((i * 4 + S) * MT + m) * 1024);
+      for (int j = 0; j < RT; ++j) h[j].fetch(rw[j], blocks, b, lane, b < b1 ? last - 4 * b : 0);
+    };
 #pragma unroll
-        for (int j = 0; j < RT; ++j) {
-          const pbf16x8 w = cur[j][i].template step<S>();
+    for (int i = 0; i < WD; ++i) weights(w[i], b0 + i);
 #pragma unroll
-          for (int m = 0; m < MTW; ++m) acc[j][m] = mfma(w, f[m], acc[j][m]);
+    for (int i = 0; i < NS - 1; ++i) stage(4 * b0 + i * SS, i);
+    __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): all of them, so that the first turns' waits, which count more loads behind, are enough
+    int slot = 0, b = b0;
+    const unsigned char* mine = lds + wm * MTW * 1024 + (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) << 4);
+    auto block = [&](auto turn) {
+      constexpr int R = decltype(turn)::value;
+#pragma unroll
+      for (int i = 0; i < PB; ++i) {
+        wait_for_stage(i);
+        __builtin_amdgcn_s_barrier();                  // everyone's pieces are there, and nobody reads the slot before this one any more
+        asm volatile("" ::: "memory");
+        stage(4 * b + (i + NS - 1) * SS, slot == 0 ? NS - 1 : slot - 1);
+        __builtin_amdgcn_sched_barrier(0);             // (the waits count the weights behind the rows)
+        if (i == 0) weights(w[(R + WD) % (WD + 1)], b + WD);
+        const unsigned char* from = mine + slot * (UNITS * 1024);
+        pbf16x8 f[2][MTW];
+#pragma unroll
+        for (int m = 0; m < MTW; ++m) f[0][m] = *reinterpret_cast<const pbf16x8*>(from + m * 1024);
+#pragma unroll
+        for (int t = 0; t < SS; ++t) {
+          if (t + 1 < SS) {
+#pragma unroll
+            for (int m = 0; m < MTW; ++m) f[(t + 1) & 1][m] = *reinterpret_cast<const pbf16x8*>(from + ((t + 1) * MT + m) * 1024);
+          }
+#pragma unroll
+          for (int j = 0; j < RT; ++j) {
+            const pbf16x8 v = w[R][j].at(i * SS + t);
+#pragma unroll
+            for (int m = 0; m < MTW; ++m) acc[j][m] = mfma(v, f[t & 1][m], acc[j][m]);
+          }
+          __builtin_amdgcn_sched_barrier(0);           // (a step's operands are widened in it, not all at once ahead: registers)
         }
-      };
-      if (c < c_full) {
-#pragma unroll
-        for (int i = 0; i < NB; ++i) all_steps([&](auto t) { use(i, t); });
-      } else {
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-          const int steps = min(4, steps_here - (c * NB + i) * 4);
-          if (steps > 0) each_step(steps, [&](auto t) { use(i, t); });
-        }
+        slot = slot + 1 == NS ? 0 : slot + 1;
       }
-#pragma unroll
-      for (int j = 0; j < RT; ++j)
-#pragma unroll
-        for (int i = 0; i < NB; ++i) cur[j][i] = next[j][i];
+      ++b;
+    };
+    while (b < b1) {                                    // (whole turns: a block behind the last one is zeros; an exit in between costs registers)
+      block(step_tag<0>());
+      if constexpr (WD >= 1) block(step_tag<1>());
+      if constexpr (WD >= 2) block(step_tag<2>());
+      if constexpr (WD >= 3) block(step_tag<3>());
     }
+    // (the loads still under way write into LDS: they end before the workgroup's memory is another's, or is used again)
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+  }
+
+  // vmcnt and lgkmcnt(0): this wave's pieces of the stage have come, and what it read of the one before
+  static __device__ __forceinline__ void wait_for_stage(int i) {
+    // weights are asked for in a block's first stage, behind the rows of NS - 1 stages on
+    constexpr auto behind = [](int at) {
+      int n = (NS - 2) * XL;
+      for (int s = 1; s < NS; ++s) n += ((at - s) % PB + PB) % PB == 0 ? WL : 0;
+      return n < 63 ? n : 63;
+    };
+    constexpr auto code = [](int n) { return (n & 15) | (n >> 4) << 14 | 7 << 4; };
+    if (PB == 1 || i == 0) __builtin_amdgcn_s_waitcnt(code(behind(0)));
+    else __builtin_amdgcn_s_waitcnt(code(behind(1)));
   }
 };
 
-template <int FMT, int OUT, int MT, int WM, int RT, int NB>      // OUT: 0 fp32, 1 bf16, 2 a part of the sums
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) void linear_staged_kernel(LinearArgs a, int whole_rows) {
-  typedef Staged<FMT, MT, WM, RT, NB> P;
+template <int FMT, int OUT, int MT, int WM, int RT, int SS, int NS, int WD>      // OUT: 0 fp32, 1 bf16, 2 a part of the sums
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT * MT / WM >= 32 ? 1 : 2, 8))) void linear_staged_kernel(LinearArgs a, int whole_rows) {
+  typedef Staged<FMT, MT, WM, RT, SS, NS, WD> P;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
   const int t = lane & 15, g = lane >> 4;
@@ -276,7 +373,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
   for (int j = 0; j < RT; ++j) tile[j] = a.packed + (int64_t)min(tile0 + j, a.shape.tiles - 1) * a.shape.tile_bytes;
   const bf16_t* x = a.x + m0 * a.x_row;
   const int rows = (int)min((int64_t)(MT * 16), a.n_rows - m0);
-  auto off = [&](int m) { return (uint32_t)((int64_t)min(m * 16 + t, rows - 1) * a.x_row * 2) + 16 * g; };
+  auto off = [&](int m) { return (uint32_t)((int64_t)min(m * 16 + (lane >> 2), rows - 1) * a.x_row * 2); };
   cf32x4 acc[RT][P::MTW];
 #pragma unroll
   for (int j = 0; j < RT; ++j)
@@ -298,17 +395,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
   }
 }
 
-// out = the sum of the parts, in their order, and the bias
-template <bool BF16>
-__global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs a) {
-  const int64_t total = a.n_rows * a.shape.n;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = i / a.shape.n, n = i - t * a.shape.n;
-    float v = a.parts[i];
-    for (int s = 1; s < a.splits; ++s) v += a.parts[s * total + i];
-    if (a.bias) v += a.bias[n];
-    if constexpr (BF16) static_cast<bf16_t*>(a.out)[t * a.out_row + n] = (bf16_t)pack2_c(v, v);
-    else static_cast<float*>(a.out)[t * a.out_row + n] = v;
+// out = the sum of the parts, in their order, and the bias; V columns a thread, up to eight parts asked for together
+template <bool BF16, int V>
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs a, int whole_rows) {
+  const int64_t total = a.n_rows * a.shape.n, t = blockIdx.x;
+  const int n = ((int)blockIdx.y * 256 + threadIdx.x) * V;
+  if (n >= a.shape.n) return;
+  const float* from = a.parts + t * a.shape.n + n;
+  typedef float part_t __attribute__((ext_vector_type(V)));
+  part_t v = {};
+  for (int s0 = 0; s0 < a.splits; s0 += 8) {
+    part_t p[8] = {};
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      if (s0 + s < a.splits) p[s] = *reinterpret_cast<const part_t*>(from + (s0 + s) * total);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) v += p[s];
+  }
+  if constexpr (V == 4) {
+    store4<BF16>(a.out, t * a.out_row + n, v + bias4(a.bias, n, a.shape.n), 4, whole_rows);
+  } else {
+    const float x = v[0] + (a.bias ? a.bias[n] : 0.f);
+    if constexpr (BF16) static_cast<bf16_t*>(a.out)[t * a.out_row + n] = (bf16_t)pack2_c(x, x);
+    else static_cast<float*>(a.out)[t * a.out_row + n] = x;
   }
 }
 
@@ -317,26 +426,24 @@ namespace {
 constexpr int DIRECT_ROWS = 16;
 
 struct LinearPlan {
-  int mt, m_tiles, n_cols, splits, blocks_of_split;
+  int mt, m_tiles, splits, blocks_of_split;
 };
 LinearPlan linear_plan(const LinearArgs& a) {
   LinearPlan p = {};
-  p.mt = a.n_rows <= 32 ? 2 : a.n_rows <= 64 ? 4 : 8;
+  p.mt = a.n_rows <= 32 ? 2 : a.n_rows <= 48 ? 3 : a.n_rows <= 64 ? 4 : 8;
   p.m_tiles = (int)((a.n_rows + p.mt * 16 - 1) / (p.mt * 16));
-  p.n_cols = p.mt == 8 && a.shape.format == CS_WEIGHTS_BF16 ? 64 : 128;
-  const int64_t groups = (int64_t)p.m_tiles * ((a.shape.n + p.n_cols - 1) / p.n_cols);
-  // workgroups that fill the chip twice, unless a part would have fewer than eight blocks
-  const int64_t want = std::max<int64_t>(1, (512 + groups / 2) / groups);
-  p.splits = (int)std::min<int64_t>({want, std::max(1, a.shape.blocks / 8), 32});
-  p.blocks_of_split = (a.shape.blocks + p.splits - 1) / p.splits;
-  p.splits = (a.shape.blocks + p.blocks_of_split - 1) / p.blocks_of_split;
+  const int64_t groups = (int64_t)p.m_tiles * ((a.shape.n + 127) / 128);
+  // a workgroup for each CU, in whole turns of four blocks
+  const int want = (int)std::max<int64_t>(1, 256 / groups), blocks = a.shape.blocks;
+  p.blocks_of_split = std::min(blocks, ((blocks + want - 1) / want + 3) / 4 * 4);
+  p.splits = (blocks + p.blocks_of_split - 1) / p.blocks_of_split;
   return p;
 }
 
-template <int FMT, int OUT, int MT, int WM, int RT, int NB>
+template <int FMT, int OUT, int MT, int WM, int RT, int SS, int NS, int WD>
 cs_status run_staged(const LinearArgs& a, int whole_rows, hipStream_t s) {
-  constexpr int LDS = Staged<FMT, MT, WM, RT, NB>::LDS;
-  const auto kernel = linear_staged_kernel<FMT, OUT, MT, WM, RT, NB>;
+  constexpr int LDS = Staged<FMT, MT, WM, RT, SS, NS, WD>::LDS;
+  const auto kernel = linear_staged_kernel<FMT, OUT, MT, WM, RT, SS, NS, WD>;
   if (LDS > 65536) CS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
   const int cols = (4 / WM) * RT * 16;
   const int64_t n_blocks = (a.shape.n + cols - 1) / cols, grid = (n_blocks + 7) / 8 * 8 * a.m_tiles;
@@ -346,24 +453,37 @@ cs_status run_staged(const LinearArgs& a, int whole_rows, hipStream_t s) {
 }
 template <int FMT, int OUT>
 cs_status run_rows(const LinearArgs& a, int mt, int whole_rows, hipStream_t s) {
-  if (mt == 2) return run_staged<FMT, OUT, 2, 1, 2, FMT == CS_WEIGHTS_E2M1 ? 4 : 2>(a, whole_rows, s);
-  if (mt == 4) return run_staged<FMT, OUT, 4, 1, 2, FMT == CS_WEIGHTS_E2M1 ? 2 : 1>(a, whole_rows, s);
-  // (bf16 weights of four tiles, this chunk's and the next one's, do not fit the registers)
-  return run_staged<FMT, OUT, 8, 2, FMT == CS_WEIGHTS_E2M1 ? 4 : 2, 1>(a, whole_rows, s);
+  constexpr int WD = FMT == CS_WEIGHTS_E2M1 ? 3 : 1;         // (bf16 weights are four times the registers)
+  if (mt == 2) return run_staged<FMT, OUT, 2, 1, 2, 4, 4, WD>(a, whole_rows, s);
+  if (mt == 3) return run_staged<FMT, OUT, 3, 1, 2, 4, 4, WD>(a, whole_rows, s);
+  if (mt == 4) return run_staged<FMT, OUT, 4, 1, 2, 2, 6, WD>(a, whole_rows, s);
+  return run_staged<FMT, OUT, 8, 1, 2, 2, 4, 1>(a, whole_rows, s);
+}
+// Up to 16 rows.  Waves of about four blocks each; tiles of a workgroup: as many (rows of x are then read once for all of them) as leave
+// workgroups for the chip.
+template <int FMT, bool BF16>
+cs_status run_direct(const LinearArgs& a, int whole_rows, hipStream_t s) {
+  const int tiles = a.shape.tiles, blocks = a.shape.blocks;
+  const bool few = tiles < 1024;
+  const int waves = std::min({16, blocks, (blocks + 3) / 4});
+  if (a.n_rows == 1 && blocks <= 160) {                      // (40 KB of LDS for the row, beside 16)
+    hipLaunchKernelGGL((linear_row_kernel<FMT, BF16>), dim3(tiles), dim3(64 * waves), (size_t)blocks * 256, s, a, whole_rows);
+  } else if (FMT == CS_WEIGHTS_E2M1 && tiles >= 256) {
+    constexpr int MANY = FMT == CS_WEIGHTS_E2M1 ? 4 : 1, SOME = FMT == CS_WEIGHTS_E2M1 ? 2 : 1;
+    if (few) hipLaunchKernelGGL((linear_direct_kernel<FMT, BF16, SOME>), dim3((tiles + 1) / 2), dim3(64 * waves), 0, s, a, whole_rows);
+    else hipLaunchKernelGGL((linear_direct_kernel<FMT, BF16, MANY>), dim3((tiles + 3) / 4), dim3(64 * waves), 0, s, a, whole_rows);
+  } else {
+    hipLaunchKernelGGL((linear_direct_kernel<FMT, BF16, 1>), dim3(tiles), dim3(64 * waves), 0, s, a, whole_rows);
+  }
+  CS_HIP(hipGetLastError());
+  return CS_OK;
 }
 template <int FMT>
 cs_status run_linear(LinearArgs a, int out_dtype, void* workspace, hipStream_t s) {
   const bool bf16 = out_dtype == CS_BF16;
   const int size = bf16 ? 2 : 4;
   const int whole = ((reinterpret_cast<uintptr_t>(a.out) | (uint64_t)(a.out_row * size)) & (4 * size - 1)) == 0;
-  if (a.n_rows <= DIRECT_ROWS) {
-    // waves that fill the chip: of the tiles' blocks, so many a workgroup
-    const int tiles = a.shape.tiles, waves = (int)std::min<int64_t>({16, a.shape.blocks, std::max<int64_t>(1, (4096 + tiles / 2) / tiles)});
-    if (bf16) hipLaunchKernelGGL((linear_direct_kernel<FMT, true, 1>), dim3(tiles), dim3(64 * waves), 0, s, a, whole);
-    else hipLaunchKernelGGL((linear_direct_kernel<FMT, false, 1>), dim3(tiles), dim3(64 * waves), 0, s, a, whole);
-    CS_HIP(hipGetLastError());
-    return CS_OK;
-  }
+  if (a.n_rows <= DIRECT_ROWS) return bf16 ? run_direct<FMT, true>(a, whole, s) : run_direct<FMT, false>(a, whole, s);
   const LinearPlan p = linear_plan(a);
   a.m_tiles = p.m_tiles;
   a.splits = p.splits;
@@ -371,9 +491,12 @@ cs_status run_linear(LinearArgs a, int out_dtype, void* workspace, hipStream_t s
   a.parts = static_cast<float*>(workspace);
   if (p.splits == 1) return bf16 ? run_rows<FMT, 1>(a, p.mt, whole, s) : run_rows<FMT, 0>(a, p.mt, whole, s);
   if (cs_status st = run_rows<FMT, 2>(a, p.mt, whole, s)) return st;
-  const unsigned groups = (unsigned)std::min<int64_t>((a.n_rows * a.shape.n + 255) / 256, 4096);
-  if (bf16) hipLaunchKernelGGL((linear_join_kernel<true>), dim3(groups), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((linear_join_kernel<false>), dim3(groups), dim3(256), 0, s, a);
+  const bool four = a.shape.n % 4 == 0;
+  const dim3 groups((unsigned)a.n_rows, (unsigned)((a.shape.n + (four ? 1023 : 255)) / (four ? 1024 : 256)));
+  if (four && bf16) hipLaunchKernelGGL((linear_join_kernel<true, 4>), groups, dim3(256), 0, s, a, whole);
+  else if (four) hipLaunchKernelGGL((linear_join_kernel<false, 4>), groups, dim3(256), 0, s, a, whole);
+  else if (bf16) hipLaunchKernelGGL((linear_join_kernel<true, 1>), groups, dim3(256), 0, s, a, whole);
+  else hipLaunchKernelGGL((linear_join_kernel<false, 1>), groups, dim3(256), 0, s, a, whole);
   CS_HIP(hipGetLastError());
   return CS_OK;
 }
@@ -394,54 +517,100 @@ cs_status launch_linear_packed(const LinearArgs& a, int out_dtype, void* workspa
 
 // ---- the mixture of experts
 
+// Numbers between the experts' counts: a line each, since the adds to one line go one behind the other
+constexpr int COUNT_APART = 16;
+
 // Scores of TT rows by EE experts a wave, in fp64: products of two bf16 numbers are exact there and their sum is off by less than any two
 // experts' scores that are not equal are likely to lie apart, so that the choice is that of the definition.  The vector unit's fp64 rate is half its
 // fp32 rate.  Also clears the experts' counts for the launch behind.
-template <int TT, int EE>
+// v of the lanes of a wave, summed: within rows of 16 by DPP, whose every step gives both sides the same sum
+__device__ __forceinline__ double wave_sum(double v) {
+  auto with = [](double x, auto ctrl) {
+    constexpr int C = decltype(ctrl)::value;
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), C, 0xf, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, __double2hiint(x), C, 0xf, 0xf, false);
+    return x + __hiloint2double(hi, lo);
+  };
+  v = with(v, std::integral_constant<int, 0xb1>());      // lanes 1 0 3 2
+  v = with(v, std::integral_constant<int, 0x4e>());      // lanes 2 3 0 1
+  v = with(v, std::integral_constant<int, 0x141>());     // half a row mirrored
+  v = with(v, std::integral_constant<int, 0x140>());     // a row mirrored
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// A workgroup takes an expert and TT rows, its waves pieces of 512 values of k in turn.
+template <int TT>
 __global__ __launch_bounds__(256) void moe_logits_kernel(MoeArgs a) {
-  if (blockIdx.x == 0 && blockIdx.y == 0)
-    for (int e = threadIdx.x; e < a.experts + a.shared; e += 256) a.counts[e] = 0;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int e0 = ((int)blockIdx.x * 4 + wave) * EE;
+  __shared__ double part[4][TT];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = blockIdx.x;
   const int64_t t0 = (int64_t)blockIdx.y * TT;
-  if (e0 >= a.experts) return;
-  const bf16_t *x[TT], *w[EE];
+  if (e == 0 && blockIdx.y == 0)
+    for (int i = threadIdx.x; i < a.experts + a.shared; i += 256) a.counts[i * COUNT_APART] = 0;
+  const bf16_t *x[TT], *w = a.router + (int64_t)e * a.hidden;
 #pragma unroll
   for (int i = 0; i < TT; ++i) x[i] = a.x + min(t0 + i, a.n_rows - 1) * a.x_row;
-#pragma unroll
-  for (int i = 0; i < EE; ++i) w[i] = a.router + (int64_t)min(e0 + i, a.experts - 1) * a.hidden;
-  double sum[TT][EE];
-#pragma unroll
-  for (int i = 0; i < TT; ++i)
-#pragma unroll
-    for (int j = 0; j < EE; ++j) sum[i][j] = 0;
-  for (int k = lane * 8; k < a.hidden; k += 512) {
-    float xs[TT][8], ws[EE][8];
+  double sum[TT] = {};
+  for (int k = (wave * 64 + lane) * 8; k < a.hidden; k += 2048) {
+    float xs[TT][8], ws[8];
+    load8<true, false>(w, k, ws);
 #pragma unroll
     for (int i = 0; i < TT; ++i) load8<true, false>(x[i], k, xs[i]);
 #pragma unroll
-    for (int i = 0; i < EE; ++i) load8<true, false>(w[i], k, ws[i]);
-#pragma unroll
     for (int v = 0; v < 8; ++v) {
-      double wd[EE];
+      const double wd = ws[v];
 #pragma unroll
-      for (int j = 0; j < EE; ++j) wd[j] = ws[j][v];
-#pragma unroll
-      for (int i = 0; i < TT; ++i) {
-        const double xd = xs[i][v];
-#pragma unroll
-        for (int j = 0; j < EE; ++j) sum[i][j] = fma(xd, wd[j], sum[i][j]);
-      }
+      for (int i = 0; i < TT; ++i) sum[i] = fma((double)xs[i][v], wd, sum[i]);
     }
   }
 #pragma unroll
-  for (int i = 0; i < TT; ++i)
+  for (int i = 0; i < TT; ++i) {
+    sum[i] = wave_sum(sum[i]);
+    if (lane == 0) part[wave][i] = sum[i];
+  }
+  __syncthreads();
+  const int i = threadIdx.x;
+  if (i < TT && t0 + i < a.n_rows) a.logits[(t0 + i) * a.experts + e] = part[0][i] + part[1][i] + part[2][i] + part[3][i];
+}
+
+// The same for many rows, 16 of them by 16 experts a workgroup, its 16 waves sharing out k: v_mfma_f64_16x16x4_f64, whose operands a lane
+// widens once for 16 products each.
+typedef double pf64x4 __attribute__((ext_vector_type(4)));
+__global__ __launch_bounds__(1024) void moe_logits_tile_kernel(MoeArgs a) {
+  __shared__ double part[16][4][64];
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int e = threadIdx.x; e < a.experts + a.shared; e += 1024) a.counts[e * COUNT_APART] = 0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int64_t t0 = (int64_t)blockIdx.y * 16;
+  const int e0 = blockIdx.x * 16;
+  const bf16_t* x = a.x + min(t0 + r, a.n_rows - 1) * a.x_row + 8 * g;
+  const bf16_t* w = a.router + (int64_t)min(e0 + r, a.experts - 1) * a.hidden + 8 * g;
+  const int steps = a.hidden / 32, s0 = steps * wave / 16, s1 = steps * (wave + 1) / 16;
+  pf64x4 acc = {0, 0, 0, 0};
+  constexpr int U = 4;
+  for (int s = s0; s < s1; s += U) {
+    float xs[U][8], ws[U][8];
 #pragma unroll
-    for (int j = 0; j < EE; ++j) {
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) sum[i][j] += __shfl_xor(sum[i][j], m);
-      if (lane == 0 && t0 + i < a.n_rows && e0 + j < a.experts) a.logits[(t0 + i) * a.experts + e0 + j] = sum[i][j];
+    for (int u = 0; u < U; ++u) {
+      load8<true, false>(x, (int64_t)min(s + u, s1 - 1) * 32, xs[u]);
+      load8<true, false>(w, (int64_t)min(s + u, s1 - 1) * 32, ws[u]);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s + u < s1) {
+#pragma unroll
+        for (int v = 0; v < 8; ++v) acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)xs[u][v], (double)ws[u][v], acc, 0, 0, 0);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) part[wave][i][lane] = acc[i];
+  __syncthreads();
+  if (wave >= 4) return;
+  // wave i has rows 4 i + lane / 16: that is how the products lie
+  double v = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v += part[i][wave][lane];
+  const int64_t t = t0 + 4 * wave + g;
+  if (t < a.n_rows && e0 + r < a.experts) a.logits[t * a.experts + e0 + r] = v;
 }
 
 // a double as a number that orders the same way; a NaN below every number
@@ -452,99 +621,340 @@ __device__ __forceinline__ uint64_t order_of(double v) {
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-__device__ __forceinline__ double block_reduce(double v, bool largest, double* shared) {
+__device__ __forceinline__ double block_sum(double v, double* shared) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return shared[0] + shared[1] + shared[2] + shared[3];
+}
+__device__ __forceinline__ double block_max(double v, double* shared) {
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const double o = __shfl_xor(v, m);
-    v = largest ? fmax(v, o) : v + o;
-  }
-  const int waves = blockDim.x >> 6;
-  if (waves > 1) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = shared[0];
-    for (int w = 1; w < waves; ++w) v = largest ? fmax(v, shared[w]) : v + shared[w];
-  }
-  return v;
+  for (int m = 1; m < 64; m <<= 1) v = fmax(v, __shfl_xor(v, m));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return fmax(fmax(shared[0], shared[1]), fmax(shared[2], shared[3]));
 }
 
-// A workgroup takes a row: an expert's place is the number of experts that come before it, counted against all of them at once.  Rows are entered in
-// the lists of their experts in whatever order the workgroups come: a row's results do not depend on its place in them.
+// The experts of a row, found by a workgroup of 256: an expert's place is the number of experts that come before it, counted against all of
+// them, the threads that an expert has to spare sharing them out.  The upper halves of the keys are compared, four at a time; the whole
+// ones only where another's upper half is the same.  Where weights are asked for, thread i < top returns that of the i-th.
+struct Choice {
+  uint64_t key[MAX_EXPERTS];
+  __attribute__((aligned(16))) uint32_t upper[MAX_EXPERTS + 32];
+  double logit[MAX_EXPERTS];
+  double shared[4];
+  int expert[MAX_TOP];
+};
+__device__ __forceinline__ float choose(const MoeArgs& a, int64_t t, Choice& c, bool weights) {
+  const int tid = threadIdx.x, E = a.experts;
+  // a softmax needs its sum only where the scores themselves count
+  const bool plain = a.renormalise && !a.choice_bias;
+  double top = -__builtin_inf(), sum = 1;
+  bool nan = false;
+  for (int e = tid; e < E; e += 256) {
+    const double l = a.logits[t * E + e];
+    c.logit[e] = l;
+    nan |= l != l;
+    top = fmax(top, l);                  // (passes over a NaN; the sum keeps it)
+  }
+  if (!a.sigmoid && !plain) {
+    top = block_max(top, c.shared);
+    sum = 0;
+    for (int e = tid; e < E; e += 256) sum += exp(c.logit[e] - top);
+    sum = block_sum(sum, c.shared);
+  }
+  auto score = [&](double logit) { return a.sigmoid ? 1 / (1 + exp(-logit)) : exp(logit - top) / sum; };
+  for (int e = tid; e < E; e += 256) {
+    const double l = c.logit[e];
+    const uint64_t k = order_of(a.choice_bias ? score(l) + (double)a.choice_bias[e] : l);
+    c.key[e] = k;
+    c.upper[e] = (uint32_t)(k >> 32);
+  }
+  if (tid < 32) c.upper[E + tid] = 0;    // (before none)
+  nan = __syncthreads_or(nan);
+  const int shares = E > 128 ? 1 : E > 64 ? 2 : E > 32 ? 4 : 8, each = (E / shares + 4) & ~3;        // (shares * each > E - 1, within upper)
+  const int first = tid % shares * each;
+  for (int e0 = 0; e0 < E; e0 += 256 / shares) {
+    const int e = e0 + tid / shares, in = min(e, E - 1);
+    const uint32_t mine = c.upper[in];
+    int before = 0, not_behind = 0;
+#pragma unroll 4
+    for (int o = first; o < first + each; o += 4) {
+      const cu32x4 v = *reinterpret_cast<const cu32x4*>(c.upper + o);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        before += v[i] > mine;
+        not_behind += v[i] >= mine;
+      }
+    }
+    if (not_behind - before > (in >= first && in < first + each)) {
+      const uint64_t key = c.key[in];
+      before = 0;
+      for (int o = first; o < min(E, first + each); ++o) before += (c.key[o] > key) | ((c.key[o] == key) & (o < in));
+    }
+    for (int m = 1; m < shares; m <<= 1) before += __shfl_xor(before, m);
+    if (e < E && before < a.top && tid % shares == 0) c.expert[before] = e;
+  }
+  __syncthreads();
+  if (!weights || tid >= 64) return 0.f;
+  double w = 0;
+  if (tid < a.top) {
+    if (!a.sigmoid && plain) top = c.logit[c.expert[0]];
+    w = nan && !a.sigmoid ? __builtin_nan("") : score(c.logit[c.expert[tid]]);
+  }
+  if (a.renormalise) w /= wave_sum(w);
+  return (float)(w * (double)a.scale);
+}
+
+// A workgroup takes a row.  Rows are entered in the lists of their experts in whatever order the workgroups come: a row's results do
+// not depend on its place in them.
 __global__ __launch_bounds__(256) void moe_select_kernel(MoeArgs a) {
-  __shared__ uint64_t key[MAX_EXPERTS];
-  __shared__ double score_of[MAX_TOP], shared[4];
-  __shared__ int chosen[MAX_TOP];
+  __shared__ Choice c;
   const int64_t t = blockIdx.x;
-  const int tid = threadIdx.x, threads = blockDim.x, E = a.experts;
-  const bool live = !a.live || a.live[t];
-  if (!live) {
+  const int tid = threadIdx.x;
+  if (a.live && !a.live[t]) {
     if (tid < a.top) {
       a.experts_out[t * a.top + tid] = -1;
       a.weights_out[t * a.top + tid] = 0.f;
     }
     return;
   }
-  const double* logits = a.logits + t * E;
-  double top = -__builtin_inf(), sum = 0;
-  if (!a.sigmoid) {                      // (fmax passes over a NaN; the sum keeps it)
-    for (int e = tid; e < E; e += threads) top = fmax(top, logits[e]);
-    top = block_reduce(top, true, shared);
-    for (int e = tid; e < E; e += threads) sum += exp(logits[e] - top);
-    sum = block_reduce(sum, false, shared);
-  }
-  auto score = [&](int e) { return a.sigmoid ? 1 / (1 + exp(-logits[e])) : exp(logits[e] - top) / sum; };
-  for (int e = tid; e < E; e += threads) key[e] = order_of(a.choice_bias ? score(e) + (double)a.choice_bias[e] : logits[e]);
-  __syncthreads();
-  for (int e = tid; e < E; e += threads) {
-    const uint64_t mine = key[e];
-    int place = 0;
-    for (int o = 0; o < E; ++o) place += (key[o] > mine) | ((key[o] == mine) & (o < e));
-    if (place < a.top) {
-      chosen[place] = e;
-      score_of[place] = score(e);
-    }
-  }
-  __syncthreads();
+  const float w = choose(a, t, c, true);
   if (tid >= a.slots) return;
-  const int64_t cells = t * a.slots + tid;
   int e = a.experts + tid - a.top;       // a shared one
   if (tid < a.top) {
-    double all = 0;
-    for (int i = 0; i < a.top; ++i) all += score_of[i];
-    const double w = a.renormalise ? score_of[tid] / all : score_of[tid];
-    e = chosen[tid];
+    e = c.expert[tid];
     a.experts_out[t * a.top + tid] = e;
-    a.weights_out[t * a.top + tid] = (float)(w * (double)a.scale);
+    a.weights_out[t * a.top + tid] = w;
   }
-  a.lists[(int64_t)e * a.list_row + atomicAdd(a.counts + e, 1)] = (int32_t)cells;
+  a.lists[(int64_t)e * a.list_row + atomicAdd(a.counts + e * COUNT_APART, 1)] = (int32_t)(t * a.slots + tid);
+}
+
+__device__ __forceinline__ cf32x4 gated(cf32x4 gate, cf32x4 up) {
+  cf32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = gate[i] / (1.f + __expf(-gate[i])) * up[i];
+  return v;
+}
+
+// ---- few rows an expert: 16 at a time, straight from memory (direct_product), a workgroup's waves sharing out k.
+// UP: a workgroup takes PAIRS pairs of tiles, gate and up.  ONE: the call has one row, and every workgroup chooses its experts for itself, which
+// is less than a launch.
+template <int FMT, bool ONE, int PAIRS>
+__global__ __launch_bounds__(256) void moe_few_up_kernel(MoeArgs a) {
+  struct Nothing {};
+  __shared__ union {
+    std::conditional_t<ONE, Choice, Nothing> c;
+    cf32x4 part[4][2 * PAIRS][64];
+  } s;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
+  int e = blockIdx.y, count = 1, cell = blockIdx.y;
+  if constexpr (ONE) {
+    const bool live = !a.live || a.live[0], writes = blockIdx.x == 0 && blockIdx.y == 0;
+    const int slot = blockIdx.y;
+    if (!live) {
+      if (writes && threadIdx.x < a.top) {
+        a.experts_out[threadIdx.x] = -1;
+        a.weights_out[threadIdx.x] = 0.f;
+      }
+      return;
+    }
+    e = a.experts + slot - a.top;
+    if (slot < a.top) {
+      const float w = choose(a, 0, s.c, writes);
+      e = __builtin_amdgcn_readfirstlane(s.c.expert[slot]);
+      if (writes && threadIdx.x < a.top) {
+        a.experts_out[threadIdx.x] = s.c.expert[threadIdx.x];
+        a.weights_out[threadIdx.x] = w;
+      }
+      __syncthreads();                   // (what follows lies in the same place)
+    }
+  } else {
+    cell = a.lists[(int64_t)e * a.list_row + min(t, a.list_row - 1)];      // (asked for with the count, used where there is a row)
+    count = a.counts[e * COUNT_APART];
+  }
+  const PackedShape& shape = a.up_shape;
+  const int pairs = a.inter / 16;
+  const unsigned char* matrix = a.up + (int64_t)e * shape.tiles * shape.tile_bytes;
+  const unsigned char* tile[2 * PAIRS];
+#pragma unroll
+  for (int j = 0; j < PAIRS; ++j) {
+    const int pair = min((int)blockIdx.x * PAIRS + j, pairs - 1);
+    tile[2 * j] = matrix + (int64_t)pair * shape.tile_bytes;
+    tile[2 * j + 1] = matrix + (int64_t)(pair + pairs) * shape.tile_bytes;
+  }
+  const int b0 = shape.blocks * wave / 4, b1 = shape.blocks * (wave + 1) / 4;
+  for (int r = 0; r < count; r += 16) {
+    if (r) __syncthreads();
+    const bool live = r + t < count;
+    if (r) cell = a.lists[(int64_t)e * a.list_row + min(r + t, count - 1)];
+    cf32x4 acc[2 * PAIRS];
+#pragma unroll
+    for (int j = 0; j < 2 * PAIRS; ++j) acc[j] = cf32x4{0.f, 0.f, 0.f, 0.f};
+    const int64_t row = ONE || !live ? 0 : cell / a.slots;
+    direct_product<FMT, 2 * PAIRS, FMT == CS_WEIGHTS_E2M1 ? 2 : 1>(acc, tile, shape.blocks, shape.k, b0, b1, a.x + row * a.x_row + 8 * g, live, lane);
+#pragma unroll
+    for (int j = 0; j < 2 * PAIRS; ++j) s.part[wave][j][lane] = acc[j];
+    __syncthreads();
+    const int pair = (int)blockIdx.x * PAIRS + wave;
+    if (wave < PAIRS && pair < pairs && live) {
+      cf32x4 v[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) v[i] = s.part[0][2 * wave + i][lane] + s.part[1][2 * wave + i][lane] + s.part[2][2 * wave + i][lane] + s.part[3][2 * wave + i][lane];
+      store4<true>(a.h, (int64_t)cell * a.inter + pair * 16 + 4 * g, gated(v[0], v[1]), 4, true);
+    }
+  }
+}
+
+// DOWN, rows by their lists, into the parts of y: a workgroup takes 2 RT tiles, two waves to each RT of them
+template <int FMT, int RT>
+__global__ __launch_bounds__(256) void moe_few_down_kernel(MoeArgs a) {
+  __shared__ cf32x4 part[2][RT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
+  const int e = blockIdx.y, at = (blockIdx.x * 2 + wave / 2) * RT, half = wave & 1;
+  int cell = a.lists[(int64_t)e * a.list_row + min(t, a.list_row - 1)];    // (asked for with the count, used where there is a row)
+  const int count = a.counts[e * COUNT_APART];
+  const PackedShape& shape = a.down_shape;
+  const unsigned char* matrix = a.down + (int64_t)e * shape.tiles * shape.tile_bytes;
+  const unsigned char* tile[RT];
+#pragma unroll
+  for (int j = 0; j < RT; ++j) tile[j] = matrix + (int64_t)min(at + j, shape.tiles - 1) * shape.tile_bytes;
+  const int b0 = half ? shape.blocks / 2 : 0, b1 = half ? shape.blocks : shape.blocks / 2;
+  for (int r = 0; r < count; r += 16) {
+    if (r) __syncthreads();
+    const bool live = r + t < count;
+    if (r) cell = a.lists[(int64_t)e * a.list_row + min(r + t, count - 1)];
+    cf32x4 acc[RT];
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[j] = cf32x4{0.f, 0.f, 0.f, 0.f};
+    direct_product<FMT, RT, FMT == CS_WEIGHTS_E2M1 ? 3 : 1>(acc, tile, shape.blocks, shape.k, b0, b1, a.h + (int64_t)(live ? cell : 0) * a.inter + 8 * g, live, lane);
+    if (half) {
+#pragma unroll
+      for (int j = 0; j < RT; ++j) part[wave / 2][j][lane] = acc[j];
+    }
+    __syncthreads();
+    if (!half && live) {
+#pragma unroll
+      for (int j = 0; j < RT; ++j)
+        if (at + j < shape.tiles)
+          store4<false>(a.parts, (int64_t)cell * a.hidden + (at + j) * 16 + 4 * g, acc[j] + part[wave / 2][j][lane], 4, true);
+    }
+  }
+}
+
+// DOWN of one row, the whole sum: a workgroup takes a tile of y, its waves a part along k of a slot's expert each
+template <int FMT>
+__global__ __launch_bounds__(1024) void moe_row_sum_kernel(MoeArgs a, int shares) {
+  __shared__ cf32x4 part[16][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
+  const PackedShape& shape = a.down_shape;
+  cf32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (!a.live || a.live[0])
+    for (int unit = wave; unit < a.slots * shares; unit += 16) {
+      const int slot = unit / shares, at = unit - slot * shares;
+      const int e = __builtin_amdgcn_readfirstlane(slot < a.top ? a.experts_out[slot] : a.experts + slot - a.top);
+      const float w = slot < a.top ? a.weights_out[slot] : 1.f;
+      const unsigned char* tile[1] = {a.down + ((int64_t)e * shape.tiles + blockIdx.x) * shape.tile_bytes};
+      cf32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
+      direct_product<FMT, 1, FMT == CS_WEIGHTS_E2M1 ? 3 : 2>(acc, tile, shape.blocks, shape.k, shape.blocks * at / shares, shape.blocks * (at + 1) / shares,
+                                                            a.h + (int64_t)slot * a.inter + 8 * g, t == 0, lane);
+      sum += w * acc[0];
+    }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave || t) return;
+  for (int w = 1; w < 16; ++w) sum += part[w][lane];
+  store4<true>(a.y, blockIdx.x * 16 + 4 * g, sum, 4, true);
+}
+
+// DOWN of up to 16 rows, the whole sum: a workgroup takes a tile of y and all experts, its waves an expert (or, where there are fewer, a part of one
+// along k) at a time.  A row that the expert was not chosen for has zeros as its operand; its weight multiplies the expert's sum, and the
+// waves' sums are added in LDS, so nothing is written but y.
+template <int FMT>
+__global__ __launch_bounds__(1024) void moe_few_sum_kernel(MoeArgs a, int shares) {
+  __shared__ cf32x4 part[16][64];
+  __shared__ signed char slot_of[MAX_EXPERTS][16];       // by expert and row: the row's slot, or none
+  __shared__ float weight[16][MAX_TOP];
+  __shared__ int used[MAX_EXPERTS], n_used;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
+  const int rows = (int)a.n_rows, top = a.top, E = a.experts;
+  const bool is = t < rows && (!a.live || a.live[t < rows ? t : 0]);
+  for (int i = threadIdx.x; i < 4 * E; i += 1024) reinterpret_cast<uint32_t*>(slot_of)[i] = 0xffffffffu;
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * top; i += 1024) {
+    const int e = a.experts_out[i], r = i / top;
+    weight[r][i - r * top] = a.weights_out[i];
+    if (e >= 0) slot_of[e][r] = (signed char)(i - r * top);
+  }
+  __syncthreads();
+  if (wave == 0) {                                       // the experts that rows have, in their order
+    int n = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+      bool any = false;
+      if (e0 + lane < E) {
+        const cu32x4 v = *reinterpret_cast<const cu32x4*>(slot_of[e0 + lane]);
+        any = (v[0] & v[1] & v[2] & v[3]) != 0xffffffffu;
+      }
+      const uint64_t m = __ballot(any);
+      if (any) used[n + __popcll(m & ((1ull << lane) - 1))] = e0 + lane;
+      n += __popcll(m);
+    }
+    if (lane == 0) n_used = n;
+  }
+  __syncthreads();
+  const PackedShape& shape = a.down_shape;
+  cf32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  const int units = (n_used + a.shared) * shares;
+  for (int unit = wave; unit < units; unit += 16) {
+    const int i = unit / shares, at = unit - i * shares, mine = n_used;
+    int e = E + i - mine, slot = is ? top + i - mine : -1;
+    float w = 1.f;
+    if (i < mine) {
+      e = __builtin_amdgcn_readfirstlane(used[i]);
+      slot = slot_of[e][t];
+      w = slot >= 0 ? weight[t][slot] : 0.f;
+    }
+    const bool live = slot >= 0;
+    const unsigned char* tile[1] = {a.down + ((int64_t)e * shape.tiles + blockIdx.x) * shape.tile_bytes};
+    const int b0 = shape.blocks * at / shares, b1 = shape.blocks * (at + 1) / shares;
+    cf32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
+    direct_product<FMT, 1, FMT == CS_WEIGHTS_E2M1 ? 3 : 2>(acc, tile, shape.blocks, shape.k, b0, b1,
+                                                          a.h + ((int64_t)(live ? t : 0) * a.slots + (live ? slot : 0)) * a.inter + 8 * g, live, lane);
+    if (live) sum += w * acc[0];
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave || t >= rows) return;
+  for (int w = 1; w < 16; ++w) sum += part[w][lane];
+  store4<true>(a.y, (int64_t)t * a.y_row + blockIdx.x * 16 + 4 * g, sum, 4, true);
 }
 
 // The experts' products, rows by their lists, in blocks of up to 64.  UP: tiles come in pairs, gate and up, and h = silu(gate) * up is
 // written; else the parts of y.
-template <int FMT, bool UP, int MT>
+constexpr int EXPERT_LDS = 36864;
+template <int FMT, bool UP, int MT, int RT, int WD>
 __device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block, const int32_t* list, int rows, unsigned char* lds) {
-  constexpr int RT = 2, NB = FMT == CS_WEIGHTS_E2M1 ? (MT == 1 ? 4 : 2) : (MT == 1 ? 2 : 1);
-  typedef Staged<FMT, MT, 1, RT, NB> P;
+  constexpr int SS = MT == 4 ? 2 : 4, NS = MT == 4 ? 4 : 3;
+  typedef Staged<FMT, MT, 1, RT, SS, NS, WD> P;
+  static_assert(P::LDS <= EXPERT_LDS, "what the launch gives");
   const PackedShape& shape = UP ? a.up_shape : a.down_shape;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
   const unsigned char* matrix = (UP ? a.up : a.down) + (int64_t)e * shape.tiles * shape.tile_bytes;
-  const int pairs = a.inter / 16;                      // UP: tiles of gate, and of up
-  const int at = n_block * 4 + wave;
-  int tiles[2] = {min(at, pairs - 1), min(at, pairs - 1) + pairs};
-  if constexpr (!UP) {
-    tiles[0] = min(2 * at, shape.tiles - 1);
-    tiles[1] = min(2 * at + 1, shape.tiles - 1);
-  }
-  const unsigned char* tile[RT] = {matrix + tiles[0] * shape.tile_bytes, matrix + tiles[1] * shape.tile_bytes};
+  const int pairs = a.inter / 16, at = (n_block * 4 + wave) * (UP ? RT / 2 : RT);        // UP: pairs of tiles, gate and up
+  const unsigned char* tile[RT];
+#pragma unroll
+  for (int j = 0; j < RT; ++j) tile[j] = matrix + (int64_t)(UP ? min(at + j / 2, pairs - 1) + j % 2 * pairs : min(at + j, shape.tiles - 1)) * shape.tile_bytes;
   uint32_t offs[MT];
   int cell[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     cell[m] = list[min(m * 16 + t, rows - 1)];
-    offs[m] = (UP ? (uint32_t)(cell[m] / a.slots) * (uint32_t)a.x_row : (uint32_t)cell[m] * (uint32_t)a.inter) * 2 + 16 * g;
+    const int asked = list[min(m * 16 + (lane >> 2), rows - 1)];
+    offs[m] = (UP ? (uint32_t)(asked / a.slots) * (uint32_t)a.x_row : (uint32_t)asked * (uint32_t)a.inter) * 2;
   }
-  auto off = [&](int m) {
+  auto off = [&](int m) __attribute__((always_inline)) {
     uint32_t o = offs[0];
 #pragma unroll
     for (int i = 1; i < MT; ++i) o = m == i ? offs[i] : o;
@@ -556,69 +966,64 @@ __device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[j][m] = cf32x4{0.f, 0.f, 0.f, 0.f};
   P::product(acc, tile, shape.blocks, shape.k, 0, shape.blocks, UP ? a.x : a.h, off, lds, lane, wave, 0);
-  if constexpr (UP) {
-    if (at < pairs) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-        if (m * 16 + t < rows) {
-          cf32x4 v;
+  for (int j = 0; j < (UP ? RT / 2 : RT); ++j) {
+    if (at + j >= (UP ? pairs : shape.tiles)) continue;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = acc[0][m][i] / (1.f + __expf(-acc[0][m][i])) * acc[1][m][i];
-          store4<true>(a.h, (int64_t)cell[m] * a.inter + at * 16 + 4 * g, v, 4, true);
-        }
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < RT; ++j)
-      if (2 * at + j < shape.tiles) {
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-          if (m * 16 + t < rows) store4<false>(a.parts, (int64_t)cell[m] * a.hidden + (2 * at + j) * 16 + 4 * g, acc[j][m], 4, true);
+    for (int m = 0; m < MT; ++m)
+      if (m * 16 + t < rows) {
+        if constexpr (UP) store4<true>(a.h, (int64_t)cell[m] * a.inter + (at + j) * 16 + 4 * g, gated(acc[2 * j][m], acc[2 * j + 1][m]), 4, true);
+        else store4<false>(a.parts, (int64_t)cell[m] * a.hidden + (at + j) * 16 + 4 * g, acc[j][m], 4, true);
       }
   }
 }
 
-template <int FMT, bool UP>
+template <int FMT, bool UP, int RT, int WD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) void moe_experts_kernel(MoeArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int e = blockIdx.y, n_block = blockIdx.x;
-  const int count = a.counts[e];
+  const int count = a.counts[e * COUNT_APART];
   for (int r = blockIdx.z * 64; r < count; r += gridDim.z * 64) {
     if (r >= (int)gridDim.z * 64) __syncthreads();     // (the rows before are still being read)
     const int rows = min(64, count - r);
     const int32_t* list = a.lists + (int64_t)e * a.list_row + r;
-    if (rows <= 16) expert_rows<FMT, UP, 1>(a, e, n_block, list, rows, lds);
-    else if (rows <= 32) expert_rows<FMT, UP, 2>(a, e, n_block, list, rows, lds);
-    else if (rows <= 48) expert_rows<FMT, UP, 3>(a, e, n_block, list, rows, lds);
-    else expert_rows<FMT, UP, 4>(a, e, n_block, list, rows, lds);
+    if (rows <= 16) expert_rows<FMT, UP, 1, RT, WD>(a, e, n_block, list, rows, lds);
+    else if (rows <= 32) expert_rows<FMT, UP, 2, RT, WD>(a, e, n_block, list, rows, lds);
+    else if (rows <= 48) expert_rows<FMT, UP, 3, RT, WD>(a, e, n_block, list, rows, lds);
+    else expert_rows<FMT, UP, 4, RT, WD>(a, e, n_block, list, rows, lds);
   }
 }
 
-// y of a row: its parts by their weights, in the order of the slots, in fp32
+// y of a row: its parts by their weights, in the order of the slots, in fp32; eight parts asked for together
 __global__ __launch_bounds__(256) void moe_sum_kernel(MoeArgs a) {
   const int64_t t = blockIdx.x;
-  const bool live = !a.live || a.live[t];
-  const float* w = a.weights_out + t * a.top;
-  for (int n = ((int)blockIdx.y * 256 + threadIdx.x) * 8; n < a.hidden; n += (int)gridDim.y * 2048) {
-    float v[8] = {};
-    if (live) {
-      for (int i = 0; i < a.slots; ++i) {
-        float p[8];
-        load8<false, false>(a.parts, (t * a.slots + i) * a.hidden + n, p);
-        const float weight = i < a.top ? w[i] : 1.f;
+  const int n = ((int)blockIdx.y * 256 + threadIdx.x) * 4;
+  if (n >= a.hidden) return;
+  cf32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (!a.live || a.live[t]) {
+    const float* from = a.parts + t * a.slots * a.hidden + n;
+    for (int i0 = 0; i0 < a.slots; i0 += 8) {
+      cf32x4 p[8];
+      float w[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = fmaf(weight, p[j], v[j]);
+      for (int i = 0; i < 8; ++i) {
+        const int slot = min(i0 + i, a.slots - 1);
+        p[i] = *reinterpret_cast<const cf32x4*>(from + (int64_t)slot * a.hidden);
+        w[i] = slot < a.top ? a.weights_out[t * a.top + slot] : 1.f;
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i0 + i < a.slots) v += w[i] * p[i];
     }
-    store8<true, false>(a.y, t * a.y_row + n, v);
   }
+  store4<true>(a.y, t * a.y_row + n, v, 4, true);
 }
 
 namespace {
 
 // Rows of a call that go through the launches together: they bound the workspace, and the rows of h lie within 32-bit offsets
 int64_t group_rows(const MoeArgs& a) {
-  const int64_t most = std::min<int64_t>(MOE_ROWS, 0xffffffffll / (2ll * (a.top + a.shared) * a.inter));
+  const int64_t most = std::min<int64_t>(MOE_ROWS, 0x7fffffffll / (2ll * (a.top + a.shared) * a.inter));
   return std::min(a.n_rows, most);
 }
 
@@ -627,19 +1032,39 @@ size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 template <int FMT>
 cs_status run_moe(const MoeArgs& a, hipStream_t s) {
   const int T = (int)a.n_rows, all = a.experts + a.shared;
-  if (T < 4) hipLaunchKernelGGL((moe_logits_kernel<1, 1>), dim3((a.experts + 3) / 4, T), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((moe_logits_kernel<4, 4>), dim3((a.experts + 15) / 16, (T + 3) / 4), dim3(256), 0, s, a);
+  if (T >= 64) hipLaunchKernelGGL(moe_logits_tile_kernel, dim3((a.experts + 15) / 16, (T + 15) / 16), dim3(1024), 0, s, a);
+  else if ((int64_t)T * a.experts <= 1024) hipLaunchKernelGGL((moe_logits_kernel<1>), dim3(a.experts, T), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((moe_logits_kernel<4>), dim3(a.experts, (T + 3) / 4), dim3(256), 0, s, a);
   CS_HIP(hipGetLastError());
-  hipLaunchKernelGGL(moe_select_kernel, dim3(T), dim3(std::max(64, std::min(256, (a.experts + 63) / 64 * 64))), 0, s, a);
+  if (T == 1) {
+    hipLaunchKernelGGL((moe_few_up_kernel<FMT, true, 1>), dim3(a.inter / 16, a.slots), dim3(256), 0, s, a);
+  } else {
+    hipLaunchKernelGGL(moe_select_kernel, dim3(T), dim3(256), 0, s, a);
+    CS_HIP(hipGetLastError());
+    // few rows an expert, on average: 16 at a time
+    if ((int64_t)T * a.top <= 6 * a.experts || T <= 16) {
+      constexpr int PAIRS = FMT == CS_WEIGHTS_E2M1 ? 2 : 1;
+      hipLaunchKernelGGL((moe_few_up_kernel<FMT, false, PAIRS>), dim3(a.inter / 16 / PAIRS, all), dim3(256), 0, s, a);
+      if (T > 16) hipLaunchKernelGGL((moe_few_down_kernel<FMT, 2>), dim3((a.hidden / 16 + 3) / 4, all), dim3(256), 0, s, a);
+    } else {
+      // workgroups for twice the rows that an expert has on average; those with more take them in turn
+      const int z = (int)std::max<int64_t>(1, std::min<int64_t>((T + 63) / 64, (2ll * T * a.top / a.experts + 63) / 64));
+      constexpr bool SMALL = FMT == CS_WEIGHTS_E2M1;           // (bf16 weights: half as many tiles a wave, for the registers)
+      constexpr int RT = SMALL ? 4 : 2, UP_WD = 1, DOWN_WD = SMALL ? 2 : 1;
+      hipLaunchKernelGGL((moe_experts_kernel<FMT, true, RT, UP_WD>), dim3((a.inter / 16 + 2 * RT - 1) / (2 * RT), all, z), dim3(256), EXPERT_LDS, s, a);
+      CS_HIP(hipGetLastError());
+      hipLaunchKernelGGL((moe_experts_kernel<FMT, false, RT, DOWN_WD>), dim3((a.hidden / 16 + 4 * RT - 1) / (4 * RT), all, z), dim3(256), EXPERT_LDS, s, a);
+    }
+  }
   CS_HIP(hipGetLastError());
-  // workgroups for twice the rows that an expert has on average; those with more take them in turn
-  const int z = (int)std::max<int64_t>(1, std::min<int64_t>((T + 63) / 64, (2ll * T * a.top / a.experts + 63) / 64));
-  const int up_lds = 65536;
-  hipLaunchKernelGGL((moe_experts_kernel<FMT, true>), dim3((a.inter / 16 + 3) / 4, all, z), dim3(256), up_lds, s, a);
-  CS_HIP(hipGetLastError());
-  hipLaunchKernelGGL((moe_experts_kernel<FMT, false>), dim3((a.hidden / 16 + 7) / 8, all, z), dim3(256), up_lds, s, a);
-  CS_HIP(hipGetLastError());
-  hipLaunchKernelGGL(moe_sum_kernel, dim3(T, T > 1024 ? 1 : (a.hidden + 2047) / 2048), dim3(256), 0, s, a);
+  if (T <= 16) {
+    // parts of an expert, so that every wave has one where few experts have rows
+    const int shares = std::max(1, std::min(a.down_shape.blocks, 16 / std::min(16, T * a.top + a.shared)));
+    if (T == 1) hipLaunchKernelGGL((moe_row_sum_kernel<FMT>), dim3(a.hidden / 16), dim3(1024), 0, s, a, std::max(1, std::min(a.down_shape.blocks, 16 / std::min(16, a.slots))));
+    else hipLaunchKernelGGL((moe_few_sum_kernel<FMT>), dim3(a.hidden / 16), dim3(1024), 0, s, a, shares);
+  } else {
+    hipLaunchKernelGGL(moe_sum_kernel, dim3(T, (a.hidden + 1023) / 1024), dim3(256), 0, s, a);
+  }
   CS_HIP(hipGetLastError());
   return CS_OK;
 }
@@ -657,7 +1082,7 @@ size_t moe_layout(MoeArgs& a, void* workspace) {
   a.slots = a.top + a.shared;
   a.list_row = (int32_t)rows;
   a.logits = reinterpret_cast<double*>(take((size_t)rows * a.experts * 8));
-  a.counts = reinterpret_cast<int32_t*>(take((size_t)(a.experts + a.shared) * 4));
+  a.counts = reinterpret_cast<int32_t*>(take((size_t)(a.experts + a.shared) * COUNT_APART * 4));
   a.lists = reinterpret_cast<int32_t*>(take((size_t)(a.experts + a.shared) * rows * 4));
   a.h = reinterpret_cast<bf16_t*>(take((size_t)rows * a.slots * a.inter * 2));
   a.parts = reinterpret_cast<float*>(take((size_t)rows * a.slots * a.hidden * 4));
