@@ -196,11 +196,12 @@ __global__ __launch_bounds__(1024) void linear_direct_kernel(LinearArgs a, int w
 #pragma unroll
   for (int j = 0; j < RT; ++j) part[wave][j][lane] = acc[j];
   __syncthreads();
-  if (wave >= RT) return;
-  cf32x4 v = part[0][wave][lane];
-  for (int w = 1; w < waves; ++w) v += part[w][wave][lane];
-  const int n = (blockIdx.x * RT + wave) * 16 + 4 * g, left = a.shape.n - n;
-  if (live && left > 0) store4<BF16>(a.out, t * a.out_row + n, v + bias4(a.bias, n, a.shape.n), left, whole_rows && left >= 4);
+  for (int j = wave; j < RT; j += waves) {
+    cf32x4 v = part[0][j][lane];
+    for (int w = 1; w < waves; ++w) v += part[w][j][lane];
+    const int n = (blockIdx.x * RT + j) * 16 + 4 * g, left = a.shape.n - n;
+    if (live && left > 0) store4<BF16>(a.out, t * a.out_row + n, v + bias4(a.bias, n, a.shape.n), left, whole_rows && left >= 4);
+  }
 }
 
 // One row: a wave's part of it waits in LDS as the lanes take it, 16 bytes for each quarter, the same for all 16 columns of the product (of which one

@@ -32,6 +32,16 @@ def test_rows(rows, format):
             check(x, w, b, format, B.cs_linear_packed(x, p, bias=b, dtype=TYPES[out]), out)
 
 
+# so many columns that a workgroup takes several tiles of them, with fewer waves along k than tiles
+@pytest.mark.parametrize("format", ["e2m1", "bf16"])
+@pytest.mark.parametrize("rows", [1, 3, 16, 30])
+def test_many_columns(rows, format):
+    for n, k in ((16397, 96), (4099, 64), (16384, 672), (4160, 352)):
+        x, w, b, p = make(rows, n, k, format)
+        for out in ("bf16", "f32"):
+            check(x, w, b, format, B.cs_linear_packed(x, p, bias=b, dtype=TYPES[out]), out)
+
+
 @pytest.mark.parametrize("format", ["e2m1", "bf16"])
 @pytest.mark.parametrize("rows", [1, 5, 20, 40, 100])
 def test_long_rows_are_shared_out(rows, format):
