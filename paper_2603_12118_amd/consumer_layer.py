@@ -1,16 +1,17 @@
 """The attention part of one layer of the LLM task, over sequences that hold what the encoder task sent.
 
-    python -m paper_2603_12118_amd.consumer_layer [--sequences N] [--steps N]
+    python -m paper_2603_12118_amd.consumer_layer [--sequences N] [--steps N] [--block]
 
 Rows of hidden states, text and placed embeddings alike, go through
 
     QKV (cs_linear_bf16) -> cs_qk_norm_rope -> cs_cache_write -> cs_attention_cache -> output projection (cs_linear_bf16)
 
 first as chunks of a prompt, then one token of every sequence a step, the step recorded as a HIP graph that is replayed while the
-lengths on the GPU grow.  A position has three axes (time, height, width): a text token stands at (p, p, p), the tokens of an image at
+lengths on the GPU grow.  ConsumerBlock is the whole layer, on the same pages and steps: the norms before and after (cs_norm_residual), the
+projections with packed weights (cs_linear_packed) and a mixture of experts (cs_moe).  A position has three axes (time, height, width): a text token stands at (p, p, p), the tokens of an image at
 its time and their place in the grid.  Run as a program it builds a layer of 3584 values, 28 heads on 4 key/value heads of 128, sends
 every sequence an image between two texts, generates some tokens, checks the last step against attention over what cs_cache_read
-returns, and prints the time of a prompt and of a step.
+returns, and prints the time of a prompt and of a step; with --block the same of the whole layer.
 """
 from __future__ import annotations
 
@@ -93,17 +94,21 @@ class ConsumerLayer:
         self.err = torch.zeros(1, dtype=torch.int32, device=device)
         self.device = device
 
+    def project(self, x, out, name):
+        """out = x times the weights `name`, "qkv" (with its bias) or "out"."""
+        B.cs_linear_bf16(x, self.w_qkv if name == "qkv" else self.w_out, self.b_qkv if name == "qkv" else None, out)
+
     def forward(self, x, positions, slots, cu, n_keys, table, max_queries, max_keys):
         """x [T, hidden] bf16 -> [T, hidden] bf16, and the queries and their attention [T, heads, head_dim]; enqueues only."""
         T, h, kv, d = x.shape[0], self.n_heads, self.n_kv_heads, self.head_dim
         qkv = torch.empty(T, h + 2 * kv, d, dtype=torch.bfloat16, device=x.device)
-        B.cs_linear_bf16(x, self.w_qkv, self.b_qkv, qkv.view(T, -1))
+        self.project(x, qkv.view(T, -1), "qkv")
         q, k, v = qkv[:, :h], qkv[:, h:h + kv], qkv[:, h + kv:]
         B.cs_qk_norm_rope(q, k, self.cos_sin, positions, self.sections, self.q_gain, self.k_gain, q_out=q, k_out=k, err_flag=self.err)
         B.cs_cache_write(self.pool, k, v, slots, self.pages.page_tokens, err_flag=self.err)
         a = B.cs_attention_cache(q, self.pool, table, n_keys, cu, max_queries, max_keys, kv, self.pages.page_tokens, err_flag=self.err)
         out = torch.empty(T, self.hidden, dtype=torch.bfloat16, device=x.device)
-        B.cs_linear_bf16(a.view(T, -1), self.w_out, None, out)
+        self.project(a.view(T, -1), out, "out")
         return out, q, a
 
     def prefill(self, which, rows, positions):
@@ -123,6 +128,40 @@ class ConsumerLayer:
         for b, n in after.items():
             self.pages.lens[b] = n
         return got
+
+
+class ConsumerBlock(ConsumerLayer):
+    """The whole layer.  Rows of the residual stream come in and go out (bf16); a row without a slot goes through no expert."""
+
+    def __init__(self, hidden=3584, inter=1280, experts=16, top=2, shared=1, score="sigmoid", format="e2m1", residual_scale=1.0, block_scale=1.0,
+                 post_norms=True, seed=0, device="cuda:0", **attention):
+        """format: of the projections and the experts; post_norms: whether a block's output is normed before it enters the stream."""
+        super().__init__(hidden=hidden, seed=seed, device=device, **attention)
+        g = torch.Generator(device).manual_seed(seed + 1)
+        bf16 = dict(generator=g, device=device, dtype=torch.bfloat16)
+        self.packed = {"qkv": B.cs_weights_pack(self.w_qkv, format), "out": B.cs_weights_pack(self.w_out, format)}
+        self.router = torch.randn(experts, hidden, **bf16) * hidden ** -0.5
+        self.choice_bias = torch.zeros(experts, device=device) if score == "sigmoid" else None
+        self.up = B.cs_weights_pack(torch.empty(experts + shared, 2 * inter, hidden, device=device, dtype=torch.bfloat16).normal_(0, hidden ** -0.5, generator=g), format)
+        self.down = B.cs_weights_pack(torch.empty(experts + shared, hidden, inter, device=device, dtype=torch.bfloat16).normal_(0, inter ** -0.5, generator=g), format)
+        gain = lambda: 1 + 0.1 * torch.randn(hidden, generator=g, device=device)
+        self.attention_gain, self.expert_gain, self.next_gain = gain(), gain(), gain()
+        self.post_gains = (gain(), gain()) if post_norms else (None, None)
+        self.top, self.score, self.scales = top, score, dict(residual_scale=residual_scale, block_scale=block_scale)
+
+    def project(self, x, out, name):
+        B.cs_linear_packed(x, self.packed[name], bias=self.b_qkv if name == "qkv" else None, out=out)
+
+    def forward(self, x, positions, slots, cu, n_keys, table, max_queries, max_keys):
+        """Rows of the residual stream x [T, hidden] bf16 -> the stream behind the layer, and the queries and their attention; enqueues only.
+        What went through is kept in `stages` until the next call: the layers' inputs and outputs and, as `next`, the stream normed for the next layer."""
+        _, y = B.cs_norm_residual(x, x, self.attention_gain, block_scale=0.0)
+        a, q, attended = super().forward(y, positions, slots, cu, n_keys, table, max_queries, max_keys)
+        r, z = B.cs_norm_residual(a, x, self.expert_gain, post_gain=self.post_gains[0], **self.scales)
+        m, experts, weights = B.cs_moe(z, self.router, self.up, self.down, self.top, score=self.score, choice_bias=self.choice_bias, live=slots >= 0)
+        out, following = B.cs_norm_residual(m, r, self.next_gain, post_gain=self.post_gains[1], **self.scales)
+        self.stages = dict(x=x, y=y, a=a, r=r, z=z, live=slots >= 0, m=m, experts=experts, weights=weights, out=out, next=following)
+        return out, q, attended
 
 
 class DecodeStep:
@@ -204,11 +243,12 @@ def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--sequences", type=int, default=8)
     ap.add_argument("--steps", type=int, default=64)
+    ap.add_argument("--block", action="store_true", help="the whole layer, with norms and experts")
     a = ap.parse_args()
     grid, before, after = (1, 16, 16), 24, 200
     positions, following = prompt_positions([before, grid, after])
     n = len(positions)
-    layer = ConsumerLayer(sequences=a.sequences, max_keys=max(1024, n + a.steps), n_pages=a.sequences * (-(-(n + a.steps) // 64)))
+    layer = (ConsumerBlock if a.block else ConsumerLayer)(sequences=a.sequences, max_keys=max(1024, n + a.steps), n_pages=a.sequences * (-(-(n + a.steps) // 64)))
     gen = torch.Generator(layer.device).manual_seed(1)
     rows, placed = [], torch.arange(before, before + grid[1] * grid[2], device=layer.device)
     for _ in range(a.sequences):
