@@ -11,10 +11,13 @@ namespace cs {
 // ---- norms around a block.  TPR lanes hold a row, P pieces of eight values each, from the loads to the stores: x and the residual are
 // read once, r and y written once, and the two means (or means and variances, deviations from the mean, not differences of squares) are
 // sums over the lanes in between.  Rows are independent, so r may lie on the residual and y on x.
+// Bound by memory: 16384 rows of 3584, bf16 with an fp32 residual and a gate a row (822 MB), 149 us, 5.5 TB/s; by latency below some
+// 1000 rows: one row 3.3 us, a launch, the reads and two sums one behind the other.  Asking for the gains with the rows instead of in front of
+// each sum took 153 us to 149, storing past the caches 158 to 153 (1125 rows of 1280, fp32: 7.5 to 6.4), reading past them
+// loses (159; 7.8).  A wave a row, which needs no barrier, is slower from 1280 values on (1125 rows: 10.3 us).
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* shared, int& turn) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
+  v = wave_sum(v);
   if constexpr (TPR > 64) {
     constexpr int W = TPR / 64;
     float* at = shared + (turn ^= W);                  // (two places in turn: one barrier a sum)
@@ -27,7 +30,7 @@ __device__ __forceinline__ float row_sum(float v, float* shared, int& turn) {
   return v;
 }
 
-template <bool XB, bool RB, bool LAYER, int TPR, int P>
+template <bool XB, bool RB, bool LAYER, int TPR, int P, bool HOLD = P <= 2>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_residual_kernel(NormResidualArgs a) {
   constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
   __shared__ float shared[TPR > 64 ? 2 * TPR / 64 : 1];
@@ -35,24 +38,21 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_residual_kernel(No
   const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / TPR : 0);
   if (ROWS > 1 && row >= a.n_rows) return;             // (a whole wave)
   const int l = threadIdx.x % TPR;
-  float z[P][8], g[P][8];
   int at[P];
   bool has[P];
+  float pre[P][8], post[P][8];                         // gains
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     at[p] = 8 * (l + p * TPR);
     has[p] = at[p] < a.width;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[p][i] = g[p][i] = 0.f;
-    if (has[p]) load8<XB, true>(a.x, row * a.x_row + at[p], z[p]);
+    if (HOLD && has[p]) {                              // (for four pieces they would take the registers of two more waves)
+      if (a.post_gain) load8<false, false>(a.post_gain, at[p], post[p]);
+      load8<false, false>(a.pre_gain, at[p], pre[p]);
+    }
   }
-  float res[P][8];
-#pragma unroll
-  for (int p = 0; p < P; ++p)
-    if (has[p]) load8<RB, true>(a.residual, row * a.residual_row + at[p], res[p]);
 
   // v = N(v) with a gain, and a bias where there is one
-  auto normed = [&](float (&v)[P][8], const float* gain, const float* bias) {
+  auto normed = [&](float (&v)[P][8], float (&w)[P][8], const float* gain, const float* bias) {
     float mean = 0.f;
     if constexpr (LAYER) {
 #pragma unroll
@@ -69,10 +69,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_residual_kernel(No
         if constexpr (LAYER) v[p][i] -= mean;
         sum += has[p] ? v[p][i] * v[p][i] : 0.f;
       }
-    float w[P][8];
+    if constexpr (!HOLD) {
 #pragma unroll
-    for (int p = 0; p < P; ++p)                        // (asked for before the sum is waited for)
-      if (has[p]) load8<false, false>(gain, at[p], w[p]);
+      for (int p = 0; p < P; ++p)                      // (asked for before the sum is waited for)
+        if (has[p]) load8<false, false>(gain, at[p], w[p]);
+    }
     const float scale = 1.f / sqrtf(row_sum<TPR>(sum, shared, turn) * a.inv_width + a.eps);
 #pragma unroll
     for (int p = 0; p < P; ++p)
@@ -82,19 +83,30 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_residual_kernel(No
 #pragma unroll
       for (int p = 0; p < P; ++p)
         if (has[p]) {
-          load8<false, false>(bias, at[p], w[p]);
+          float c[8];
+          load8<false, false>(bias, at[p], c);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[p][i] += w[p][i];
+          for (int i = 0; i < 8; ++i) v[p][i] += c[i];
         }
     }
   };
 
+  float z[P][8], g[P][8], res[P][8];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[p][i] = 0.f;
+    if (has[p]) load8<XB, false>(a.x, row * a.x_row + at[p], z[p]);
+  }
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    if (has[p]) load8<RB, false>(a.residual, row * a.residual_row + at[p], res[p]);
   if (a.gate) {
 #pragma unroll
     for (int p = 0; p < P; ++p)
       if (has[p]) load8<XB, false>(a.gate, row * a.gate_row + at[p], g[p]);
   }
-  if (a.post_gain) normed(z, a.post_gain, a.post_bias);
+  if (a.post_gain) normed(z, post, a.post_gain, a.post_bias);
   if (a.gate) {
 #pragma unroll
     for (int p = 0; p < P; ++p)
@@ -106,12 +118,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_residual_kernel(No
     if (has[p]) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) z[p][i] = fmaf(a.block_scale, z[p][i], a.residual_scale * res[p][i]);
-      store8<RB, false>(a.r_out, row * a.r_row + at[p], z[p]);
+      store8<RB, true>(a.r_out, row * a.r_row + at[p], z[p]);
     }
-  normed(z, a.pre_gain, a.pre_bias);
+  normed(z, pre, a.pre_gain, a.pre_bias);
 #pragma unroll
   for (int p = 0; p < P; ++p)
-    if (has[p]) store8<XB, false>(a.y, row * a.y_row + at[p], z[p]);
+    if (has[p]) store8<XB, true>(a.y, row * a.y_row + at[p], z[p]);
 }
 
 // Workgroups that a launch may have (HIP refuses more than 2^32 - 1 threads along a dimension)
@@ -129,6 +141,9 @@ static void launch_norm_rows(const NormResidualArgs& a, hipStream_t s) {
   const int w = a.width;
   if (w <= 512) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 64, 1>), dim3(quarter), dim3(256), 0, s, a);
   else if (w <= 1024) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 64, 2>), dim3(quarter), dim3(256), 0, s, a);
+#ifdef W64
+  else if (w <= 1536) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 64, 3>), dim3(quarter), dim3(256), 0, s, a);
+#endif
   else if (w <= 2048) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 256, 1>), dim3(rows), dim3(256), 0, s, a);
   else if (w <= 4096) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 256, 2>), dim3(rows), dim3(256), 0, s, a);
   else if (w <= 8192) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 256, 4>), dim3(rows), dim3(256), 0, s, a);

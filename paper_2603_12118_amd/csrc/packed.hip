@@ -524,21 +524,6 @@ constexpr int COUNT_APART = 16;
 // Scores of TT rows by EE experts a wave, in fp64: products of two bf16 numbers are exact there and their sum is off by less than any two
 // experts' scores that are not equal are likely to lie apart, so that the choice is that of the definition.  The vector unit's fp64 rate is half its
 // fp32 rate.  Also clears the experts' counts for the launch behind.
-// v of the lanes of a wave, summed: within rows of 16 by DPP, whose every step gives both sides the same sum
-__device__ __forceinline__ double wave_sum(double v) {
-  auto with = [](double x, auto ctrl) {
-    constexpr int C = decltype(ctrl)::value;
-    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), C, 0xf, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, __double2hiint(x), C, 0xf, 0xf, false);
-    return x + __hiloint2double(hi, lo);
-  };
-  v = with(v, std::integral_constant<int, 0xb1>());      // lanes 1 0 3 2
-  v = with(v, std::integral_constant<int, 0x4e>());      // lanes 2 3 0 1
-  v = with(v, std::integral_constant<int, 0x141>());     // half a row mirrored
-  v = with(v, std::integral_constant<int, 0x140>());     // a row mirrored
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
-}
-
 // A workgroup takes an expert and TT rows, its waves pieces of 512 values of k in turn.
 template <int TT>
 __global__ __launch_bounds__(256) void moe_logits_kernel(MoeArgs a) {

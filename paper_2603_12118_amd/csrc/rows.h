@@ -2,6 +2,8 @@
 #pragma once
 #include "common.h"
 
+#include <type_traits>
+
 namespace cs {
 
 typedef unsigned int cu32x4 __attribute__((ext_vector_type(4)));
@@ -94,6 +96,27 @@ __device__ __forceinline__ void values8(uint32_t w, int byte, float (&x)[8]) {
   const cf32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
   const cf32x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
   x[0] = p0.x; x[1] = p0.y; x[2] = p1.x; x[3] = p1.y; x[4] = p2.x; x[5] = p2.y; x[6] = p3.x; x[7] = p3.y;
+}
+
+// v of the lanes of a wave, summed: within rows of 16 by DPP, whose every step gives both sides the same sum, across them by two
+// exchanges (an exchange goes through LDS)
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) {
+  auto with = [](T x, auto ctrl) {
+    constexpr int C = decltype(ctrl)::value;
+    if constexpr (sizeof(T) == 8) {
+      const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), C, 0xf, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, __double2hiint(x), C, 0xf, 0xf, false);
+      return x + __hiloint2double(hi, lo);
+    } else {
+      return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), C, 0xf, 0xf, false));
+    }
+  };
+  v = with(v, std::integral_constant<int, 0xb1>());      // lanes 1 0 3 2
+  v = with(v, std::integral_constant<int, 0x4e>());      // lanes 2 3 0 1
+  v = with(v, std::integral_constant<int, 0x141>());     // half a row mirrored
+  v = with(v, std::integral_constant<int, 0x140>());     // a row mirrored
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
 }
 
 // codes 2 SEL, 2 SEL + 1 of a word, times 2^(byte - 127) where the byte is in bits 23..30 of `scale`: two bf16
