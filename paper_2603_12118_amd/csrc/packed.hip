@@ -7,10 +7,14 @@
 #include "block.h"
 
 #include <algorithm>
+#include <stdlib.h>
 #include <type_traits>
 
 #include "rows.h"
 
+#ifndef UWD
+#define UWD 1
+#endif
 namespace cs {
 
 typedef __bf16 pbf16x8 __attribute__((ext_vector_type(8)));
@@ -44,10 +48,10 @@ struct Held<CS_WEIGHTS_E2M1> {
     codes = *reinterpret_cast<const cu32x4*>(tile + (int64_t)b * 1024 + lane * 16);
     scales = *reinterpret_cast<const uint32_t*>(tile + (int64_t)blocks * 1024 + b * 64 + (lane & 15) * 4);
   }
-  // the same through a resource; nothing where there are no steps
-  __device__ __forceinline__ void fetch(Resource r, int blocks, int b, int lane, int steps) {
-    codes = fetch16(r, lane * 16, steps > 0 ? (uint32_t)b * 1024 : PAST);
-    scales = fetch4(r, (lane & 15) * 4, steps > 0 ? (uint32_t)blocks * 1024 + (uint32_t)b * 64 : PAST);
+  // the same through a resource, of the tile at byte `from` of it; nothing where there are no steps
+  __device__ __forceinline__ void fetch(Resource r, int blocks, int b, int lane, int steps, uint32_t from = 0) {
+    codes = fetch16(r, lane * 16, steps > 0 ? from + (uint32_t)b * 1024 : PAST);
+    scales = fetch4(r, (lane & 15) * 4, steps > 0 ? from + (uint32_t)blocks * 1024 + (uint32_t)b * 64 : PAST);
   }
   __device__ __forceinline__ pbf16x8 at(int s) const {      // s: known when compiled
     return s == 0 ? step<0>() : s == 1 ? step<1>() : s == 2 ? step<2>() : step<3>();
@@ -67,9 +71,9 @@ struct Held<CS_WEIGHTS_BF16> {
     for (int s = 0; s < 4; ++s)             // (a step that is not there: the one before, used with zeros)
       v[s] = *reinterpret_cast<const cu32x4*>(tile + (int64_t)b * 4096 + min(s, steps - 1) * 1024 + lane * 16);
   }
-  __device__ __forceinline__ void fetch(Resource r, int, int b, int lane, int steps) {
+  __device__ __forceinline__ void fetch(Resource r, int, int b, int lane, int steps, uint32_t from = 0) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) v[s] = fetch16(r, lane * 16, s < steps ? (uint32_t)(b * 4096 + s * 1024) : PAST);
+    for (int s = 0; s < 4; ++s) v[s] = fetch16(r, lane * 16, s < steps ? from + (uint32_t)(b * 4096 + s * 1024) : PAST);
   }
   __device__ __forceinline__ pbf16x8 at(int s) const { return __builtin_bit_cast(pbf16x8, v[s]); }
   // as if the steps from `steps` on were zeros (an infinity among what stands in their place would make a NaN)
@@ -246,6 +250,21 @@ __global__ __launch_bounds__(1024) void linear_row_kernel(LinearArgs a, int whol
   if ((lane & 15) == 0 && left > 0) store4<BF16>(a.out, n, acc + bias4(a.bias, n, a.shape.n), left, whole_rows && left >= 4);
 }
 
+// The order of a step's instructions: the first tile widened, then products with the next tile's widening between them (a product keeps the
+// matrix pipe for 16 cycles and the issue for four: what stands between two of them is done meanwhile, behind them it would be waited for)
+template <int FMT, int RT, int MT>
+__device__ __forceinline__ void interleave() {
+  if constexpr (FMT == CS_WEIGHTS_E2M1) {
+    __builtin_amdgcn_sched_group_barrier(0x100, MT, 0);            // reads of LDS
+    __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);               // VALU
+#pragma unroll
+    for (int i = 0; i < RT * MT; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);             // MFMA
+      __builtin_amdgcn_sched_group_barrier(0x2, (6 * (RT - 1) + RT * MT - 1) / (RT * MT), 0);
+    }
+  }
+}
+
 // ---- more rows: four waves share the rows' operands in LDS, and each wave has RT tiles of the weights (and, WM > 1, every WM-th part of
 // the rows).  The rows come in stages of SS steps, NS of them in turn: while one is used, NS - 1 are on their way; the weights, which come from
 // farther, are asked for WD blocks ahead, into registers.  A piece (step, tile of 16 rows) is 1 KB, 64 bytes a row, and neighbouring lanes ask for
@@ -273,13 +292,20 @@ struct Staged {
     Resource rw[RT];
 #pragma unroll
     for (int j = 0; j < RT; ++j) rw[j] = resource(tile[j]);
-    uint32_t offs[XL];
+    Held<FMT> w[WD + 1][RT];
+    auto weights = [&](Held<FMT> (&h)[RT], int b) {
+#pragma unroll
+      for (int j = 0; j < RT; ++j) h[j].fetch(rw[j], blocks, b, lane, b < b1 ? last - 4 * b : 0);
+    };
+#pragma unroll
+    for (int i = 0; i < WD; ++i) weights(w[i], b0 + i);
+    uint32_t offs[XL];                                 // (behind the weights: off may read memory)
     int place[XL];
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
       int u = i * 4 + wave;                            // step u / MT of the stage, tile u % MT
       u = u < UNITS ? u : UNITS - 1;
-      offs[i] = off(u % MT) + (((lane & 3) ^ (lane >> 4)) << 4);
+      offs[i] = off(u % MT) + (((lane & 3) ^ ((lane >> 3) & 3)) << 4);
       place[i] = u;
     }
     auto stage = [&](int first, int slot) {            // the stage from step `first` on, into the slot
@@ -289,18 +315,11 @@ struct Staged {
         fetch_lds16(rx, offs[i], step < last ? (uint32_t)step * 64 : PAST, lds + (slot * UNITS + place[i]) * 1024);
       }
     };
-    Held<FMT> w[WD + 1][RT];
-    auto weights = [&](Held<FMT> (&h)[RT], int b) {
-#pragma unroll
-      for (int j = 0; j < RT; ++j) h[j].fetch(rw[j], blocks, b, lane, b < b1 ? last - 4 * b : 0);
-    };
-#pragma unroll
-    for (int i = 0; i < WD; ++i) weights(w[i], b0 + i);
 #pragma unroll
     for (int i = 0; i < NS - 1; ++i) stage(4 * b0 + i * SS, i);
     __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): all of them, so that the first turns' waits, which count more loads behind, are enough
     int slot = 0, b = b0;
-    const unsigned char* mine = lds + wm * MTW * 1024 + (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) << 4);
+    const unsigned char* mine = lds + wm * MTW * 1024 + (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 1) & 3)) << 4);
     auto block = [&](auto turn) {
       constexpr int R = decltype(turn)::value;
 #pragma unroll
@@ -327,6 +346,7 @@ struct Staged {
 #pragma unroll
             for (int m = 0; m < MTW; ++m) acc[j][m] = mfma(v, f[t & 1][m], acc[j][m]);
           }
+          interleave<FMT, RT, MTW>();
           __builtin_amdgcn_sched_barrier(0);           // (a step's operands are widened in it, not all at once ahead: registers)
         }
         slot = slot + 1 == NS ? 0 : slot + 1;
@@ -725,6 +745,19 @@ __device__ __forceinline__ cf32x4 gated(cf32x4 gate, cf32x4 up) {
   return v;
 }
 
+// Which rows of which expert a workgroup takes, `size` at a time: of its expert's list every gridDim.z-th block; the shared experts, which every row
+// has, are given a workgroup for each block instead (entries of blockIdx.y behind the others').
+struct Share {
+  int e, first, stride;
+};
+__device__ __forceinline__ Share share_of(const MoeArgs& a, int size) {
+  const int y = blockIdx.y, z = blockIdx.z;
+  if (y < a.experts) return {y, z * size, (int)gridDim.z * size};
+  const int blocks = ((int)a.n_rows + size - 1) / size, i = y - a.experts;
+  return {a.experts + i / blocks, z ? 0x7fffffff - 64 : i % blocks * size, blocks * size};
+}
+int share_rows(const MoeArgs& a, int size) { return a.experts + a.shared * (((int)a.n_rows + size - 1) / size); }
+
 // ---- few rows an expert: 16 at a time, straight from memory (direct_product), a workgroup's waves sharing out k.
 // UP: a workgroup takes PAIRS pairs of tiles, gate and up.  ONE: the call has one row, and every workgroup chooses its experts for itself, which
 // is less than a launch.
@@ -736,7 +769,8 @@ __global__ __launch_bounds__(256) void moe_few_up_kernel(MoeArgs a) {
     cf32x4 part[4][2 * PAIRS][64];
   } s;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
-  int e = blockIdx.y, count = 1, cell = blockIdx.y;
+  const Share share = ONE ? Share{0, 0, 16} : share_of(a, 16);
+  int e = share.e, count = 1, cell = blockIdx.y;
   if constexpr (ONE) {
     const bool live = !a.live || a.live[0], writes = blockIdx.x == 0 && blockIdx.y == 0;
     const int slot = blockIdx.y;
@@ -758,7 +792,7 @@ __global__ __launch_bounds__(256) void moe_few_up_kernel(MoeArgs a) {
       __syncthreads();                   // (what follows lies in the same place)
     }
   } else {
-    cell = a.lists[(int64_t)e * a.list_row + min(t, a.list_row - 1)];      // (asked for with the count, used where there is a row)
+    cell = a.lists[(int64_t)e * a.list_row + min(share.first + t, a.list_row - 1)];      // (asked for with the count, used where there is a row)
     count = a.counts[e * COUNT_APART];
   }
   const PackedShape& shape = a.up_shape;
@@ -772,10 +806,10 @@ __global__ __launch_bounds__(256) void moe_few_up_kernel(MoeArgs a) {
     tile[2 * j + 1] = matrix + (int64_t)(pair + pairs) * shape.tile_bytes;
   }
   const int b0 = shape.blocks * wave / 4, b1 = shape.blocks * (wave + 1) / 4;
-  for (int r = 0; r < count; r += 16) {
-    if (r) __syncthreads();
+  for (int r = share.first; r < count; r += share.stride) {
+    if (r != share.first) __syncthreads();
     const bool live = r + t < count;
-    if (r) cell = a.lists[(int64_t)e * a.list_row + min(r + t, count - 1)];
+    if (r != share.first) cell = a.lists[(int64_t)e * a.list_row + min(r + t, count - 1)];
     cf32x4 acc[2 * PAIRS];
 #pragma unroll
     for (int j = 0; j < 2 * PAIRS; ++j) acc[j] = cf32x4{0.f, 0.f, 0.f, 0.f};
@@ -799,8 +833,9 @@ template <int FMT, int RT>
 __global__ __launch_bounds__(256) void moe_few_down_kernel(MoeArgs a) {
   __shared__ cf32x4 part[2][RT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
-  const int e = blockIdx.y, at = (blockIdx.x * 2 + wave / 2) * RT, half = wave & 1;
-  int cell = a.lists[(int64_t)e * a.list_row + min(t, a.list_row - 1)];    // (asked for with the count, used where there is a row)
+  const Share share = share_of(a, 16);
+  const int e = share.e, at = (blockIdx.x * 2 + wave / 2) * RT, half = wave & 1;
+  int cell = a.lists[(int64_t)e * a.list_row + min(share.first + t, a.list_row - 1)];    // (asked for with the count, used where there is a row)
   const int count = a.counts[e * COUNT_APART];
   const PackedShape& shape = a.down_shape;
   const unsigned char* matrix = a.down + (int64_t)e * shape.tiles * shape.tile_bytes;
@@ -808,10 +843,10 @@ __global__ __launch_bounds__(256) void moe_few_down_kernel(MoeArgs a) {
 #pragma unroll
   for (int j = 0; j < RT; ++j) tile[j] = matrix + (int64_t)min(at + j, shape.tiles - 1) * shape.tile_bytes;
   const int b0 = half ? shape.blocks / 2 : 0, b1 = half ? shape.blocks : shape.blocks / 2;
-  for (int r = 0; r < count; r += 16) {
-    if (r) __syncthreads();
+  for (int r = share.first; r < count; r += share.stride) {
+    if (r != share.first) __syncthreads();
     const bool live = r + t < count;
-    if (r) cell = a.lists[(int64_t)e * a.list_row + min(r + t, count - 1)];
+    if (r != share.first) cell = a.lists[(int64_t)e * a.list_row + min(r + t, count - 1)];
     cf32x4 acc[RT];
 #pragma unroll
     for (int j = 0; j < RT; ++j) acc[j] = cf32x4{0.f, 0.f, 0.f, 0.f};
@@ -920,6 +955,11 @@ __global__ __launch_bounds__(1024) void moe_few_sum_kernel(MoeArgs a, int shares
 // The experts' products, rows by their lists, in blocks of up to 64.  UP: tiles come in pairs, gate and up, and h = silu(gate) * up is
 // written; else the parts of y.
 constexpr int EXPERT_LDS = 36864;
+// byte offset of a listed row, of x (UP) or h
+template <bool UP>
+__device__ __forceinline__ uint32_t row_offset(const MoeArgs& a, int cell) {
+  return (UP ? (uint32_t)(cell / a.slots) * (uint32_t)a.x_row : (uint32_t)cell * (uint32_t)a.inter) * 2;
+}
 template <int FMT, bool UP, int MT, int RT, int WD>
 __device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block, const int32_t* list, int rows, unsigned char* lds) {
   constexpr int SS = MT == 4 ? 2 : 4, NS = MT == 4 ? 4 : 3;
@@ -932,20 +972,10 @@ __device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block
   const unsigned char* tile[RT];
 #pragma unroll
   for (int j = 0; j < RT; ++j) tile[j] = matrix + (int64_t)(UP ? min(at + j / 2, pairs - 1) + j % 2 * pairs : min(at + j, shape.tiles - 1)) * shape.tile_bytes;
-  uint32_t offs[MT];
   int cell[MT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    cell[m] = list[min(m * 16 + t, rows - 1)];
-    const int asked = list[min(m * 16 + (lane >> 2), rows - 1)];
-    offs[m] = (UP ? (uint32_t)(asked / a.slots) * (uint32_t)a.x_row : (uint32_t)asked * (uint32_t)a.inter) * 2;
-  }
-  auto off = [&](int m) __attribute__((always_inline)) {
-    uint32_t o = offs[0];
-#pragma unroll
-    for (int i = 1; i < MT; ++i) o = m == i ? offs[i] : o;
-    return o;
-  };
+  for (int m = 0; m < MT; ++m) cell[m] = list[min(m * 16 + t, rows - 1)];
+  auto off = [&](int m) { return row_offset<UP>(a, list[min(m * 16 + (lane >> 2), rows - 1)]); };
   cf32x4 acc[RT][MT];
 #pragma unroll
   for (int j = 0; j < RT; ++j)
@@ -967,16 +997,126 @@ __device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block
 template <int FMT, bool UP, int RT, int WD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) void moe_experts_kernel(MoeArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const int e = blockIdx.y, n_block = blockIdx.x;
+  const Share share = share_of(a, 64);
+  const int e = share.e, n_block = blockIdx.x;
   const int count = a.counts[e * COUNT_APART];
-  for (int r = blockIdx.z * 64; r < count; r += gridDim.z * 64) {
-    if (r >= (int)gridDim.z * 64) __syncthreads();     // (the rows before are still being read)
+  for (int r = share.first; r < count; r += share.stride) {
+    if (r != share.first) __syncthreads();             // (the rows before are still being read)
     const int rows = min(64, count - r);
     const int32_t* list = a.lists + (int64_t)e * a.list_row + r;
     if (rows <= 16) expert_rows<FMT, UP, 1, RT, WD>(a, e, n_block, list, rows, lds);
     else if (rows <= 32) expert_rows<FMT, UP, 2, RT, WD>(a, e, n_block, list, rows, lds);
     else if (rows <= 48) expert_rows<FMT, UP, 3, RT, WD>(a, e, n_block, list, rows, lds);
     else expert_rows<FMT, UP, 4, RT, WD>(a, e, n_block, list, rows, lds);
+  }
+}
+
+// DOWN where the rows of an expert fit LDS whole (inter up to 1152): eight waves read them from there, and each goes through its tiles, four
+// at a time, without a barrier, the weights WD blocks ahead across the tiles' ends.
+constexpr int RESIDENT_BLOCKS = 9;
+template <int FMT, int MT>
+__device__ __forceinline__ void resident_rows(const MoeArgs& a, int e, const int32_t* list, int rows, int tile0, int tile1, unsigned char* lds) {
+  constexpr bool SMALL = FMT == CS_WEIGHTS_E2M1;
+  constexpr int RT = SMALL ? 4 : 2, WD = SMALL ? 3 : 1;
+  const PackedShape& shape = a.down_shape;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
+  const int blocks = shape.blocks, steps = shape.k / 32;
+  const Resource rw = resource(a.down + (int64_t)e * shape.tiles * shape.tile_bytes), rx = resource(a.h);
+  const int total = (tile1 - tile0 + 8 * RT - 1) / (8 * RT) * blocks;          // blocks of all turns of the wave
+  Held<FMT> w[WD + 1][RT];
+  int ahead = 0, ahead_b = 0, ahead_tile = tile0 + wave * RT;
+  auto weights = [&](Held<FMT> (&h)[RT]) {                                     // the next block
+#pragma unroll
+    for (int j = 0; j < RT; ++j)
+      h[j].fetch(rw, blocks, ahead_b, lane, ahead < total && ahead_tile + j < tile1 ? steps - 4 * ahead_b : 0, (uint32_t)(ahead_tile + j) * (uint32_t)shape.tile_bytes);
+    ++ahead;
+    if (++ahead_b == blocks) {
+      ahead_b = 0;
+      ahead_tile += 8 * RT;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < WD; ++i) weights(w[i]);
+  int cell[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) cell[m] = list[min(m * 16 + t, rows - 1)];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const uint32_t off = row_offset<false>(a, list[min(m * 16 + (lane >> 2), rows - 1)]) + (((lane & 3) ^ ((lane >> 3) & 3)) << 4);
+    for (int step = wave; step < 4 * blocks; step += 8) fetch_lds16(rx, off, step < steps ? (uint32_t)step * 64 : PAST, lds + (step * MT + m) * 1024);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0)
+  __syncthreads();
+  const unsigned char* mine = lds + (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 1) & 3)) << 4);
+  cf32x4 acc[RT][MT];
+  auto clear = [&]() {
+#pragma unroll
+    for (int j = 0; j < RT; ++j)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[j][m] = cf32x4{0.f, 0.f, 0.f, 0.f};
+  };
+  clear();
+  int b = 0, tile = tile0 + wave * RT, done = 0;
+  auto block = [&](auto turn) {
+    constexpr int R = decltype(turn)::value;
+    weights(w[(R + WD) % (WD + 1)]);
+    const unsigned char* from = mine + b * 4 * MT * 1024;
+    pbf16x8 f[2][MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) f[0][m] = *reinterpret_cast<const pbf16x8*>(from + m * 1024);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (s < 3) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) f[(s + 1) & 1][m] = *reinterpret_cast<const pbf16x8*>(from + ((s + 1) * MT + m) * 1024);
+      }
+#pragma unroll
+      for (int j = 0; j < RT; ++j) {
+        const pbf16x8 v = w[R][j].at(s);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[j][m] = mfma(v, f[s & 1][m], acc[j][m]);
+      }
+      interleave<FMT, RT, MT>();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (++b == blocks) {
+      if (done < total) {
+#pragma unroll
+        for (int j = 0; j < RT; ++j)
+          if (tile + j < tile1) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+              if (m * 16 + t < rows) store4<false>(a.parts, (int64_t)cell[m] * a.hidden + (tile + j) * 16 + 4 * g, acc[j][m], 4, true);
+          }
+      }
+      clear();
+      b = 0;
+      tile += 8 * RT;
+    }
+    ++done;
+  };
+  while (done < total) {
+    block(step_tag<0>());
+    if constexpr (WD >= 1) block(step_tag<1>());
+    if constexpr (WD >= 2) block(step_tag<2>());
+    if constexpr (WD >= 3) block(step_tag<3>());
+  }
+}
+
+template <int FMT>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void moe_resident_kernel(MoeArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const Share share = share_of(a, 64);
+  const int e = share.e, count = a.counts[e * COUNT_APART], tiles = a.down_shape.tiles;
+  const int tile0 = (int)((int64_t)tiles * blockIdx.x / gridDim.x), tile1 = (int)((int64_t)tiles * (blockIdx.x + 1) / gridDim.x);
+  for (int r = share.first; r < count; r += share.stride) {
+    if (r != share.first) __syncthreads();             // (the rows before are still being read)
+    const int rows = min(64, count - r);
+    const int32_t* list = a.lists + (int64_t)e * a.list_row + r;
+    if (rows <= 16) resident_rows<FMT, 1>(a, e, list, rows, tile0, tile1, lds);
+    else if (rows <= 32) resident_rows<FMT, 2>(a, e, list, rows, tile0, tile1, lds);
+    else if (rows <= 48) resident_rows<FMT, 3>(a, e, list, rows, tile0, tile1, lds);
+    else resident_rows<FMT, 4>(a, e, list, rows, tile0, tile1, lds);
   }
 }
 
@@ -1017,7 +1157,7 @@ size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
 template <int FMT>
 cs_status run_moe(const MoeArgs& a, hipStream_t s) {
-  const int T = (int)a.n_rows, all = a.experts + a.shared;
+  const int T = (int)a.n_rows;
   if (T >= 64) hipLaunchKernelGGL(moe_logits_tile_kernel, dim3((a.experts + 15) / 16, (T + 15) / 16), dim3(1024), 0, s, a);
   else if ((int64_t)T * a.experts <= 1024) hipLaunchKernelGGL((moe_logits_kernel<1>), dim3(a.experts, T), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((moe_logits_kernel<4>), dim3(a.experts, (T + 3) / 4), dim3(256), 0, s, a);
@@ -1027,19 +1167,29 @@ cs_status run_moe(const MoeArgs& a, hipStream_t s) {
   } else {
     hipLaunchKernelGGL(moe_select_kernel, dim3(T), dim3(256), 0, s, a);
     CS_HIP(hipGetLastError());
-    // few rows an expert, on average: 16 at a time
-    if ((int64_t)T * a.top <= 6 * a.experts || T <= 16) {
+    // Few rows an expert and little to read: 16 at a time, straight from memory (24 rows for 24 experts of 1056 x 352: 21 us, staged 27);
+    // where the weights are what takes the time, staged is as fast or faster (128 experts of 2048 x 768: 20 rows 60.5 and 61 us, 96 rows 85 and 79;
+    // 16 of 3584 x 1280 in bf16, 40 rows 117 and 106).
+    if (T <= 16 || ((int64_t)T * a.top <= 6 * a.experts && (int64_t)a.hidden * a.inter * a.experts <= 64 << 20)) {
       constexpr int PAIRS = FMT == CS_WEIGHTS_E2M1 ? 2 : 1;
-      hipLaunchKernelGGL((moe_few_up_kernel<FMT, false, PAIRS>), dim3(a.inter / 16 / PAIRS, all), dim3(256), 0, s, a);
-      if (T > 16) hipLaunchKernelGGL((moe_few_down_kernel<FMT, 2>), dim3((a.hidden / 16 + 3) / 4, all), dim3(256), 0, s, a);
+      const int shares = share_rows(a, 16);
+      hipLaunchKernelGGL((moe_few_up_kernel<FMT, false, PAIRS>), dim3(a.inter / 16 / PAIRS, shares), dim3(256), 0, s, a);
+      if (T > 16) hipLaunchKernelGGL((moe_few_down_kernel<FMT, 2>), dim3((a.hidden / 16 + 3) / 4, shares), dim3(256), 0, s, a);
     } else {
       // workgroups for twice the rows that an expert has on average; those with more take them in turn
-      const int z = (int)std::max<int64_t>(1, std::min<int64_t>((T + 63) / 64, (2ll * T * a.top / a.experts + 63) / 64));
+      const int z = (int)std::max<int64_t>(1, std::min<int64_t>((T + 63) / 64, (2ll * T * a.top / a.experts + 63) / 64)), shares = share_rows(a, 64);
       constexpr bool SMALL = FMT == CS_WEIGHTS_E2M1;           // (bf16 weights: half as many tiles a wave, for the registers)
-      constexpr int RT = SMALL ? 4 : 2, UP_WD = 1, DOWN_WD = SMALL ? 2 : 1;
-      hipLaunchKernelGGL((moe_experts_kernel<FMT, true, RT, UP_WD>), dim3((a.inter / 16 + 2 * RT - 1) / (2 * RT), all, z), dim3(256), EXPERT_LDS, s, a);
+      constexpr int RT = SMALL ? 4 : 2, DOWN_WD = SMALL ? 2 : 1;
+      hipLaunchKernelGGL((moe_experts_kernel<FMT, true, RT, 1>), dim3((a.inter / 16 + 2 * RT - 1) / (2 * RT), shares, z), dim3(256), EXPERT_LDS, s, a);
       CS_HIP(hipGetLastError());
-      hipLaunchKernelGGL((moe_experts_kernel<FMT, false, RT, DOWN_WD>), dim3((a.hidden / 16 + 4 * RT - 1) / (4 * RT), all, z), dim3(256), EXPERT_LDS, s, a);
+      if (a.down_shape.blocks <= RESIDENT_BLOCKS) {
+        const int lds = a.down_shape.blocks * 16384;
+        CS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(moe_resident_kernel<FMT>), hipFuncAttributeMaxDynamicSharedMemorySize, RESIDENT_BLOCKS * 16384));
+        const int parts = std::max(1, std::min((256 + shares * z - 1) / (shares * z), a.down_shape.tiles / (8 * RT)));
+        hipLaunchKernelGGL((moe_resident_kernel<FMT>), dim3(parts, shares, z), dim3(512), lds, s, a);
+      } else {
+        hipLaunchKernelGGL((moe_experts_kernel<FMT, false, RT, DOWN_WD>), dim3((a.hidden / 16 + 4 * RT - 1) / (4 * RT), shares, z), dim3(256), EXPERT_LDS, s, a);
+      }
     }
   }
   CS_HIP(hipGetLastError());
