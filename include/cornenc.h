@@ -448,7 +448,7 @@ cs_status cs_weights_read(const cs_weights_config* config, const void* packed, v
 
 /* out[t, j] = sum_k x[t, k] W[j, k] + bias[j], one matrix (config.matrices == 1).  Exact products of what the weights are held as,
  * sums in fp32, one rounding to out_dtype.  Laid out for up to a few hundred rows and right for any number.
- *  x    dev bf16 rows, at most 2^22 elements apart        out  dev rows of out_dtype (CS_F32 or CS_BF16); out and its rows aligned to an element
+ *  x    dev bf16 rows, at most 2^22 elements apart        out  dev rows of out_dtype (CS_F32 or CS_BF16); out and its rows aligned to an element; it must not overlap x
  *  bias dev fp32 [n] or NULL, 4-byte aligned              workspace  dev, as cs_linear_packed_query reports; contents are scratch
  * Errors (nothing enqueued): CS_ERR_INVALID_ARG, CS_ERR_WORKSPACE, CS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op. */
 cs_status cs_linear_packed_query(const cs_weights_config* config, int64_t n_rows, size_t* workspace_bytes);   /* host-only */

@@ -477,7 +477,7 @@ cs_status run_rows(const LinearArgs& a, int mt, int whole_rows, hipStream_t s) {
   constexpr int WD = FMT == CS_WEIGHTS_E2M1 ? 3 : 1;         // (bf16 weights are four times the registers)
   if (mt == 2) return run_staged<FMT, OUT, 2, 1, 2, 4, 4, WD>(a, whole_rows, s);
   if (mt == 3) return run_staged<FMT, OUT, 3, 1, 2, 4, 4, WD>(a, whole_rows, s);
-  if (mt == 4) return run_staged<FMT, OUT, 4, 1, 2, 2, 6, WD>(a, whole_rows, s);
+  if (mt == 4) return run_staged<FMT, OUT, 4, 1, 2, 4, 3, 1>(a, whole_rows, s);
   return run_staged<FMT, OUT, 8, 1, 2, 2, 4, 1>(a, whole_rows, s);
 }
 // Up to 16 rows.  Waves of about four blocks each; tiles of a workgroup: as many (rows of x are then read once for all of them) as leave
@@ -896,7 +896,7 @@ __global__ __launch_bounds__(1024) void moe_row_sum_kernel(MoeArgs a, int shares
 template <int FMT>
 __global__ __launch_bounds__(1024) void moe_few_sum_kernel(MoeArgs a, int shares) {
   __shared__ cf32x4 part[16][64];
-  __shared__ signed char slot_of[MAX_EXPERTS][16];       // by expert and row: the row's slot, or none
+  __shared__ __attribute__((aligned(16))) signed char slot_of[MAX_EXPERTS][16];       // by expert and row: the row's slot, or none
   __shared__ float weight[16][MAX_TOP];
   __shared__ int used[MAX_EXPERTS], n_used;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;

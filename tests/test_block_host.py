@@ -96,7 +96,10 @@ def test_weights_refusals(read):
     assert st(weights(k=48)) == UNS and st(weights(n=(1 << 24) + 1)) == UNS and st(weights(matrices=1 << 20, n=1 << 24, k=1 << 24)) == UNS
     assert st(dtype=5) == INV and st(w=0) == INV and st(w=8) == INV and st(row=56) == INV and st(row=68) == UNS
     assert st(packed=0) == INV and st(packed=24) == INV and st(matrix=-64) == INV and st(weights(matrices=2), matrix=4100) == UNS
-    if not read:
+    assert st(matrix=0, w=0) == INV
+    if read:
+        assert st(weights(matrices=2), matrix=47 * 64 + 56) == INV and "overlap" in B.last_error()
+    else:
         assert st(err=2) == INV
 
 

@@ -46,6 +46,23 @@ def test_layers(hidden, inter, experts, top, shared, format):
         layer.check(layer.rows(rows), top)
 
 
+# as many experts as there may be, most of them without a row
+@pytest.mark.parametrize("rows", [1, 2, 16, 40, 90])
+def test_many_experts(rows):
+    layer = Layer(64, 32, 1000, 24, "e2m1")
+    layer.check(layer.rows(rows), 32)
+    layer.check(layer.rows(rows), 1, choice_bias=layer.bias)
+
+
+# second products over rows that LDS holds whole, and longer ones
+@pytest.mark.parametrize("format", ["e2m1", "bf16"])
+@pytest.mark.parametrize("inter", [1120, 1152, 1184])
+def test_long_second_products(inter, format):
+    layer = Layer(160, inter, 5, 1, format)
+    for rows in (3, 75, 200):
+        layer.check(layer.rows(rows), 3)
+
+
 # experts with every number of tiles of rows, and more rows than a workgroup takes at once
 @pytest.mark.parametrize("rows", [1, 5, 16, 17, 40, 64, 65, 100, 190, 515])
 def test_rows(rows):
