@@ -645,6 +645,18 @@ _FORMATS = {"e2m1": CS_WEIGHTS_E2M1, "bf16": CS_WEIGHTS_BF16}
 _SCORES = {"softmax": CS_SCORE_SOFTMAX, "sigmoid": CS_SCORE_SIGMOID}
 
 
+_codes = None
+
+
+def _dtype_codes():
+    """torch's types by their codes."""
+    global _codes
+    if _codes is None:
+        import torch
+        _codes = {torch.float32: CS_F32, torch.bfloat16: CS_BF16}
+    return _codes
+
+
 def _named(table, name: str, what: str) -> int:
     if name not in table:
         raise ValueError(f"{what}: expected one of {', '.join(table)}, got {name!r}")
@@ -731,13 +743,12 @@ def cs_weights_read(packed: PackedWeights, dtype=None, out=None, stream=None):
 def cs_linear_packed(x, weights: PackedWeights, bias=None, dtype=None, out=None, workspace=None, stream=None):
     """x [T, k] bf16 times packed weights of one matrix, plus bias (fp32 [n]) -> [T, n] of dtype (bf16 unless given, or out's).  A
     workspace of fewer bytes than needed (or None) is replaced by a new one."""
-    import torch
     if stream is not None:
         with _on(stream):
             return cs_linear_packed(x, weights, bias, dtype, out, workspace)
-    if dtype is None:
-        dtype = torch.bfloat16 if out is None else out.dtype
-    code = CS_BF16 if dtype is torch.bfloat16 else CS_F32 if dtype is torch.float32 else -1
+    if dtype is None and out is not None:
+        dtype = out.dtype
+    code = CS_BF16 if dtype is None else _dtype_codes().get(dtype, -1)
     if code < 0:
         raise TypeError("out must be bf16 or fp32")
     r = _calls().linear_packed(x, *_weights(weights, "weights"), bias, code, out, workspace)
