@@ -181,6 +181,10 @@ def test_more_rows_than_go_together():
     layer.check(x[4000:], 2, got=tuple(g[4000:] for g in got), live=live[4000:])
     tail = B.cs_moe(x[4096:], layer.router, layer.up, layer.down, 2, live=live[4096:])
     assert torch.equal(tail[1], got[1][4096:])
+    # behind the first 4096 a few, one, or none
+    for n in (4096 + 9, 4097, 4096):
+        got = B.cs_moe(x[:n], layer.router, layer.up, layer.down, 2)
+        layer.check(x[4060:n], 2, got=tuple(g[4060:] for g in got))
 
 
 def test_no_rows():
