@@ -756,6 +756,10 @@ __device__ __forceinline__ Share share_of(const MoeArgs& a, int size) {
   const int blocks = ((int)a.n_rows + size - 1) / size, i = y - a.experts;
   return {a.experts + i / blocks, z ? 0x7fffffff - 64 : i % blocks * size, blocks * size};
 }
+// Entry r + lane of an expert's list (whatever lies there, where it has no more rows)
+__device__ __forceinline__ int listed_row(const MoeArgs& a, int e, int r) {
+  return a.lists[(int64_t)e * a.list_row + min(r + (int)(threadIdx.x & 63), a.list_row - 1)];
+}
 int share_rows(const MoeArgs& a, int size) { return a.experts + a.shared * (((int)a.n_rows + size - 1) / size); }
 
 // ---- few rows an expert: 16 at a time, straight from memory (direct_product), a workgroup's waves sharing out k.
@@ -961,7 +965,7 @@ __device__ __forceinline__ uint32_t row_offset(const MoeArgs& a, int cell) {
   return (UP ? (uint32_t)(cell / a.slots) * (uint32_t)a.x_row : (uint32_t)cell * (uint32_t)a.inter) * 2;
 }
 template <int FMT, bool UP, int MT, int RT, int WD>
-__device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block, const int32_t* list, int rows, unsigned char* lds) {
+__device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block, int listed, int rows, unsigned char* lds) {
   constexpr int SS = MT == 4 ? 2 : 4, NS = MT == 4 ? 4 : 3;
   typedef Staged<FMT, MT, 1, RT, SS, NS, WD> P;
   static_assert(P::LDS <= EXPERT_LDS, "what the launch gives");
@@ -974,8 +978,8 @@ __device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block
   for (int j = 0; j < RT; ++j) tile[j] = matrix + (int64_t)(UP ? min(at + j / 2, pairs - 1) + j % 2 * pairs : min(at + j, shape.tiles - 1)) * shape.tile_bytes;
   int cell[MT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) cell[m] = list[min(m * 16 + t, rows - 1)];
-  auto off = [&](int m) { return row_offset<UP>(a, list[min(m * 16 + (lane >> 2), rows - 1)]); };
+  for (int m = 0; m < MT; ++m) cell[m] = __shfl(listed, min(m * 16 + t, rows - 1));
+  auto off = [&](int m) { return row_offset<UP>(a, __shfl(listed, min(m * 16 + (lane >> 2), rows - 1))); };
   cf32x4 acc[RT][MT];
 #pragma unroll
   for (int j = 0; j < RT; ++j)
@@ -999,15 +1003,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const Share share = share_of(a, 64);
   const int e = share.e, n_block = blockIdx.x;
+  int listed = listed_row(a, e, share.first);          // (asked for with the count)
   const int count = a.counts[e * COUNT_APART];
   for (int r = share.first; r < count; r += share.stride) {
-    if (r != share.first) __syncthreads();             // (the rows before are still being read)
+    if (r != share.first) {
+      __syncthreads();                                 // (the rows before are still being read)
+      listed = listed_row(a, e, r);
+    }
     const int rows = min(64, count - r);
-    const int32_t* list = a.lists + (int64_t)e * a.list_row + r;
-    if (rows <= 16) expert_rows<FMT, UP, 1, RT, WD>(a, e, n_block, list, rows, lds);
-    else if (rows <= 32) expert_rows<FMT, UP, 2, RT, WD>(a, e, n_block, list, rows, lds);
-    else if (rows <= 48) expert_rows<FMT, UP, 3, RT, WD>(a, e, n_block, list, rows, lds);
-    else expert_rows<FMT, UP, 4, RT, WD>(a, e, n_block, list, rows, lds);
+    if (rows <= 16) expert_rows<FMT, UP, 1, RT, WD>(a, e, n_block, listed, rows, lds);
+    else if (rows <= 32) expert_rows<FMT, UP, 2, RT, WD>(a, e, n_block, listed, rows, lds);
+    else if (rows <= 48) expert_rows<FMT, UP, 3, RT, WD>(a, e, n_block, listed, rows, lds);
+    else expert_rows<FMT, UP, 4, RT, WD>(a, e, n_block, listed, rows, lds);
   }
 }
 
@@ -1015,7 +1022,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
 // at a time, without a barrier, the weights WD blocks ahead across the tiles' ends.
 constexpr int RESIDENT_BLOCKS = 9;
 template <int FMT, int MT>
-__device__ __forceinline__ void resident_rows(const MoeArgs& a, int e, const int32_t* list, int rows, int tile0, int tile1, unsigned char* lds) {
+__device__ __forceinline__ void resident_rows(const MoeArgs& a, int e, int listed, int rows, int tile0, int tile1, unsigned char* lds) {
   constexpr bool SMALL = FMT == CS_WEIGHTS_E2M1;
   constexpr int RT = SMALL ? 4 : 2, WD = SMALL ? 3 : 1;
   const PackedShape& shape = a.down_shape;
@@ -1039,10 +1046,10 @@ __device__ __forceinline__ void resident_rows(const MoeArgs& a, int e, const int
   for (int i = 0; i < WD; ++i) weights(w[i]);
   int cell[MT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) cell[m] = list[min(m * 16 + t, rows - 1)];
+  for (int m = 0; m < MT; ++m) cell[m] = __shfl(listed, min(m * 16 + t, rows - 1));
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const uint32_t off = row_offset<false>(a, list[min(m * 16 + (lane >> 2), rows - 1)]) + (((lane & 3) ^ ((lane >> 3) & 3)) << 4);
+    const uint32_t off = row_offset<false>(a, __shfl(listed, min(m * 16 + (lane >> 2), rows - 1))) + (((lane & 3) ^ ((lane >> 3) & 3)) << 4);
     for (int step = wave; step < 4 * blocks; step += 8) fetch_lds16(rx, off, step < steps ? (uint32_t)step * 64 : PAST, lds + (step * MT + m) * 1024);
   }
   __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0)
@@ -1107,16 +1114,20 @@ template <int FMT>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void moe_resident_kernel(MoeArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const Share share = share_of(a, 64);
-  const int e = share.e, count = a.counts[e * COUNT_APART], tiles = a.down_shape.tiles;
+  const int e = share.e, tiles = a.down_shape.tiles;
+  int listed = listed_row(a, e, share.first);          // (asked for with the count)
+  const int count = a.counts[e * COUNT_APART];
   const int tile0 = (int)((int64_t)tiles * blockIdx.x / gridDim.x), tile1 = (int)((int64_t)tiles * (blockIdx.x + 1) / gridDim.x);
   for (int r = share.first; r < count; r += share.stride) {
-    if (r != share.first) __syncthreads();             // (the rows before are still being read)
+    if (r != share.first) {
+      __syncthreads();                                 // (the rows before are still being read)
+      listed = listed_row(a, e, r);
+    }
     const int rows = min(64, count - r);
-    const int32_t* list = a.lists + (int64_t)e * a.list_row + r;
-    if (rows <= 16) resident_rows<FMT, 1>(a, e, list, rows, tile0, tile1, lds);
-    else if (rows <= 32) resident_rows<FMT, 2>(a, e, list, rows, tile0, tile1, lds);
-    else if (rows <= 48) resident_rows<FMT, 3>(a, e, list, rows, tile0, tile1, lds);
-    else resident_rows<FMT, 4>(a, e, list, rows, tile0, tile1, lds);
+    if (rows <= 16) resident_rows<FMT, 1>(a, e, listed, rows, tile0, tile1, lds);
+    else if (rows <= 32) resident_rows<FMT, 2>(a, e, listed, rows, tile0, tile1, lds);
+    else if (rows <= 48) resident_rows<FMT, 3>(a, e, listed, rows, tile0, tile1, lds);
+    else resident_rows<FMT, 4>(a, e, listed, rows, tile0, tile1, lds);
   }
 }
 
