@@ -176,7 +176,7 @@ cs_status launch_norm_residual(const NormResidualArgs& args, bool layer, int dty
 
 // ---- weights.  A wave takes a block: 16 rows of 128 values.  Lane l reads the eight values of each step that it will hold as an operand, so
 // that what it writes lies at its own place: 16 bytes a lane of codes, or 16 bytes a step of bf16.  The four lanes of a row share its
-// scales.  Rows of the last tile behind n become zeros.
+// scales.  Rows of the last tile behind n become zeros.  128 matrices of 1536 x 2048 from bf16 (805 MB) into 4 bits: 305 us, 3.3 TB/s; it is done once.
 template <bool BF16, bool E2M1>
 __global__ __launch_bounds__(256) void weights_pack_kernel(PackArgs a) {
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);

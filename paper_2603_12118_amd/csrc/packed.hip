@@ -3,7 +3,11 @@
 // y^T = W x^T with v_mfma_f32_16x16x32_bf16: the weights are the first operand (a lane holds row l % 16, eight values along k), the rows
 // the second (a lane holds row l % 16 of x, the same eight values of k), and a lane ends with four neighbouring columns of one row.
 // Weights come from memory straight into the registers that hold the operand; 4-bit ones are widened there, exactly (a level times a power of two is a
-// bf16 number), so no operand of theirs passes LDS.
+// bf16 number), so no operand of theirs passes LDS.  They are read with plain loads: past the caches the scales, 64 bytes a block, fetched
+// their lines twice (one row of 28672 x 3584, 55 MB: 15.1 us past them, 11.7 through them).
+//
+// What bounds the products: memory up to some 64 rows, with few rows the time that the first load takes; the matrix pipe and the widening beside it
+// from 128 rows on.  Figures: loops of calls on three sets of weights, 4 bits unless said otherwise.
 #include "block.h"
 
 #include <algorithm>
@@ -88,14 +92,6 @@ struct Held<CS_WEIGHTS_BF16> {
 
 template <int S>
 struct step_tag { static constexpr int value = S; };
-// f(step_tag<0>) .. f(step_tag<3>), as many as a block has
-template <class F>
-__device__ __forceinline__ void each_step(int steps, F&& f) {
-  f(step_tag<0>());
-  if (steps > 1) f(step_tag<1>());
-  if (steps > 2) f(step_tag<2>());
-  if (steps > 3) f(step_tag<3>());
-}
 template <class F>
 __device__ __forceinline__ void all_steps(F&& f) {
   f(step_tag<0>());
@@ -106,8 +102,10 @@ __device__ __forceinline__ void all_steps(F&& f) {
 
 __device__ __forceinline__ cf32x4 mfma(pbf16x8 w, pbf16x8 x, cf32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0); }
 
-// ---- up to 16 rows: no LDS on the way in.  acc[j] += blocks [b0, b1) of tile j times x.  xl: the lane's row of x, at 8 (lane / 16); lanes
-// without a row (!live) keep zeros and load nothing.  U blocks are asked for together.
+// ---- up to 16 rows: no LDS on the way in, no barrier.  acc[j] += blocks [b0, b1) of tile j times x.  xl: the lane's row of x, at 8 (lane / 16); lanes
+// without a row (!live) keep zeros and load nothing: lanes of different rows take an address each, and that is what more rows cost.  U blocks are
+// asked for together; the last ones, fewer or with fewer steps, with clamped places and zeros for operands, since a branch between the loads
+// and their use would have them wait in scratch memory.
 template <int FMT, int RT, int U>
 __device__ __forceinline__ void direct_product(cf32x4 (&acc)[RT], const unsigned char* const (&tile)[RT], int blocks, int k, int b0, int b1,
                                                const bf16_t* xl, bool live, int lane) {
@@ -182,7 +180,8 @@ __device__ __forceinline__ cf32x4 bias4(const float* bias, int n, int N) {
   return b;
 }
 
-// A workgroup takes RT tiles of the weights; its waves share out k and their sums are added in LDS, wave by wave.
+// A workgroup takes RT tiles of the weights; its waves share out k and their sums are added in LDS, wave by wave.  28672 x 3584: 2 rows 11.5 us, 8
+// rows 12.2, 16 rows 14.2 (3.9 TB/s); 3584 x 3584 in bf16, 8 rows: 7.0 us (3.7 TB/s).
 template <int FMT, bool BF16, int RT>
 __global__ __launch_bounds__(1024) void linear_direct_kernel(LinearArgs a, int whole_rows) {
   __shared__ cf32x4 part[16][RT][64];
@@ -209,7 +208,8 @@ __global__ __launch_bounds__(1024) void linear_direct_kernel(LinearArgs a, int w
 }
 
 // One row: a wave's part of it waits in LDS as the lanes take it, 16 bytes for each quarter, the same for all 16 columns of the product (of which one
-// is used): no lane is masked and no operand cleared.  A wave writes and reads its own part only.
+// is used): no lane is masked and no operand cleared.  A wave writes and reads its own part only.  28672 x 3584: 10.9 us, 5.0 TB/s (masked lanes,
+// as above: 12.4); reading the weights alone takes 8.2.  4608 x 3584: 4.2 us, a launch and two reads one behind the other.
 template <int FMT, bool BF16>
 __global__ __launch_bounds__(1024) void linear_row_kernel(LinearArgs a, int whole_rows) {
   constexpr int U = FMT == CS_WEIGHTS_E2M1 ? 4 : 2;
@@ -265,16 +265,18 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-// ---- more rows: four waves share the rows' operands in LDS, and each wave has RT tiles of the weights (and, WM > 1, every WM-th part of
-// the rows).  The rows come in stages of SS steps, NS of them in turn: while one is used, NS - 1 are on their way; the weights, which come from
+// ---- more rows: four waves share the rows' operands in LDS, and each wave has RT tiles of the weights.  The rows come in stages of SS steps, NS of them in turn: while one is used, NS - 1 are on their way; the weights, which come from
 // farther, are asked for WD blocks ahead, into registers.  A piece (step, tile of 16 rows) is 1 KB, 64 bytes a row, and neighbouring lanes ask for
 // neighbouring 16 bytes of a row (lanes that ask for different rows take an address each: 16 bytes a clock, not 64).  The four
-// chunks of row t lie turned by t / 4, so that the 16 rows of a chunk are read from different banks.
+// chunks of row t lie turned by t / 2, so that eight rows of a chunk are read from different banks.
 // Both are buffer loads with a bound: what lies behind the last step is asked for behind the bound, and is zeros that cost no memory.  So
 // the number of loads under way is always the same, the waits are constants, and no step of the loop is conditional.
-template <int FMT, int MT, int WM, int RT, int SS, int NS, int WD>
+// 256 rows, 28672 x 3584 (52.6 GFLOP): 46 - 48 us on different cards, 1.1 PFLOP/s, where a library product of 8192^3 in bf16 reaches 1.21.  Of that: rows by an address
+// a lane 62 us to 48; chunks turned by t / 4, which leaves two rows on a bank, 48 to 46; an exit between the blocks of a turn, for which the
+// accumulators were kept twice, 59 to 54 with four tiles a wave.  The matrix pipe is busy for two fifths of the cycles, LDS for one.  Four tiles a wave and
+// one wave a SIMD: 53; the rows shared out to two pairs of waves, which widen twice: 48.  64 rows 18.6 us, 45 rows 16.0, 32 rows 13.1 (4.3 TB/s).
+template <int FMT, int MT, int RT, int SS, int NS, int WD>
 struct Staged {
-  static constexpr int MTW = MT / WM;                  // tiles of rows of a wave
   static constexpr int UNITS = MT * SS;                // pieces of a stage
   static constexpr int XL = (UNITS + 3) / 4;           // loads of a wave for a stage (a wave without a piece fetches one again)
   static constexpr int WL = RT * (FMT == CS_WEIGHTS_E2M1 ? 2 : 4);
@@ -282,11 +284,11 @@ struct Staged {
   static_assert((SS == 2 || SS == 4) && WD <= 3, "what the loop is written for");
   static constexpr int LDS = NS * UNITS * 1024;
 
-  // acc[j][m] += blocks [b0, b1) of tile[j] times tile m of the wave's rows.  All waves of the workgroup call it alike.
+  // acc[j][m] += blocks [b0, b1) of tile[j] times tile m of the rows.  All waves of the workgroup call it alike.
   // off(m): the byte offset from x of row lane / 4 of tile m.
   template <class Off>
-  static __device__ __forceinline__ void product(cf32x4 (&acc)[RT][MTW], const unsigned char* const (&tile)[RT], int blocks, int k, int b0, int b1,
-                                                 const bf16_t* x, Off&& off, unsigned char* lds, int lane, int wave, int wm) {
+  static __device__ __forceinline__ void product(cf32x4 (&acc)[RT][MT], const unsigned char* const (&tile)[RT], int blocks, int k, int b0, int b1,
+                                                 const bf16_t* x, Off&& off, unsigned char* lds, int lane, int wave) {
     const int last = min(4 * b1, k / 32);              // steps
     const Resource rx = resource(x);
     Resource rw[RT];
@@ -319,7 +321,7 @@ struct Staged {
     for (int i = 0; i < NS - 1; ++i) stage(4 * b0 + i * SS, i);
     __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): all of them, so that the first turns' waits, which count more loads behind, are enough
     int slot = 0, b = b0;
-    const unsigned char* mine = lds + wm * MTW * 1024 + (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 1) & 3)) << 4);
+    const unsigned char* mine = lds + (lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 1) & 3)) << 4);
     auto block = [&](auto turn) {
       constexpr int R = decltype(turn)::value;
 #pragma unroll
@@ -331,22 +333,22 @@ struct Staged {
         __builtin_amdgcn_sched_barrier(0);             // (the waits count the weights behind the rows)
         if (i == 0) weights(w[(R + WD) % (WD + 1)], b + WD);
         const unsigned char* from = mine + slot * (UNITS * 1024);
-        pbf16x8 f[2][MTW];
+        pbf16x8 f[2][MT];
 #pragma unroll
-        for (int m = 0; m < MTW; ++m) f[0][m] = *reinterpret_cast<const pbf16x8*>(from + m * 1024);
+        for (int m = 0; m < MT; ++m) f[0][m] = *reinterpret_cast<const pbf16x8*>(from + m * 1024);
 #pragma unroll
         for (int t = 0; t < SS; ++t) {
           if (t + 1 < SS) {
 #pragma unroll
-            for (int m = 0; m < MTW; ++m) f[(t + 1) & 1][m] = *reinterpret_cast<const pbf16x8*>(from + ((t + 1) * MT + m) * 1024);
+            for (int m = 0; m < MT; ++m) f[(t + 1) & 1][m] = *reinterpret_cast<const pbf16x8*>(from + ((t + 1) * MT + m) * 1024);
           }
 #pragma unroll
           for (int j = 0; j < RT; ++j) {
             const pbf16x8 v = w[R][j].at(i * SS + t);
 #pragma unroll
-            for (int m = 0; m < MTW; ++m) acc[j][m] = mfma(v, f[t & 1][m], acc[j][m]);
+            for (int m = 0; m < MT; ++m) acc[j][m] = mfma(v, f[t & 1][m], acc[j][m]);
           }
-          interleave<FMT, RT, MTW>();
+          interleave<FMT, RT, MT>();
           __builtin_amdgcn_sched_barrier(0);           // (a step's operands are widened in it, not all at once ahead: registers)
         }
         slot = slot + 1 == NS ? 0 : slot + 1;
@@ -377,38 +379,38 @@ struct Staged {
   }
 };
 
-template <int FMT, int OUT, int MT, int WM, int RT, int SS, int NS, int WD>      // OUT: 0 fp32, 1 bf16, 2 a part of the sums
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT * MT / WM >= 32 ? 1 : 2, 8))) void linear_staged_kernel(LinearArgs a, int whole_rows) {
-  typedef Staged<FMT, MT, WM, RT, SS, NS, WD> P;
+template <int FMT, int OUT, int MT, int RT, int SS, int NS, int WD>      // OUT: 0 fp32, 1 bf16, 2 a part of the sums
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) void linear_staged_kernel(LinearArgs a, int whole_rows) {
+  typedef Staged<FMT, MT, RT, SS, NS, WD> P;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = lane & 15, g = lane >> 4;
   // workgroups that read the same weights are eight apart: on one XCD, one behind the other
   const int per = 8 * a.m_tiles, group = blockIdx.x / per, in = blockIdx.x % per;
   const int n_block = group * 8 + in % 8, split = blockIdx.y;
   const int64_t m0 = (int64_t)(in / 8) * (MT * 16);
-  const int tile0 = (n_block * (4 / WM) + wn) * RT;
-  if ((n_block * (4 / WM)) * RT >= a.shape.tiles) return;          // (the whole workgroup)
+  const int tile0 = (n_block * 4 + wave) * RT;
+  if (n_block * 4 * RT >= a.shape.tiles) return;          // (the whole workgroup)
   const unsigned char* tile[RT];
 #pragma unroll
   for (int j = 0; j < RT; ++j) tile[j] = a.packed + (int64_t)min(tile0 + j, a.shape.tiles - 1) * a.shape.tile_bytes;
   const bf16_t* x = a.x + m0 * a.x_row;
   const int rows = (int)min((int64_t)(MT * 16), a.n_rows - m0);
   auto off = [&](int m) { return (uint32_t)((int64_t)min(m * 16 + (lane >> 2), rows - 1) * a.x_row * 2); };
-  cf32x4 acc[RT][P::MTW];
+  cf32x4 acc[RT][MT];
 #pragma unroll
   for (int j = 0; j < RT; ++j)
 #pragma unroll
-    for (int m = 0; m < P::MTW; ++m) acc[j][m] = cf32x4{0.f, 0.f, 0.f, 0.f};
+    for (int m = 0; m < MT; ++m) acc[j][m] = cf32x4{0.f, 0.f, 0.f, 0.f};
   const int b0 = split * a.blocks_of_split, b1 = min(a.shape.blocks, b0 + a.blocks_of_split);
-  P::product(acc, tile, a.shape.blocks, a.shape.k, b0, b1, x, off, lds, lane, wave, wm);
+  P::product(acc, tile, a.shape.blocks, a.shape.k, b0, b1, x, off, lds, lane, wave);
 #pragma unroll
   for (int j = 0; j < RT; ++j) {
     const int n = (tile0 + j) * 16 + 4 * g, left = a.shape.n - n;
     const cf32x4 bias = bias4(OUT == 2 ? nullptr : a.bias, n, a.shape.n);
 #pragma unroll
-    for (int m = 0; m < P::MTW; ++m) {
-      const int r = (wm * P::MTW + m) * 16 + t;
+    for (int m = 0; m < MT; ++m) {
+      const int r = m * 16 + t;
       if (r >= rows || left <= 0) continue;
       if constexpr (OUT == 2) store4<false>(a.parts, ((int64_t)split * a.n_rows + m0 + r) * a.shape.n + n, acc[j][m], left, a.shape.n % 4 == 0);
       else store4<OUT == 1>(a.out, (m0 + r) * a.out_row + n, acc[j][m] + bias, left, whole_rows && left >= 4);
@@ -416,7 +418,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RT * MT / W
   }
 }
 
-// out = the sum of the parts, in their order, and the bias; V columns a thread, up to eight parts asked for together
+// out = the sum of the parts, in their order, and the bias; V columns a thread, up to eight parts asked for together.  45 rows of 3584, seven parts:
+// 4.0 us behind 12.5 for the parts.
 template <bool BF16, int V>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs a, int whole_rows) {
   const int64_t total = a.n_rows * a.shape.n, t = blockIdx.x;
@@ -454,19 +457,20 @@ LinearPlan linear_plan(const LinearArgs& a) {
   p.mt = a.n_rows <= 32 ? 2 : a.n_rows <= 48 ? 3 : a.n_rows <= 64 ? 4 : 8;
   p.m_tiles = (int)((a.n_rows + p.mt * 16 - 1) / (p.mt * 16));
   const int64_t groups = (int64_t)p.m_tiles * ((a.shape.n + 127) / 128);
-  // a workgroup for each CU, in whole turns of four blocks
+  // A workgroup for each CU, in whole turns of four blocks (45 rows, 3584 x 14336: 7 parts of 16 blocks 16.0 us, 4 of 28 18.9, 14 of 8 19.4; a part more
+  // costs its writing and reading, one less the time that a wave alone on its SIMD takes for a block)
   const int want = (int)std::max<int64_t>(1, 256 / groups), blocks = a.shape.blocks;
   p.blocks_of_split = std::min(blocks, ((blocks + want - 1) / want + 3) / 4 * 4);
   p.splits = (blocks + p.blocks_of_split - 1) / p.blocks_of_split;
   return p;
 }
 
-template <int FMT, int OUT, int MT, int WM, int RT, int SS, int NS, int WD>
+template <int FMT, int OUT, int MT, int RT, int SS, int NS, int WD>
 cs_status run_staged(const LinearArgs& a, int whole_rows, hipStream_t s) {
-  constexpr int LDS = Staged<FMT, MT, WM, RT, SS, NS, WD>::LDS;
-  const auto kernel = linear_staged_kernel<FMT, OUT, MT, WM, RT, SS, NS, WD>;
+  constexpr int LDS = Staged<FMT, MT, RT, SS, NS, WD>::LDS;
+  const auto kernel = linear_staged_kernel<FMT, OUT, MT, RT, SS, NS, WD>;
   if (LDS > 65536) CS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-  const int cols = (4 / WM) * RT * 16;
+  const int cols = 4 * RT * 16;
   const int64_t n_blocks = (a.shape.n + cols - 1) / cols, grid = (n_blocks + 7) / 8 * 8 * a.m_tiles;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid, (unsigned)a.splits), dim3(256), LDS, s, a, whole_rows);
   CS_HIP(hipGetLastError());
@@ -475,13 +479,14 @@ cs_status run_staged(const LinearArgs& a, int whole_rows, hipStream_t s) {
 template <int FMT, int OUT>
 cs_status run_rows(const LinearArgs& a, int mt, int whole_rows, hipStream_t s) {
   constexpr int WD = FMT == CS_WEIGHTS_E2M1 ? 3 : 1;         // (bf16 weights are four times the registers)
-  if (mt == 2) return run_staged<FMT, OUT, 2, 1, 2, 4, 4, WD>(a, whole_rows, s);
-  if (mt == 3) return run_staged<FMT, OUT, 3, 1, 2, 4, 4, WD>(a, whole_rows, s);
-  if (mt == 4) return run_staged<FMT, OUT, 4, 1, 2, 4, 3, 1>(a, whole_rows, s);
-  return run_staged<FMT, OUT, 8, 1, 2, 2, 4, 1>(a, whole_rows, s);
+  if (mt == 2) return run_staged<FMT, OUT, 2, 2, 4, 4, WD>(a, whole_rows, s);
+  if (mt == 3) return run_staged<FMT, OUT, 3, 2, 4, 4, WD>(a, whole_rows, s);
+  if (mt == 4) return run_staged<FMT, OUT, 4, 2, 4, 3, 1>(a, whole_rows, s);
+  return run_staged<FMT, OUT, 8, 2, 2, 4, 1>(a, whole_rows, s);
 }
 // Up to 16 rows.  Waves of about four blocks each; tiles of a workgroup: as many (rows of x are then read once for all of them) as leave
-// workgroups for the chip.
+// workgroups for the chip.  16 rows by 1 / 2 / 4 tiles, us: 28672 x 3584 26 / 18 / 14, 4608 x 3584 9.2 / 6.4 / 7.3, 3584 x 14336 16 / 17 / 20.  bf16
+// weights, which are four times the bytes and need the registers: one tile (8 rows of 28672: 39 / 41 / 90).
 template <int FMT, bool BF16>
 cs_status run_direct(const LinearArgs& a, int whole_rows, hipStream_t s) {
   const int tiles = a.shape.tiles, blocks = a.shape.blocks;
@@ -541,10 +546,11 @@ cs_status launch_linear_packed(const LinearArgs& a, int out_dtype, void* workspa
 // Numbers between the experts' counts: a line each, since the adds to one line go one behind the other
 constexpr int COUNT_APART = 16;
 
-// Scores of TT rows by EE experts a wave, in fp64: products of two bf16 numbers are exact there and their sum is off by less than any two
-// experts' scores that are not equal are likely to lie apart, so that the choice is that of the definition.  The vector unit's fp64 rate is half its
-// fp32 rate.  Also clears the experts' counts for the launch behind.
-// A workgroup takes an expert and TT rows, its waves pieces of 512 values of k in turn.
+// Scores in fp64: products of two bf16 numbers are exact there and their sum is off by less than any two experts' scores that are not equal
+// are likely to lie apart, so that the choice is that of the definition; in fp32 some hundred rows would have one in which two neighbours change places.
+// Also clears the experts' counts for the launch behind.
+// A workgroup takes an expert and TT rows, its waves pieces of 512 values of k in turn.  One row by 128 experts of 2048: 2.7 us, a launch and a read; 48
+// rows: 5.1 (a wave for four rows and four experts over all of k: 9.6).
 template <int TT>
 __global__ __launch_bounds__(256) void moe_logits_kernel(MoeArgs a) {
   __shared__ double part[4][TT];
@@ -579,7 +585,8 @@ __global__ __launch_bounds__(256) void moe_logits_kernel(MoeArgs a) {
 }
 
 // The same for many rows, 16 of them by 16 experts a workgroup, its 16 waves sharing out k: v_mfma_f64_16x16x4_f64, whose operands a lane
-// widens once for 16 products each.
+// widens once for 16 products each.  512 rows by 128 experts of 2048: 9.5 us, 3.4 of them the matrix pipe's (64 cycles each); four waves, four reads one
+// behind the other: 13; on the vector unit, where widening takes longer than the products, 16.
 typedef double pf64x4 __attribute__((ext_vector_type(4)));
 __global__ __launch_bounds__(1024) void moe_logits_tile_kernel(MoeArgs a) {
   __shared__ double part[16][4][64];
@@ -715,7 +722,8 @@ __device__ __forceinline__ float choose(const MoeArgs& a, int64_t t, Choice& c, 
 }
 
 // A workgroup takes a row.  Rows are entered in the lists of their experts in whatever order the workgroups come: a row's results do
-// not depend on its place in them.
+// not depend on its place in them.  48 rows of 128 experts 5.4 us, 512 rows 7.0: a launch, the scores, three barriers and the add's way there
+// and back, one behind the other.  (Instead of the lists, a map of experts and rows that the products' workgroups search: no faster here, and those lost 3 to 6 us.)
 __global__ __launch_bounds__(256) void moe_select_kernel(MoeArgs a) {
   __shared__ Choice c;
   const int64_t t = blockIdx.x;
@@ -764,7 +772,8 @@ int share_rows(const MoeArgs& a, int size) { return a.experts + a.shared * (((in
 
 // ---- few rows an expert: 16 at a time, straight from memory (direct_product), a workgroup's waves sharing out k.
 // UP: a workgroup takes PAIRS pairs of tiles, gate and up.  ONE: the call has one row, and every workgroup chooses its experts for itself, which
-// is less than a launch.
+// is less than a launch.  8 rows, 16 experts and a shared one of 3584 x 1280 in bf16 (211 MB): 41 us, 5.1 TB/s; one row, 8 of 128 experts of 2048 x
+// 768 (13 MB): 9 us, of which choosing is about half.
 template <int FMT, bool ONE, int PAIRS>
 __global__ __launch_bounds__(256) void moe_few_up_kernel(MoeArgs a) {
   struct Nothing {};
@@ -832,7 +841,8 @@ __global__ __launch_bounds__(256) void moe_few_up_kernel(MoeArgs a) {
   }
 }
 
-// DOWN, rows by their lists, into the parts of y: a workgroup takes 2 RT tiles, two waves to each RT of them
+// DOWN, rows by their lists, into the parts of y: a workgroup takes 2 RT tiles, two waves to each RT of them.  (Four tiles a wave: slower, 77 us to 80 for
+// the layer of 48 rows below.)
 template <int FMT, int RT>
 __global__ __launch_bounds__(256) void moe_few_down_kernel(MoeArgs a) {
   __shared__ cf32x4 part[2][RT][64];
@@ -869,7 +879,8 @@ __global__ __launch_bounds__(256) void moe_few_down_kernel(MoeArgs a) {
   }
 }
 
-// DOWN of one row, the whole sum: a workgroup takes a tile of y, its waves a part along k of a slot's expert each
+// DOWN of one row, the whole sum: a workgroup takes a tile of y, its waves a part along k of a slot's expert each.  8 experts of 768 x 2048 (7 MB): 4.7 us, a
+// launch, the experts' numbers, the weights, one behind the other.
 template <int FMT>
 __global__ __launch_bounds__(1024) void moe_row_sum_kernel(MoeArgs a, int shares) {
   __shared__ cf32x4 part[16][64];
@@ -896,7 +907,7 @@ __global__ __launch_bounds__(1024) void moe_row_sum_kernel(MoeArgs a, int shares
 
 // DOWN of up to 16 rows, the whole sum: a workgroup takes a tile of y and all experts, its waves an expert (or, where there are fewer, a part of one
 // along k) at a time.  A row that the expert was not chosen for has zeros as its operand; its weight multiplies the expert's sum, and the
-// waves' sums are added in LDS, so nothing is written but y.
+// waves' sums are added in LDS, so nothing is written but y.  8 rows, 1280 x 3584 in bf16 (105 MB): 19 - 23 us, 4.6 - 5.5 TB/s.
 template <int FMT>
 __global__ __launch_bounds__(1024) void moe_few_sum_kernel(MoeArgs a, int shares) {
   __shared__ cf32x4 part[16][64];
@@ -957,7 +968,8 @@ __global__ __launch_bounds__(1024) void moe_few_sum_kernel(MoeArgs a, int shares
 }
 
 // The experts' products, rows by their lists, in blocks of up to 64.  UP: tiles come in pairs, gate and up, and h = silu(gate) * up is
-// written; else the parts of y.
+// written; else the parts of y.  128 experts of 2048 x 768 (214 MB), 48 rows: 36 us, 5.9 TB/s; 512 rows: 44 us, where the matrix pipe (30 k cycles a
+// SIMD), widening and what an expert of 48 rows takes longer than one of 32 add up.  Two tiles a wave 52 us, the weights of three blocks ahead 47.
 constexpr int EXPERT_LDS = 36864;
 // byte offset of a listed row, of x (UP) or h
 template <bool UP>
@@ -967,7 +979,7 @@ __device__ __forceinline__ uint32_t row_offset(const MoeArgs& a, int cell) {
 template <int FMT, bool UP, int MT, int RT, int WD>
 __device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block, int listed, int rows, unsigned char* lds) {
   constexpr int SS = MT == 4 ? 2 : 4, NS = MT == 4 ? 4 : 3;
-  typedef Staged<FMT, MT, 1, RT, SS, NS, WD> P;
+  typedef Staged<FMT, MT, RT, SS, NS, WD> P;
   static_assert(P::LDS <= EXPERT_LDS, "what the launch gives");
   const PackedShape& shape = UP ? a.up_shape : a.down_shape;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = lane & 15, g = lane >> 4;
@@ -985,7 +997,7 @@ __device__ __forceinline__ void expert_rows(const MoeArgs& a, int e, int n_block
   for (int j = 0; j < RT; ++j)
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[j][m] = cf32x4{0.f, 0.f, 0.f, 0.f};
-  P::product(acc, tile, shape.blocks, shape.k, 0, shape.blocks, UP ? a.x : a.h, off, lds, lane, wave, 0);
+  P::product(acc, tile, shape.blocks, shape.k, 0, shape.blocks, UP ? a.x : a.h, off, lds, lane, wave);
 #pragma unroll
   for (int j = 0; j < (UP ? RT / 2 : RT); ++j) {
     if (at + j >= (UP ? pairs : shape.tiles)) continue;
@@ -1019,7 +1031,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
 }
 
 // DOWN where the rows of an expert fit LDS whole (inter up to 1152): eight waves read them from there, and each goes through its tiles, four
-// at a time, without a barrier, the weights WD blocks ahead across the tiles' ends.
+// at a time, without a barrier, the weights WD blocks ahead across the tiles' ends.  128 experts of 768 x 2048 (107 MB): 48 rows 22 us, 512 rows 33 (34 MB of
+// parts among it); through stages 23 and 35.  One workgroup an expert 47, four 43: the first costs idle CUs, the other a second round of reading rows.
 constexpr int RESIDENT_BLOCKS = 9;
 template <int FMT, int MT>
 __device__ __forceinline__ void resident_rows(const MoeArgs& a, int e, int listed, int rows, int tile0, int tile1, unsigned char* lds) {
@@ -1131,7 +1144,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
 }
 
-// y of a row: its parts by their weights, in the order of the slots, in fp32; eight parts asked for together
+// y of a row: its parts by their weights, in the order of the slots, in fp32; eight parts asked for together.  512 rows of 8 parts of 2048 (34 MB): 7.0 us.
+// (Parts in bf16 would be half of that and of the second products' writing, at an error of half a step each.)
 __global__ __launch_bounds__(256) void moe_sum_kernel(MoeArgs a) {
   const int64_t t = blockIdx.x;
   const int n = ((int)blockIdx.y * 256 + threadIdx.x) * 4;
