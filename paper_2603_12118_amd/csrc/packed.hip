@@ -547,7 +547,7 @@ cs_status launch_linear_packed(const LinearArgs& a, int out_dtype, void* workspa
 constexpr int COUNT_APART = 16;
 
 // Scores in fp64: products of two bf16 numbers are exact there and their sum is off by less than any two experts' scores that are not equal
-// are likely to lie apart, so that the choice is that of the definition; in fp32 some hundred rows would have one in which two neighbours change places.
+// are likely to lie apart, so that the choice is that of the definition; in fp32 two neighbours would change places in one row of some thousands.
 // Also clears the experts' counts for the launch behind.
 // A workgroup takes an expert and TT rows, its waves pieces of 512 values of k in turn.  One row by 128 experts of 2048: 2.7 us, a launch and a read; 48
 // rows: 5.1 (a wave for four rows and four experts over all of k: 9.6).
