@@ -269,7 +269,7 @@ Call::Rows matrix(const Call& call, const at::Tensor& x, int64_t n, int64_t widt
   if (x.dim() != 2 || x.size(0) != n || x.size(1) != width || x.scalar_type() != type || x.device() != call.device || (n > 0 && width > 1 && x.stride(1) != 1))
     throw Value(std::string(name) + ": expected [" + std::to_string(n) + ", " + std::to_string(width) +
                 "] of its type with consecutive values, on the GPU");
-  return {x.data_ptr(), n > 1 || x.stride(0) >= width ? x.stride(0) : width};
+  return {x.data_ptr(), n > 1 ? x.stride(0) : width};        // (one row lies no distance from another)
 }
 void two(const at::Tensor& x, const char* name) {
   if (x.dim() != 2) throw Value(std::string(name) + ": expected [rows, width]");

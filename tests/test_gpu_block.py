@@ -114,6 +114,46 @@ def test_nan_and_infinity_stay_in_their_row():
     assert got[1][2].isnan().all() and got[1][6].isnan().any() and got[0][6, 5] == float("inf")
 
 
+def test_more_rows_than_a_launch_takes():
+    n = 4_194_303 + 70                                     # of 1024 threads: HIP's limit
+    x, res, g = (torch.randn(n, 8, device=DEV, dtype=torch.bfloat16) for _ in range(2)), None, dev(1 + np.arange(8) / 8)
+    x, res = x
+    r, y = B.cs_norm_residual(x, res, g, post_gain=g)
+    for at in (slice(0, 50), slice(4_194_250, 4_194_350), slice(n - 20, n)):
+        check_norm(dict(x=x[at], residual=res[at], pre_gain=g, post_gain=g), r[at], y[at], "rms", "bf16", "bf16")
+    assert torch.isfinite(y).all()
+
+
+def test_on_another_stream_and_in_a_graph():
+    a = inputs(37, 1024, "bf16", "f32", "row", True, "layer")
+    side = torch.cuda.Stream()
+    r, y = torch.empty_like(a["residual"]), torch.empty_like(a["x"])
+    torch.cuda.synchronize()
+    B.cs_norm_residual(**a, norm="layer", r=r, y=y, stream=side)
+    side.synchronize()
+    check_norm(a, r, y, "layer", "bf16", "f32")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.cs_norm_residual(**a, norm="layer", r=r, y=y)
+    for _ in range(3):
+        a["x"].normal_()
+        a["residual"].normal_()
+        torch.cuda.synchronize()
+        graph.replay()
+        want = B.cs_norm_residual(**a, norm="layer")
+        torch.cuda.synchronize()
+        assert torch.equal(r, want[0]) and torch.equal(y, want[1])
+
+
+def test_one_row_of_a_tensor_whose_rows_lie_anywhere():
+    x, res = torch.randn(3, 68, device=DEV)[1:2, :64], torch.randn(3, 65, device=DEV)
+    g = dev(np.ones(64))
+    r, y = B.cs_norm_residual(x.bfloat16()[:, :64], res[:1, :64], g)          # 260 bytes apart
+    assert r.shape == (1, 64) and torch.isfinite(y).all()
+    with pytest.raises(B.CsError):
+        B.cs_norm_residual(torch.randn(3, 64, device=DEV), res[:, :64], g)
+
+
 def test_no_rows():
     g = dev(np.ones(64))
     r, y = B.cs_norm_residual(torch.zeros(0, 64, device=DEV), torch.zeros(0, 64, device=DEV), g)

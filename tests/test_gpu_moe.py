@@ -54,6 +54,14 @@ def test_many_experts(rows):
     layer.check(layer.rows(rows), 1, choice_bias=layer.bias)
 
 
+# the widest layers that the calls take
+@pytest.mark.parametrize("hidden,inter", [(65536, 32), (64, 65536)])
+@pytest.mark.parametrize("rows", [1, 3, 70])
+def test_widest_layers(hidden, inter, rows):
+    layer = Layer(hidden, inter, 2, 1, "e2m1")
+    layer.check(layer.rows(rows), 1)
+
+
 # second products over rows that LDS holds whole, and longer ones
 @pytest.mark.parametrize("format", ["e2m1", "bf16"])
 @pytest.mark.parametrize("inter", [1120, 1152, 1184])

@@ -49,6 +49,25 @@ def test_long_rows_are_shared_out(rows, format):
     check(x, w, b, format, B.cs_linear_packed(x, p, dtype=torch.float32), "f32")
 
 
+# one row: both sides of what LDS holds of it
+@pytest.mark.parametrize("format", ["e2m1", "bf16"])
+@pytest.mark.parametrize("k", [20448, 20480, 20512])
+def test_longest_rows_in_lds(k, format):
+    x, w, b, p = make(1, 33, k, format)
+    check(x, w, b, format, B.cs_linear_packed(x, p, bias=b, dtype=torch.float32), "f32")
+
+
+@pytest.mark.parametrize("k", [96, 128, 416])
+@pytest.mark.parametrize("rows", [1, 5, 20, 40, 60, 100])
+def test_a_weight_that_is_no_number_leaves_the_other_columns(rows, k):
+    x, w, b, p = make(rows, 83, k, "bf16")
+    want = B.cs_linear_packed(x, p, bias=b)
+    w[3, k - 1], w[82, 0], w[40, k // 2] = float("inf"), float("nan"), -float("inf")
+    got = B.cs_linear_packed(x, B.cs_weights_pack(w, "bf16"), bias=b)
+    ok = [j for j in range(83) if j not in (3, 40, 82)]
+    assert torch.equal(got[:, ok], want[:, ok]) and not got[:, [3, 40, 82]].isfinite().any()
+
+
 @pytest.mark.parametrize("rows", [3, 30, 90])
 def test_rows_apart_and_results_apart(rows):
     for n, gap in ((96, 8), (96, 2), (96, 1), (95, 3)):
