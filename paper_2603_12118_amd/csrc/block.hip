@@ -141,9 +141,6 @@ static void launch_norm_rows(const NormResidualArgs& a, hipStream_t s) {
   const int w = a.width;
   if (w <= 512) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 64, 1>), dim3(quarter), dim3(256), 0, s, a);
   else if (w <= 1024) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 64, 2>), dim3(quarter), dim3(256), 0, s, a);
-#ifdef W64
-  else if (w <= 1536) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 64, 3>), dim3(quarter), dim3(256), 0, s, a);
-#endif
   else if (w <= 2048) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 256, 1>), dim3(rows), dim3(256), 0, s, a);
   else if (w <= 4096) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 256, 2>), dim3(rows), dim3(256), 0, s, a);
   else if (w <= 8192) hipLaunchKernelGGL((norm_residual_kernel<XB, RB, LAYER, 256, 4>), dim3(rows), dim3(256), 0, s, a);

@@ -11,14 +11,10 @@
 #include "block.h"
 
 #include <algorithm>
-#include <stdlib.h>
 #include <type_traits>
 
 #include "rows.h"
 
-#ifndef UWD
-#define UWD 1
-#endif
 namespace cs {
 
 typedef __bf16 pbf16x8 __attribute__((ext_vector_type(8)));
