@@ -57,7 +57,7 @@ struct LinearArgs {
   int64_t n_rows;
   // set by the launcher
   int32_t splits, blocks_of_split, m_tiles;
-  float* parts;             // [splits, n_rows, n]
+  float* parts;             // [splits, n_rows / 16, tiles, 64 lanes, 4]
 };
 cs_status plan_linear_packed(const LinearArgs& a, size_t& bytes);
 cs_status launch_linear_packed(const LinearArgs& a, int out_dtype, void* workspace, hipStream_t s);

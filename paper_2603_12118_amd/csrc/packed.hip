@@ -270,7 +270,8 @@ __device__ __forceinline__ void interleave() {
 // 256 rows, 28672 x 3584 (52.6 GFLOP): 46 - 48 us on different cards, 1.1 PFLOP/s, where a library product of 8192^3 in bf16 reaches 1.21.  Of that: rows by an address
 // a lane 62 us to 48; chunks turned by t / 4, which leaves two rows on a bank, 48 to 46; an exit between the blocks of a turn, for which the
 // accumulators were kept twice, 59 to 54 with four tiles a wave.  The matrix pipe is busy for two fifths of the cycles, LDS for one.  Four tiles a wave and
-// one wave a SIMD: 53; the rows shared out to two pairs of waves, which widen twice: 48.  64 rows 18.6 us, 45 rows 16.0, 32 rows 13.1 (4.3 TB/s).
+// one wave a SIMD: 53; the rows shared out to two pairs of waves, which widen twice: 48.  64 rows 18.6 us, 45 rows 15.9, 32 rows 13.1 (4.3 TB/s); there the
+// loop's instructions take what its reads do: with reads that bring zeros, 45 rows of 3584 x 14336 take 12.2 us of 13.3.
 template <int FMT, int MT, int RT, int SS, int NS, int WD>
 struct Staged {
   static constexpr int UNITS = MT * SS;                // pieces of a stage
@@ -375,6 +376,12 @@ struct Staged {
   }
 };
 
+// The sums of 16 rows by a tile as a wave holds them, 1 KB: by their rows they would be written and read in pieces of 64 bytes (the call of 45 rows
+// by 3584 x 14336, seven parts: 15.9 us to 14.4; 64 rows by 3584 x 3584, 13.3 to 11.1)
+__device__ __forceinline__ cf32x4* part_of(const LinearArgs& a, int split, int m, int tile) {
+  return reinterpret_cast<cf32x4*>(a.parts) + (((int64_t)split * ((a.n_rows + 15) / 16) + m) * a.shape.tiles + tile) * 64;
+}
+
 template <int FMT, int OUT, int MT, int RT, int SS, int NS, int WD>      // OUT: 0 fp32, 1 bf16, 2 a part of the sums
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) void linear_staged_kernel(LinearArgs a, int whole_rows) {
   typedef Staged<FMT, MT, RT, SS, NS, WD> P;
@@ -408,37 +415,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) voi
     for (int m = 0; m < MT; ++m) {
       const int r = m * 16 + t;
       if (r >= rows || left <= 0) continue;
-      if constexpr (OUT == 2) store4<false>(a.parts, ((int64_t)split * a.n_rows + m0 + r) * a.shape.n + n, acc[j][m], left, a.shape.n % 4 == 0);
+      if constexpr (OUT == 2) part_of(a, split, (int)(m0 / 16) + m, tile0 + j)[lane] = acc[j][m];
       else store4<OUT == 1>(a.out, (m0 + r) * a.out_row + n, acc[j][m] + bias, left, whole_rows && left >= 4);
     }
   }
 }
 
-// out = the sum of the parts, in their order, and the bias; V columns a thread, up to eight parts asked for together.  45 rows of 3584, seven parts:
-// 4.0 us behind 12.5 for the parts.
-template <bool BF16, int V>
+// out = the sum of the parts, in their order, and the bias: a wave takes 16 rows by a tile, up to eight parts asked for together.  45 rows of 3584, seven
+// parts: 3.5 - 4.0 us behind 12.5 for the parts.
+template <bool BF16>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs a, int whole_rows) {
-  const int64_t total = a.n_rows * a.shape.n, t = blockIdx.x;
-  const int n = ((int)blockIdx.y * 256 + threadIdx.x) * V;
-  if (n >= a.shape.n) return;
-  const float* from = a.parts + t * a.shape.n + n;
-  typedef float part_t __attribute__((ext_vector_type(V)));
-  part_t v = {};
+  const int lane = threadIdx.x & 63, tile = (int)blockIdx.x * 4 + (threadIdx.x >> 6), m = blockIdx.y;
+  const int64_t t = (int64_t)m * 16 + (lane & 15);
+  const int n = tile * 16 + 4 * (lane >> 4), left = a.shape.n - n;
+  if (left <= 0 || t >= a.n_rows) return;
+  const cf32x4 bias = bias4(a.bias, n, a.shape.n);
+  cf32x4 v = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < a.splits; s0 += 8) {
-    part_t p[8] = {};
+    cf32x4 p[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) p[s] = part_of(a, min(s0 + s, a.splits - 1), m, tile)[lane];
 #pragma unroll
     for (int s = 0; s < 8; ++s)
-      if (s0 + s < a.splits) p[s] = *reinterpret_cast<const part_t*>(from + (s0 + s) * total);
-#pragma unroll
-    for (int s = 0; s < 8; ++s) v += p[s];
+      if (s0 + s < a.splits) v += p[s];
   }
-  if constexpr (V == 4) {
-    store4<BF16>(a.out, t * a.out_row + n, v + bias4(a.bias, n, a.shape.n), 4, whole_rows);
-  } else {
-    const float x = v[0] + (a.bias ? a.bias[n] : 0.f);
-    if constexpr (BF16) static_cast<bf16_t*>(a.out)[t * a.out_row + n] = (bf16_t)pack2_c(x, x);
-    else static_cast<float*>(a.out)[t * a.out_row + n] = x;
-  }
+  store4<BF16>(a.out, t * a.out_row + n, v + bias, left, whole_rows && left >= 4);
 }
 
 namespace {
@@ -453,7 +454,7 @@ LinearPlan linear_plan(const LinearArgs& a) {
   p.mt = a.n_rows <= 32 ? 2 : a.n_rows <= 48 ? 3 : a.n_rows <= 64 ? 4 : 8;
   p.m_tiles = (int)((a.n_rows + p.mt * 16 - 1) / (p.mt * 16));
   const int64_t groups = (int64_t)p.m_tiles * ((a.shape.n + 127) / 128);
-  // A workgroup for each CU, in whole turns of four blocks (45 rows, 3584 x 14336: 7 parts of 16 blocks 16.0 us, 4 of 28 18.9, 14 of 8 19.4; a part more
+  // A workgroup for each CU, in whole turns of four blocks (45 rows, 3584 x 14336: 7 parts of 16 blocks 14.5 us, 6 of 20 15.5, 10 of 12 17.2, 14 of 8 16.4; a part more
   // costs its writing and reading, one less the time that a wave alone on its SIMD takes for a block)
   const int want = (int)std::max<int64_t>(1, 256 / groups), blocks = a.shape.blocks;
   p.blocks_of_split = std::min(blocks, ((blocks + want - 1) / want + 3) / 4 * 4);
@@ -513,12 +514,9 @@ cs_status run_linear(LinearArgs a, int out_dtype, void* workspace, hipStream_t s
   a.parts = static_cast<float*>(workspace);
   if (p.splits == 1) return bf16 ? run_rows<FMT, 1>(a, p.mt, whole, s) : run_rows<FMT, 0>(a, p.mt, whole, s);
   if (cs_status st = run_rows<FMT, 2>(a, p.mt, whole, s)) return st;
-  const bool four = a.shape.n % 4 == 0;
-  const dim3 groups((unsigned)a.n_rows, (unsigned)((a.shape.n + (four ? 1023 : 255)) / (four ? 1024 : 256)));
-  if (four && bf16) hipLaunchKernelGGL((linear_join_kernel<true, 4>), groups, dim3(256), 0, s, a, whole);
-  else if (four) hipLaunchKernelGGL((linear_join_kernel<false, 4>), groups, dim3(256), 0, s, a, whole);
-  else if (bf16) hipLaunchKernelGGL((linear_join_kernel<true, 1>), groups, dim3(256), 0, s, a, whole);
-  else hipLaunchKernelGGL((linear_join_kernel<false, 1>), groups, dim3(256), 0, s, a, whole);
+  const dim3 groups((unsigned)((a.shape.tiles + 3) / 4), (unsigned)((a.n_rows + 15) / 16));
+  if (bf16) hipLaunchKernelGGL((linear_join_kernel<true>), groups, dim3(256), 0, s, a, whole);
+  else hipLaunchKernelGGL((linear_join_kernel<false>), groups, dim3(256), 0, s, a, whole);
   CS_HIP(hipGetLastError());
   return CS_OK;
 }
@@ -530,7 +528,7 @@ cs_status plan_linear_packed(const LinearArgs& a, size_t& bytes) {
   if (a.n_rows <= DIRECT_ROWS) return CS_OK;
   const LinearPlan p = linear_plan(a);
   if ((int64_t)p.m_tiles * ((a.shape.n + 63) / 64 + 8) > 0xffffffffll / 256) return fail(CS_ERR_UNSUPPORTED, "cs_linear_packed: more workgroups than a grid has");
-  if (p.splits > 1) bytes = (size_t)p.splits * a.n_rows * a.shape.n * 4;
+  if (p.splits > 1) bytes = (size_t)p.splits * ((a.n_rows + 15) / 16) * a.shape.tiles * 1024;
   return CS_OK;
 }
 cs_status launch_linear_packed(const LinearArgs& a, int out_dtype, void* workspace, hipStream_t s) {
