@@ -11,6 +11,7 @@
 #include "block.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "rows.h"
@@ -176,8 +177,8 @@ __device__ __forceinline__ cf32x4 bias4(const float* bias, int n, int N) {
   return b;
 }
 
-// A workgroup takes RT tiles of the weights; its waves share out k and their sums are added in LDS, wave by wave.  28672 x 3584: 2 rows 11.5 us, 8
-// rows 12.2, 16 rows 14.2 (3.9 TB/s); 3584 x 3584 in bf16, 8 rows: 7.0 us (3.7 TB/s).
+// A workgroup takes RT tiles of the weights; its waves share out k and their sums are added in LDS, wave by wave.  14336 x 3584: 2 rows 7.9 us,
+// 8 rows 8.8 (3.1 TB/s); 3584 x 3584 in bf16, 8 rows: 7.0 us (3.7 TB/s).
 template <int FMT, bool BF16, int RT>
 __global__ __launch_bounds__(1024) void linear_direct_kernel(LinearArgs a, int whole_rows) {
   __shared__ cf32x4 part[16][RT][64];
@@ -444,14 +445,14 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs a, int whol
 
 namespace {
 
-constexpr int DIRECT_ROWS = 16;
+constexpr int DIRECT_ROWS = 16;        // at most
 
 struct LinearPlan {
   int mt, m_tiles, splits, blocks_of_split;
 };
 LinearPlan linear_plan(const LinearArgs& a) {
   LinearPlan p = {};
-  p.mt = a.n_rows <= 32 ? 2 : a.n_rows <= 48 ? 3 : a.n_rows <= 64 ? 4 : 8;
+  p.mt = a.n_rows <= 16 ? 1 : a.n_rows <= 32 ? 2 : a.n_rows <= 48 ? 3 : a.n_rows <= 64 ? 4 : 8;
   p.m_tiles = (int)((a.n_rows + p.mt * 16 - 1) / (p.mt * 16));
   const int64_t groups = (int64_t)p.m_tiles * ((a.shape.n + 127) / 128);
   // A workgroup for each CU, in whole turns of four blocks (45 rows, 3584 x 14336: 7 parts of 16 blocks 14.5 us, 6 of 20 15.5, 10 of 12 17.2, 14 of 8 16.4; a part more
@@ -460,6 +461,23 @@ LinearPlan linear_plan(const LinearArgs& a) {
   p.blocks_of_split = std::min(blocks, ((blocks + want - 1) / want + 3) / 4 * 4);
   p.splits = (blocks + p.blocks_of_split - 1) / p.blocks_of_split;
   return p;
+}
+
+// Tiles that a workgroup of linear_direct_kernel takes: two (rows of x are then read once for both) where that leaves workgroups for half of the chip (16
+// rows by one / two tiles, us: 4608 x 3584 9.2 / 6.4, 3584 x 14336 16 / 17).  bf16 weights, which are four times the bytes and need the registers: one
+// (8 rows of 28672 x 3584: 39 / 41).
+int direct_tiles(const PackedShape& shape) { return shape.format == CS_WEIGHTS_BF16 || shape.tiles < 256 ? 1 : 2; }
+// Up to 16 rows go straight from memory where k would be split and a CU's workgroups read up to some 100 000 numbers of x between them: below that the joining
+// launch costs more than these reads (straight and staged, us: 14336 x 3584, 8 rows 8.8 and 10.6, 16 rows 11.0 and 11.2; 3584 x 14336, 4 rows 10.2
+// and 10.8, 16 rows 16.8 and 11.0; 1024 x 8192, 8 rows 7.6 and 8.7, 16 rows 10.2 and 8.8).  Where k is not split, staged is as fast from two rows on (28672 x
+// 3584, 2 rows 11.5 and 10.6, 16 rows 14.6 and 10.9; 512 x 512 5.2 and 4.6).  bf16 weights the same, but that staged workgroups beyond one a CU
+// read in too many places at once (100000 x 2048, 2 / 8 / 16 rows 69 / 73 / 90 and 87 / 89 / 90; 28672 x 3584, 16 rows 48.6 and 35.9).
+bool is_direct(const LinearArgs& a, const LinearPlan& staged) {
+  if (a.n_rows == 1 || a.n_rows > DIRECT_ROWS) return a.n_rows == 1;
+  const int tiles = direct_tiles(a.shape);
+  const double read = (double)a.n_rows * a.shape.k * std::max(1., (a.shape.tiles + tiles - 1) / tiles / 256.);
+  if (a.shape.format == CS_WEIGHTS_BF16) return read <= 100e3 * std::max(1., a.shape.tiles / 1024.);
+  return staged.splits > 1 && read <= 100e3;
 }
 
 template <int FMT, int OUT, int MT, int RT, int SS, int NS, int WD>
@@ -476,25 +494,22 @@ cs_status run_staged(const LinearArgs& a, int whole_rows, hipStream_t s) {
 template <int FMT, int OUT>
 cs_status run_rows(const LinearArgs& a, int mt, int whole_rows, hipStream_t s) {
   constexpr int WD = FMT == CS_WEIGHTS_E2M1 ? 3 : 1;         // (bf16 weights are four times the registers)
+  if (mt == 1) return run_staged<FMT, OUT, 1, 2, 4, 4, WD>(a, whole_rows, s);
   if (mt == 2) return run_staged<FMT, OUT, 2, 2, 4, 4, WD>(a, whole_rows, s);
   if (mt == 3) return run_staged<FMT, OUT, 3, 2, 4, 4, WD>(a, whole_rows, s);
   if (mt == 4) return run_staged<FMT, OUT, 4, 2, 4, 3, 1>(a, whole_rows, s);
   return run_staged<FMT, OUT, 8, 2, 2, 4, 1>(a, whole_rows, s);
 }
-// Up to 16 rows.  Waves of about four blocks each; tiles of a workgroup: as many (rows of x are then read once for all of them) as leave
-// workgroups for the chip.  16 rows by 1 / 2 / 4 tiles, us: 28672 x 3584 26 / 18 / 14, 4608 x 3584 9.2 / 6.4 / 7.3, 3584 x 14336 16 / 17 / 20.  bf16
-// weights, which are four times the bytes and need the registers: one tile (8 rows of 28672: 39 / 41 / 90).
+// Waves of about four blocks each.
 template <int FMT, bool BF16>
 cs_status run_direct(const LinearArgs& a, int whole_rows, hipStream_t s) {
   const int tiles = a.shape.tiles, blocks = a.shape.blocks;
-  const bool few = tiles < 1024;
   const int waves = std::min({16, blocks, (blocks + 3) / 4});
   if (a.n_rows == 1 && blocks <= 160) {                      // (40 KB of LDS for the row, beside 16)
     hipLaunchKernelGGL((linear_row_kernel<FMT, BF16>), dim3(tiles), dim3(64 * waves), (size_t)blocks * 256, s, a, whole_rows);
-  } else if (FMT == CS_WEIGHTS_E2M1 && tiles >= 256) {
-    constexpr int MANY = FMT == CS_WEIGHTS_E2M1 ? 4 : 1, SOME = FMT == CS_WEIGHTS_E2M1 ? 2 : 1;
-    if (few) hipLaunchKernelGGL((linear_direct_kernel<FMT, BF16, SOME>), dim3((tiles + 1) / 2), dim3(64 * waves), 0, s, a, whole_rows);
-    else hipLaunchKernelGGL((linear_direct_kernel<FMT, BF16, MANY>), dim3((tiles + 3) / 4), dim3(64 * waves), 0, s, a, whole_rows);
+  } else if (FMT == CS_WEIGHTS_E2M1 && direct_tiles(a.shape) == 2) {
+    constexpr int TWO = FMT == CS_WEIGHTS_E2M1 ? 2 : 1;
+    hipLaunchKernelGGL((linear_direct_kernel<FMT, BF16, TWO>), dim3((tiles + 1) / 2), dim3(64 * waves), 0, s, a, whole_rows);
   } else {
     hipLaunchKernelGGL((linear_direct_kernel<FMT, BF16, 1>), dim3(tiles), dim3(64 * waves), 0, s, a, whole_rows);
   }
@@ -506,8 +521,8 @@ cs_status run_linear(LinearArgs a, int out_dtype, void* workspace, hipStream_t s
   const bool bf16 = out_dtype == CS_BF16;
   const int size = bf16 ? 2 : 4;
   const int whole = ((reinterpret_cast<uintptr_t>(a.out) | (uint64_t)(a.out_row * size)) & (4 * size - 1)) == 0;
-  if (a.n_rows <= DIRECT_ROWS) return bf16 ? run_direct<FMT, true>(a, whole, s) : run_direct<FMT, false>(a, whole, s);
   const LinearPlan p = linear_plan(a);
+  if (is_direct(a, p)) return bf16 ? run_direct<FMT, true>(a, whole, s) : run_direct<FMT, false>(a, whole, s);
   a.m_tiles = p.m_tiles;
   a.splits = p.splits;
   a.blocks_of_split = p.blocks_of_split;
@@ -525,8 +540,8 @@ cs_status run_linear(LinearArgs a, int out_dtype, void* workspace, hipStream_t s
 
 cs_status plan_linear_packed(const LinearArgs& a, size_t& bytes) {
   bytes = 0;
-  if (a.n_rows <= DIRECT_ROWS) return CS_OK;
   const LinearPlan p = linear_plan(a);
+  if (is_direct(a, p)) return CS_OK;
   if ((int64_t)p.m_tiles * ((a.shape.n + 63) / 64 + 8) > 0xffffffffll / 256) return fail(CS_ERR_UNSUPPORTED, "cs_linear_packed: more workgroups than a grid has");
   if (p.splits > 1) bytes = (size_t)p.splits * ((a.n_rows + 15) / 16) * a.shape.tiles * 1024;
   return CS_OK;
@@ -1177,6 +1192,11 @@ size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 template <int FMT>
 cs_status run_moe(const MoeArgs& a, hipStream_t s) {
   const int T = (int)a.n_rows;
+  // Up to 16 rows: the second products and the sum in one launch, unless the experts that have rows are many for its hidden / 16 workgroups (128 experts
+  // of 2048 x 768, 8 a row, in one and in two launches: 4 rows 33.0 and 32.1 us, 8 rows 50.1 and 43.7, 16 rows 69.3 and 57.1; 256 of 512 x 1024, 8 rows 47 and 36; 16
+  // of 3584 x 1280, 8 rows 35.3 and 37.7; 24 of 1056 x 352, 16 rows 21.2 and 23.2)
+  const double used = a.experts * (1 - std::pow(1 - (double)a.top / a.experts, T));
+  const bool at_once = T == 1 || (T <= 16 && used * a.inter * (4096 - a.hidden) <= 50e6);
   if (T >= 64) hipLaunchKernelGGL(moe_logits_tile_kernel, dim3((a.experts + 15) / 16, (T + 15) / 16), dim3(1024), 0, s, a);
   else if ((int64_t)T * a.experts <= 1024) hipLaunchKernelGGL((moe_logits_kernel<1>), dim3(a.experts, T), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((moe_logits_kernel<4>), dim3(a.experts, (T + 3) / 4), dim3(256), 0, s, a);
@@ -1187,13 +1207,13 @@ cs_status run_moe(const MoeArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(moe_select_kernel, dim3(T), dim3(256), 0, s, a);
     CS_HIP(hipGetLastError());
     // Few rows an expert and little to read: 16 at a time, straight from memory (24 rows for 24 experts of 1056 x 352: 21 us, staged 27);
-    // where the weights are what takes the time, staged is as fast or faster (128 experts of 2048 x 768: 20 rows 60.5 and 61 us, 96 rows 85 and 79;
-    // 16 of 3584 x 1280 in bf16, 40 rows 117 and 106).
-    if (T <= 16 || ((int64_t)T * a.top <= 6 * a.experts && (int64_t)a.hidden * a.inter * a.experts <= 64 << 20)) {
+    // where the weights are what takes the time, staged is as fast or faster (us: 128 experts of 2048 x 768, 20 rows 61 and 61, 96 rows 85 and 79; 48 of
+    // 2048 x 1024, 40 rows 50 and 47; but 16 of 3584 x 1280 and a shared one 48 and 54, in bf16 100 and 107).
+    if (T <= 16 || ((int64_t)T * a.top <= 6 * a.experts && (int64_t)a.hidden * a.inter * a.experts <= 80 << 20)) {
       constexpr int PAIRS = FMT == CS_WEIGHTS_E2M1 ? 2 : 1;
       const int shares = share_rows(a, 16);
       hipLaunchKernelGGL((moe_few_up_kernel<FMT, false, PAIRS>), dim3(a.inter / 16 / PAIRS, shares), dim3(256), 0, s, a);
-      if (T > 16) hipLaunchKernelGGL((moe_few_down_kernel<FMT, 2>), dim3((a.hidden / 16 + 3) / 4, shares), dim3(256), 0, s, a);
+      if (!at_once) hipLaunchKernelGGL((moe_few_down_kernel<FMT, 2>), dim3((a.hidden / 16 + 3) / 4, shares), dim3(256), 0, s, a);
     } else {
       // workgroups for twice the rows that an expert has on average; those with more take them in turn
       const int z = (int)std::max<int64_t>(1, std::min<int64_t>((T + 63) / 64, (2ll * T * a.top / a.experts + 63) / 64)), shares = share_rows(a, 64);
@@ -1212,7 +1232,7 @@ cs_status run_moe(const MoeArgs& a, hipStream_t s) {
     }
   }
   CS_HIP(hipGetLastError());
-  if (T <= 16) {
+  if (at_once) {
     // parts of an expert, so that every wave has one where few experts have rows
     const int shares = std::max(1, std::min(a.down_shape.blocks, 16 / std::min(16, T * a.top + a.shared)));
     if (T == 1) hipLaunchKernelGGL((moe_row_sum_kernel<FMT>), dim3(a.hidden / 16), dim3(1024), 0, s, a, std::max(1, std::min(a.down_shape.blocks, 16 / std::min(16, a.slots))));

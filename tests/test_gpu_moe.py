@@ -78,6 +78,15 @@ def test_rows(rows):
     layer.check(layer.rows(rows), 2)
 
 
+# few rows on both sides of where second products and the sum get launches of their own, one of them idle
+@pytest.mark.parametrize("format", ["e2m1", "bf16"])
+@pytest.mark.parametrize("rows", [2, 8, 9, 16])
+def test_few_rows_of_many_experts(rows, format):
+    layer = Layer(96, 352, 64, 1, format)
+    layer.check(layer.rows(rows), 6)
+    layer.check(layer.rows(rows), 6, live=torch.arange(rows, device=DEV) != rows - 2)
+
+
 @pytest.mark.parametrize("format", ["e2m1", "bf16"])
 def test_all_rows_take_the_same_experts(format):
     # 700 rows for two of 32 experts, the average being 44

@@ -49,6 +49,15 @@ def test_long_rows_are_shared_out(rows, format):
     check(x, w, b, format, B.cs_linear_packed(x, p, dtype=torch.float32), "f32")
 
 
+# few rows on both sides of where they are staged
+@pytest.mark.parametrize("format", ["e2m1", "bf16"])
+@pytest.mark.parametrize("rows", [2, 6, 7, 15, 16])
+def test_few_long_rows(rows, format):
+    x, w, b, p = make(rows, 333, 16416, format)
+    for out in ("bf16", "f32"):
+        check(x, w, b, format, B.cs_linear_packed(x, p, bias=b, dtype=TYPES[out]), out)
+
+
 # one row: both sides of what LDS holds of it
 @pytest.mark.parametrize("format", ["e2m1", "bf16"])
 @pytest.mark.parametrize("k", [20448, 20480, 20512])
