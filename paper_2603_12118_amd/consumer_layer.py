@@ -131,7 +131,8 @@ class ConsumerLayer:
 
 
 class ConsumerBlock(ConsumerLayer):
-    """The whole layer.  Rows of the residual stream come in and go out (bf16); a row without a slot goes through no expert."""
+    """The whole layer.  Rows of the residual stream come in and go out (bf16).  A row without a slot, of a sequence that a step leaves out, is not
+    looked at: its stream begins as zeros and goes through no expert, so that without keys to attend to it ends as zeros, whatever x holds there."""
 
     def __init__(self, hidden=3584, inter=1280, experts=16, top=2, shared=1, score="sigmoid", format="e2m1", residual_scale=1.0, block_scale=1.0,
                  post_norms=True, seed=0, device="cuda:0", **attention):
@@ -155,12 +156,14 @@ class ConsumerBlock(ConsumerLayer):
     def forward(self, x, positions, slots, cu, n_keys, table, max_queries, max_keys):
         """Rows of the residual stream x [T, hidden] bf16 -> the stream behind the layer, and the queries and their attention; enqueues only.
         What went through is kept in `stages` until the next call: the layers' inputs and outputs and, as `next`, the stream normed for the next layer."""
+        live = slots >= 0
+        x = torch.where(live[:, None], x, 0)
         _, y = B.cs_norm_residual(x, x, self.attention_gain, block_scale=0.0)
         a, q, attended = super().forward(y, positions, slots, cu, n_keys, table, max_queries, max_keys)
         r, z = B.cs_norm_residual(a, x, self.expert_gain, post_gain=self.post_gains[0], **self.scales)
-        m, experts, weights = B.cs_moe(z, self.router, self.up, self.down, self.top, score=self.score, choice_bias=self.choice_bias, live=slots >= 0)
+        m, experts, weights = B.cs_moe(z, self.router, self.up, self.down, self.top, score=self.score, choice_bias=self.choice_bias, live=live)
         out, following = B.cs_norm_residual(m, r, self.next_gain, post_gain=self.post_gains[1], **self.scales)
-        self.stages = dict(x=x, y=y, a=a, r=r, z=z, live=slots >= 0, m=m, experts=experts, weights=weights, out=out, next=following)
+        self.stages = dict(x=x, y=y, a=a, r=r, z=z, live=live, m=m, experts=experts, weights=weights, out=out, next=following)
         return out, q, attended
 
 

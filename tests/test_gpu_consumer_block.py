@@ -99,3 +99,35 @@ def test_prompts_in_chunks():
             block.prefill([which], [x[first:last]], [pos[first:last]])
             check(block)
     assert block.pages.lens == [120, 120] and block.err.item() == 0
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(post_norms=False, score="softmax", shared=0), dict(format="bf16", residual_scale=0.9, shared=2)])
+def test_rows_of_a_sequence_that_is_left_out_are_zeros_until_take(kw):
+    # whatever stands in its row of x
+    block = small(**kw)
+    pos = torch.as_tensor(prompt_positions([6])[0], device="cuda:0")
+    block.prefill([0, 1, 2], [rows(6, seed=i) for i in range(3)], [pos] * 3)
+    step = DecodeStep(block, [6, 6, 6])
+    stages = dict(block.stages)
+    block.pages.release(1)
+    for i, left in enumerate((0.5, float("nan"), float("inf"), -3e38)):
+        step.x.copy_(rows(3, seed=50 + i))
+        step.x[1] = left
+        kept = step.x.clone()
+        torch.cuda.synchronize()
+        step.run()
+        torch.cuda.synchronize()
+        for name in ("y", "a", "r", "z", "m", "out", "next"):
+            assert not stages[name][1].any(), (name, left)               # (a NaN is not zero either)
+            assert stages[name][[0, 2]].any(-1).all(), name
+        assert not step.out[1].any() and not step.attended[1].any() and step.out.isfinite().all()
+        check(block, {k: v[[0, 2]] for k, v in stages.items()})
+        assert torch.equal(step.x.view(torch.int16), kept.view(torch.int16))      # the caller's rows are left as they are
+    block.prefill([1], [rows(4, seed=60)], [pos[:4]])
+    step.take(1, 4)
+    step.x.copy_(rows(3, seed=61))
+    torch.cuda.synchronize()
+    step.run()
+    torch.cuda.synchronize()
+    assert step.out.any(-1).all()
+    check(block, stages)
