@@ -158,7 +158,8 @@ class ConsumerBlock(ConsumerLayer):
         What went through is kept in `stages` until the next call: the layers' inputs and outputs and, as `next`, the stream normed for the next layer."""
         live = slots >= 0
         x = torch.where(live[:, None], x, 0)
-        _, y = B.cs_norm_residual(x, x, self.attention_gain, block_scale=0.0)
+        # the stream's norm alone: x / 2 + x / 2 is x to the bit, and an infinity stays one (times a block scale of zero it would be a NaN)
+        _, y = B.cs_norm_residual(x, x, self.attention_gain, residual_scale=0.5, block_scale=0.5)
         a, q, attended = super().forward(y, positions, slots, cu, n_keys, table, max_queries, max_keys)
         r, z = B.cs_norm_residual(a, x, self.expert_gain, post_gain=self.post_gains[0], **self.scales)
         m, experts, weights = B.cs_moe(z, self.router, self.up, self.down, self.top, score=self.score, choice_bias=self.choice_bias, live=live)

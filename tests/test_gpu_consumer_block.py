@@ -131,3 +131,17 @@ def test_rows_of_a_sequence_that_is_left_out_are_zeros_until_take(kw):
     torch.cuda.synchronize()
     assert step.out.any(-1).all()
     check(block, stages)
+
+
+def test_an_infinity_in_the_stream_is_normed_as_one():
+    block = small()
+    pos = torch.as_tensor(prompt_positions([5])[0], device="cuda:0")
+    x = rows(5, seed=7)
+    x[1, 3], x[3, 250] = float("inf"), -float("inf")
+    block.prefill([0], [x], [pos])
+    y = host(block.stages["y"])
+    # 1 / sqrt(mean) is zero: a zero for every finite value, a NaN for the infinity
+    with np.errstate(invalid="ignore"):
+        want = O.norm(host(x), "rms", host(block.attention_gain), None, 1e-6)[0]
+    assert np.isnan(want[1, 3]) and np.isnan(want[3, 250]) and np.isnan(want).sum() == 2
+    assert np.array_equal(np.isnan(y), np.isnan(want)) and not y[1, :3].any() and not y[1, 4:].any() and not y[3, :250].any()
