@@ -469,7 +469,7 @@ cs_status cs_linear_packed(const cs_weights_config* config, const void* packed, 
  *  x, y       dev bf16 rows, x's at most 2^17 elements apart; y must not overlap x
  *  router     dev bf16 [n_experts, hidden];  choice_bias dev fp32 [n_experts] or NULL;  live dev uint8 [n_rows] (any alignment) or NULL
  *  experts, weights   dev int32, fp32 [n_rows, top]
- *  workspace  dev, as cs_moe_query reports; contents are scratch
+ *  workspace  dev, as cs_moe_query reports (at most 2 GiB, however many rows there are); contents are scratch
  * Errors (nothing enqueued): CS_ERR_INVALID_ARG, CS_ERR_WORKSPACE, CS_ERR_UNSUPPORTED.  n_rows == 0 is a no-op. */
 typedef enum { CS_SCORE_SOFTMAX = 0, CS_SCORE_SIGMOID = 1 } cs_score;
 typedef struct {

@@ -65,6 +65,7 @@ cs_status launch_linear_packed(const LinearArgs& a, int out_dtype, void* workspa
 constexpr int MAX_TOP = 32;
 constexpr int MAX_EXPERTS = 1024;
 constexpr int64_t MOE_ROWS = 4096;
+constexpr int64_t MOE_WORKSPACE = (int64_t)1 << 31;      // bytes at most
 
 struct MoeArgs {
   const bf16_t* x;

@@ -1181,13 +1181,17 @@ __global__ __launch_bounds__(256) void moe_sum_kernel(MoeArgs a) {
 
 namespace {
 
-// Rows of a call that go through the launches together: they bound the workspace, and the rows of h lie within 32-bit offsets
+size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
+
+// Rows of a call that go through the launches together: as many as MOE_WORKSPACE holds (the counts and the widest row, 26 MB, fit in it), the
+// rows of h within 32-bit offsets.  Each group reads its experts' weights again: 4096 rows of 256 experts of 7168 x 2048 and a shared one, top 8, take 4.48 ms
+// and 1.14 GiB at once, 4.82 in two groups, 5.09 in three, so the bound is one that only wider layers meet.
 int64_t group_rows(const MoeArgs& a) {
-  const int64_t most = std::min<int64_t>(MOE_ROWS, 0x7fffffffll / (2ll * (a.top + a.shared) * a.inter));
+  const int64_t slots = a.top + a.shared, experts = a.experts + a.shared;
+  const int64_t row = 8ll * a.experts + 4 * experts + slots * (2ll * a.inter + 4ll * a.hidden);      // what moe_layout takes for one
+  const int64_t most = std::min<int64_t>({MOE_ROWS, 0x7fffffffll / (2 * slots * a.inter), (MOE_WORKSPACE - experts * COUNT_APART * 4 - 80) / row});
   return std::min(a.n_rows, most);
 }
-
-size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
 template <int FMT>
 cs_status run_moe(const MoeArgs& a, hipStream_t s) {

@@ -199,3 +199,18 @@ def test_the_binding_refuses_what_it_cannot_describe():
             B.cs_moe(x, x, weights, p, 2)
     with pytest.raises(ValueError):
         B.cs_moe(x, x, p, p, 2, score="max")
+
+
+@pytest.mark.parametrize("kw", [dict(hidden=65536, inter=32, n_experts=32, n_shared=32, top=32), dict(hidden=65536, inter=65536, n_experts=32, n_shared=32, top=32),
+                                dict(hidden=32, inter=65536, n_experts=1024, n_shared=32, top=32), dict(hidden=65536, inter=32, n_experts=1024, n_shared=63, top=1),
+                                dict(hidden=7168, inter=2048, n_experts=256, n_shared=1, top=8), dict(hidden=2048, inter=768, n_experts=128, n_shared=0, top=8)])
+def test_moe_workspace_is_bounded(kw):
+    need = C.c_size_t()
+    sizes = []
+    for n in (1, 60, 1000, 4096, 1 << 20, (1 << 31) - 1):
+        assert B.lib().cs_moe_query(C.byref(moe(**kw)), n, C.byref(need)) == 0
+        sizes.append(need.value)
+    assert sizes == sorted(sizes) and sizes[-1] == sizes[-2] == sizes[-3] <= 1 << 31
+    # layers that fit take 4096 rows at once
+    if kw["hidden"] <= 7168 and kw["inter"] <= 2048:
+        assert B.lib().cs_moe_query(C.byref(moe(**kw)), 4095, C.byref(need)) == 0 and need.value < sizes[-1]

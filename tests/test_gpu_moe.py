@@ -1,4 +1,6 @@
 """The mixture-of-experts layer on the GPU, against the CPU oracle."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -208,3 +210,23 @@ def test_no_rows():
     layer = Layer(64, 32, 8, 0, "e2m1")
     y, experts, weights = B.cs_moe(layer.rows(0), layer.router, layer.up, layer.down, 2)
     assert y.shape == (0, 64) and experts.shape == weights.shape == (0, 2)
+
+
+def test_more_rows_than_the_workspace_holds():
+    # a layer so wide that its workspace's bound and not the number of rows ends a group
+    layer = Layer(65536, 32, 2, 14, "bf16")
+    c, need = B.cs_moe_config(C.sizeof(B.cs_moe_config), B.CS_WEIGHTS_BF16, 65536, 32, 2, 14, 2, B.CS_SCORE_SOFTMAX, 1, 1.0), C.c_size_t()
+
+    def size(n):
+        assert B.lib().cs_moe_query(C.byref(c), n, C.byref(need)) == 0
+        return need.value
+    group = next(n for n in range(1, 4096) if size(n) == size(n + 1))
+    assert 64 < group < 4000 and size(group - 1) < size(group) == size(1 << 20) <= 1 << 31
+    x = layer.rows(group + 21)
+    live = torch.arange(len(x), device=DEV) % 7 != 3
+    work = torch.full((size(group),), 255, dtype=torch.uint8, device=DEV)          # NaNs, and no byte more than is asked for
+    for n in (len(x), group + 1, group):
+        got = B.cs_moe(x[:n], layer.router, layer.up, layer.down, 2, live=live[:n], workspace=work)
+        assert got[0].isfinite().all() and not got[0][~live[:n]].any() and got[0][live[:n]].any(-1).all()
+        for at in (slice(0, 3), slice(group - 3, min(n, group + 21))):
+            layer.check(x[:n][at], 2, got=tuple(g[at] for g in got), live=live[:n][at])
