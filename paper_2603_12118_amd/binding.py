@@ -180,6 +180,13 @@ def _check(status: int) -> None:
         raise CsError(status, f"{L.cs_status_string(status).decode()}: {L.cs_last_error().decode()}")
 
 
+def _fits(v: int, bits: int, what: str) -> int:
+    """v, which a structure holds in `bits` bits: ctypes would keep the lower ones of a larger number."""
+    if not -(1 << bits - 1) <= v < 1 << bits - 1:
+        raise ValueError(f"{what}: {v} does not fit {bits} bits")
+    return v
+
+
 def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(np.asarray(a, dtype=np.int32))
 
@@ -697,7 +704,8 @@ def _weights(packed, what: str):
 
 def cs_weights_query(format: str, n: int, k: int, matrices: int = 1) -> int:
     """Host-only: bytes that packed weights take."""
-    c = cs_weights_config(C.sizeof(cs_weights_config), _named(_FORMATS, format, "format"), matrices, n, k)
+    c = cs_weights_config(C.sizeof(cs_weights_config), _named(_FORMATS, format, "format"), _fits(matrices, 64, "matrices"), _fits(n, 32, "n"),
+                          _fits(k, 32, "k"))
     size = C.c_size_t()
     _check(lib().cs_weights_query(C.byref(c), C.byref(size)))
     return size.value

@@ -214,3 +214,10 @@ def test_moe_workspace_is_bounded(kw):
     # layers that fit take 4096 rows at once
     if kw["hidden"] <= 7168 and kw["inter"] <= 2048:
         assert B.lib().cs_moe_query(C.byref(moe(**kw)), 4095, C.byref(need)) == 0 and need.value < sizes[-1]
+
+
+@pytest.mark.parametrize("args", [("e2m1", (1 << 32) + 48, 64), ("e2m1", 48, (1 << 32) + 64), ("bf16", -(1 << 32) + 48, 64), ("e2m1", 48, 64, (1 << 64) + 1),
+                                  ("bf16", 1 << 31, 64)])
+def test_sizes_that_do_not_fit_are_refused(args):
+    with pytest.raises(ValueError, match="does not fit"):
+        B.cs_weights_query(*args)
