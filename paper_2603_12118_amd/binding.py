@@ -597,7 +597,8 @@ def cs_qk_norm_rope(q, k, cos_sin, positions, sections, q_gain=None, k_gain=None
 
 def cs_cache_query(n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int = 1):
     """Host-only: (bytes of a page, bytes of the pool).  A pool is a uint8 tensor [n_pages, page bytes]."""
-    c = cs_cache_config(C.sizeof(cs_cache_config), n_kv_heads, head_dim, page_tokens, n_pages)
+    c = cs_cache_config(C.sizeof(cs_cache_config), _fits(n_kv_heads, 32, "n_kv_heads"), _fits(head_dim, 32, "head_dim"),
+                        _fits(page_tokens, 32, "page_tokens"), _fits(n_pages, 64, "n_pages"))
     page, pool = C.c_size_t(), C.c_size_t()
     _check(lib().cs_cache_query(C.byref(c), C.byref(page), C.byref(pool)))
     return page.value, pool.value

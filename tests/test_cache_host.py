@@ -214,3 +214,9 @@ def test_the_binding_refuses_what_it_cannot_describe():
         B.cs_attention_cache(x.float(), pool, slots, slots, slots, 1, 1, 2, 32)
     with pytest.raises(ValueError):
         B.cs_qk_norm_rope(x, x[:3], torch.zeros(4, 64, 2), slots, (64,))
+
+
+def test_sizes_of_a_cache_that_do_not_fit_are_refused():
+    for args in (((1 << 32) + 2, 128, 32), (2, (1 << 32) + 128, 32), (2, 128, (1 << 32) + 32), (2, 128, 32, (1 << 64) + 5), (2, 128, 1 << 31)):
+        with pytest.raises(ValueError, match="does not fit"):
+            B.cs_cache_query(*args)
