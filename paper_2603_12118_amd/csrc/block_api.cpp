@@ -203,7 +203,8 @@ cs_status cs_weights_read(const cs_weights_config* config, const void* packed, v
                           void* stream) try {
   PackArgs a = {};
   if (cs_status st = weights("cs_weights_read", config, w, w_row, w_matrix, dtype, packed, nullptr, a)) return st;
-  if (config->matrices > 1 && w_matrix < (config->n - 1) * w_row + config->k) return invalid("cs_weights_read", "matrices overlap");
+  // (the last row's place in 128 bits: 2^24 rows of 2^40 values pass 64)
+  if (config->matrices > 1 && w_matrix < (__int128)(config->n - 1) * w_row + config->k) return invalid("cs_weights_read", "matrices overlap");
   return launch_weights_read(a, dtype, static_cast<hipStream_t>(stream));
 }
 CS_CATCH_ALL("cs_weights_read")

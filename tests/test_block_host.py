@@ -221,3 +221,11 @@ def test_moe_workspace_is_bounded(kw):
 def test_sizes_that_do_not_fit_are_refused(args):
     with pytest.raises(ValueError, match="does not fit"):
         B.cs_weights_query(*args)
+
+
+def test_overlapping_matrices_of_far_rows_are_refused():
+    # (n - 1) w_row is past 64 bits
+    c = weights(matrices=2, n=1 << 24)
+    st = lambda row, matrix: B.lib().cs_weights_read(C.byref(c), 512, 256, row, matrix, B.CS_BF16, None)
+    assert st(1 << 40, 1 << 50) == INV and "overlap" in B.last_error()
+    assert st(1 << 39, 1 << 50) == INV and "overlap" in B.last_error()
