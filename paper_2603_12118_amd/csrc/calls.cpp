@@ -412,7 +412,7 @@ PyObject* weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int code = dtype_code(w);
     if (w.dim() != 3 || w.size(0) != c.matrices || w.size(1) != c.n || w.size(2) != c.k || (c.k > 1 && w.stride(2) != 1) || w.stride(0) < 0)
       throw Value("w: expected [matrices, n, k] with consecutive values");
-    const int64_t row = c.n > 1 || w.stride(1) >= c.k ? w.stride(1) : c.k;
+    const int64_t row = c.n > 1 ? w.stride(1) : c.k;           // (one row lies no distance from another)
     void* flag = call.optional(a[7], at::kInt, 1, "err_flag");
     const int st = truth(a[6]) ? cs_weights_read(&c, packed, w.data_ptr(), row, w.stride(0), code, call.stream())
                                : cs_weights_pack(&c, w.data_ptr(), row, w.stride(0), code, packed, static_cast<int32_t*>(flag), call.stream());

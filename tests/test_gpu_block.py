@@ -187,6 +187,20 @@ def test_one_matrix_may_come_without_its_dimension():
     assert torch.equal(B.cs_weights_pack(w).data, B.cs_weights_pack(w[None]).data)
 
 
+@pytest.mark.parametrize("format", ["e2m1", "bf16"])
+def test_matrices_of_one_row_that_lie_anywhere(format):
+    # one row lies no distance from another: 67 values between rows that there are none of
+    w = torch.randn(3, 67, device=DEV)[:1, :64]
+    p = B.cs_weights_pack(w, format)
+    assert torch.equal(p.data, B.cs_weights_pack(w.contiguous(), format).data)
+    into = torch.full((1, 2, 67), 5.0, device=DEV)
+    B.cs_weights_read(p, out=into[:, :1, :64])
+    assert torch.equal(into[:, :1, :64], B.cs_weights_read(p, torch.float32)) and (into[:, 1] == 5).all() and (into[:, :, 64:] == 5).all()
+    three = torch.randn(3, 1, 72, device=DEV)[:, :, :64]
+    p = B.cs_weights_pack(three, format)
+    assert torch.equal(p.data, B.cs_weights_pack(three.contiguous(), format).data)
+
+
 def test_non_finite_weights_set_the_flag():
     w = torch.randn(2, 20, 64, device=DEV)
     w[1, 3, 4], w[0, 19, 63], w[0, 0, 0] = float("nan"), float("inf"), -float("inf")
