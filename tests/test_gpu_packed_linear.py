@@ -42,6 +42,19 @@ def test_many_columns(rows, format):
             check(x, w, b, format, B.cs_linear_packed(x, p, bias=b, dtype=TYPES[out]), out)
 
 
+# two tiles of columns a workgroup, straight from memory (4 bits, 256 tiles and more, k that would be split): an odd number of tiles, columns that end
+# inside the first and the second tile of a workgroup, k that ends inside a block; with one row, k beyond what LDS holds of it
+@pytest.mark.parametrize("rows,n,k", [(rows, n, k) for rows in (2, 5, 16) for n in (4099, 4112, 4115, 4128) for k in (672, 1184)] +
+                         [(1, n, 20512) for n in (4099, 4115)])
+def test_two_tiles_of_columns_a_workgroup(rows, n, k):
+    x, w, b, p = make(rows, n, k, "e2m1")
+    for out in ("bf16", "f32"):
+        y = apart(torch.zeros(rows, n, dtype=TYPES[out], device=DEV), 5)
+        B.cs_linear_packed(x, p, bias=b, out=y)
+        check(x, w, b, "e2m1", y, out)
+        assert (y._base[:, n:] == 7).all()
+
+
 @pytest.mark.parametrize("format", ["e2m1", "bf16"])
 @pytest.mark.parametrize("rows", [1, 5, 20, 40, 100])
 def test_long_rows_are_shared_out(rows, format):
