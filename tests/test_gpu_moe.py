@@ -230,3 +230,21 @@ def test_more_rows_than_the_workspace_holds():
         assert got[0].isfinite().all() and not got[0][~live[:n]].any() and got[0][live[:n]].any(-1).all()
         for at in (slice(0, 3), slice(group - 3, min(n, group + 21))):
             layer.check(x[:n][at], 2, got=tuple(g[at] for g in got), live=live[:n][at])
+
+
+# A row's bits do not depend on the rows beside it, while the call takes the same launches: rows in another order, and fewer of them, so that lists
+# end inside 16, 32, 48 and 64 rows.  Second products whole in LDS, through stages, and few rows straight from memory.
+@pytest.mark.parametrize("format", ["e2m1", "bf16"])
+@pytest.mark.parametrize("hidden,inter,experts,top,shared,counts", [(512, 96, 16, 4, 1, (200, 193, 177, 150, 131, 64)), (160, 1184, 5, 2, 1, (190, 170, 143, 100, 70)),
+                                                                    (96, 352, 200, 10, 0, (110, 97, 83, 64)), (96, 352, 64, 3, 1, (60, 41, 17))])
+def test_rows_have_the_same_bits_beside_other_rows(hidden, inter, experts, top, shared, counts, format):
+    layer = Layer(hidden, inter, experts, shared, format)
+    x = layer.rows(counts[0])
+    first = B.cs_moe(x, layer.router, layer.up, layer.down, top)
+    layer.check(x, top, got=first)
+    for n in counts:
+        for seed in range(3):
+            rows = torch.from_numpy(np.random.default_rng(seed + n).permutation(counts[0])[:n]).to(DEV)
+            got = B.cs_moe(x[rows], layer.router, layer.up, layer.down, top)
+            for a, b, name in zip(first, got, ("y", "experts", "weights")):
+                assert torch.equal(a[rows], b), (n, seed, name)
