@@ -484,7 +484,7 @@ template <int FMT, int OUT, int MT, int RT, int SS, int NS, int WD>
 cs_status run_staged(const LinearArgs& a, int whole_rows, hipStream_t s) {
   constexpr int LDS = Staged<FMT, MT, RT, SS, NS, WD>::LDS;
   const auto kernel = linear_staged_kernel<FMT, OUT, MT, RT, SS, NS, WD>;
-  if (LDS > 65536) CS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+  static_assert(LDS <= 65536, "what a launch may have unasked");
   const int cols = 4 * RT * 16;
   const int64_t n_blocks = (a.shape.n + cols - 1) / cols, grid = (n_blocks + 7) / 8 * 8 * a.m_tiles;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid, (unsigned)a.splits), dim3(256), LDS, s, a, whole_rows);
