@@ -392,8 +392,9 @@ cs_status cs_attention_cache(const cs_cache_config* config, const void* pool, co
                              size_t workspace_bytes, int32_t* err_flag, void* stream);
 
 /* ---- the LLM task's layer behind its attention -------------------------------------------------------------------
- * What one of the LLM task's layers does with the attention's output: a norm before and after each block, and the block,
- * dense or a mixture of experts, on the few rows of a decode step, on batches of them and on chunks of a prompt.
+ * What one of the LLM task's layers does with the attention's output: a norm before and after each block, and the block, a mixture
+ * of experts (of a dense block the products; what stands between them is the caller's), on the few rows of a decode step, on
+ * batches of them and on chunks of a prompt.
  *
  *   cs_norm_residual    the residual stream takes a block's output and the next block's input is normed from it
  *   cs_weights_pack     weights laid out once, in 4 bits or bf16; cs_weights_read: the values they are held as

@@ -12,9 +12,9 @@ namespace cs {
 // read once, r and y written once, and the two means (or means and variances, deviations from the mean, not differences of squares) are
 // sums over the lanes in between.  Rows are independent, so r may lie on the residual and y on x.
 // Bound by memory: 16384 rows of 3584, bf16 with an fp32 residual and a gate a row (822 MB), 149 us, 5.5 TB/s; by latency below some
-// 1000 rows: one row 3.3 us, a launch, the reads and two sums one behind the other.  Asking for the gains with the rows instead of in front of
+// 1000 rows: one row 2.9 us, a launch, the reads and two sums one behind the other.  Asking for the gains with the rows instead of in front of
 // each sum took 153 us to 149, storing past the caches 158 to 153 (1125 rows of 1280, fp32: 7.5 to 6.4), reading past them
-// loses (159; 7.8).  A wave a row, which needs no barrier, is slower from 1280 values on (1125 rows: 10.3 us).
+// loses (159; 7.8).  Rows of 8192 in four pieces a lane and of 16384 in 1024 lanes: 4096 of them in bf16 60 and 118 us, 4.5 TB/s.  A wave a row, which needs no barrier, is slower from 1280 values on (1125 rows: 10.3 us).
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* shared, int& turn) {
   v = wave_sum(v);
@@ -173,7 +173,8 @@ cs_status launch_norm_residual(const NormResidualArgs& args, bool layer, int dty
 
 // ---- weights.  A wave takes a block: 16 rows of 128 values.  Lane l reads the eight values of each step that it will hold as an operand, so
 // that what it writes lies at its own place: 16 bytes a lane of codes, or 16 bytes a step of bf16.  The four lanes of a row share its
-// scales.  Rows of the last tile behind n become zeros.  128 matrices of 1536 x 2048 from bf16 (805 MB) into 4 bits: 305 us, 3.3 TB/s; it is done once.
+// scales.  Rows of the last tile behind n become zeros.  128 matrices of 1536 x 2048 from bf16 (805 MB) into 4 bits:
+// 265 - 305 us, 3.3 - 3.8 TB/s, into bf16 396, 4.1 TB/s, and read back 213 and 338; it is done once.
 template <bool BF16, bool E2M1>
 __global__ __launch_bounds__(256) void weights_pack_kernel(PackArgs a) {
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);

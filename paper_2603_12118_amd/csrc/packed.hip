@@ -6,8 +6,8 @@
 // bf16 number), so no operand of theirs passes LDS.  They are read with plain loads: past the caches the scales, 64 bytes a block, fetched
 // their lines twice (one row of 28672 x 3584, 55 MB: 15.1 us past them, 11.7 through them).
 //
-// What bounds the products: memory up to some 64 rows, with few rows the time that the first load takes; the matrix pipe and the widening beside it
-// from 128 rows on.  Figures: loops of calls on three sets of weights, 4 bits unless said otherwise.
+// What bounds the products: memory up to some 32 rows, with few rows the time that the first load takes; from there on the instructions of the loop, of
+// which from 128 rows the matrix pipe's and the widening beside them are most.  Figures: loops of calls on three sets of weights, 4 bits unless said otherwise.
 #include "block.h"
 
 #include <algorithm>
@@ -755,6 +755,9 @@ __global__ __launch_bounds__(256) void moe_select_kernel(MoeArgs a) {
   a.lists[(int64_t)e * a.list_row + atomicAdd(a.counts + e * COUNT_APART, 1)] = (int32_t)(t * a.slots + tid);
 }
 
+// silu(gate) up, fp32.  It is written in bf16, the type of the second products' operand, half a step of 2^-8 each: y is then off by 0.0023 - 0.0024 of
+// its norm (one row to 512), where fp32 or two bf16 parts of it leave 0.0016 - 0.0017, y's own rounding.  Two parts would be twice the second products' matrix
+// instructions and twice the rows that they read.
 __device__ __forceinline__ cf32x4 gated(cf32x4 gate, cf32x4 up) {
   cf32x4 v;
 #pragma unroll
@@ -850,8 +853,7 @@ __global__ __launch_bounds__(256) void moe_few_up_kernel(MoeArgs a) {
   }
 }
 
-// DOWN, rows by their lists, into the parts of y: a workgroup takes 2 RT tiles, two waves to each RT of them.  (Four tiles a wave: slower, 77 us to 80 for
-// the layer of 48 rows below.)
+// DOWN, rows by their lists, into the parts of y: a workgroup takes 2 RT tiles, two waves to each RT of them.
 template <int FMT, int RT>
 __global__ __launch_bounds__(256) void moe_few_down_kernel(MoeArgs a) {
   __shared__ cf32x4 part[2][RT][64];
@@ -916,7 +918,7 @@ __global__ __launch_bounds__(1024) void moe_row_sum_kernel(MoeArgs a, int shares
 
 // DOWN of up to 16 rows, the whole sum: a workgroup takes a tile of y and all experts, its waves an expert (or, where there are fewer, a part of one
 // along k) at a time.  A row that the expert was not chosen for has zeros as its operand; its weight multiplies the expert's sum, and the
-// waves' sums are added in LDS, so nothing is written but y.  8 rows, 1280 x 3584 in bf16 (105 MB): 19 - 23 us, 4.6 - 5.5 TB/s.
+// waves' sums are added in LDS, so nothing is written but y.  (Which wave has an expert depends on the others that have rows: so does the order of a row's sum.)  8 rows, 1280 x 3584 in bf16 (105 MB): 19 - 23 us, 4.6 - 5.5 TB/s.
 template <int FMT>
 __global__ __launch_bounds__(1024) void moe_few_sum_kernel(MoeArgs a, int shares) {
   __shared__ cf32x4 part[16][64];
